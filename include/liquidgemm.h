@@ -255,6 +255,96 @@ int w4a8_quantize_activations(int M, int K, const uint16_t *X_f16, const float *
                               int8_t *X_i8, float *act_scales, void *hip_stream);
 
 /* ------------------------------------------------------------------------------------
+ * Attention (device): what stands between the qkv projection and the output projection of a decoder layer, with a cache of
+ * keys and values in 4 bits.  Rotary positions with the norms of queries and keys, the cache written, read back and attended
+ * to, attention over whole prompts.
+ *
+ *   - Elements are FP16 (LQ_F16) or BF16 (LQ_BF16); everything in between is FP32.  Heads have 64 or 128 elements.
+ *   - q, k, v are [tokens, heads, head_dim] with strides of their own (in elements, multiples of 8) for tokens and heads, so
+ *     that they can be views of the projection's output; a head's elements are consecutive.  Results without strides are
+ *     contiguous.  Device pointers are 16-byte aligned, those of integers 4-byte.
+ *   - The cache is num_pages pages of kv4_page_bytes() each, 16-byte aligned, num_pages * page_size < 2^31; a slot is
+ *     page * page_size + place in the page.  A page holds, for each kv head, P = page_size tokens in P * (head_dim + 8) bytes:
+ *       P * head_dim/2   key codes, token by token, element 2i in the low half of byte i
+ *       P * head_dim/2   value codes: for every four tokens 16 column groups of head_dim/16 elements, in each the token pairs
+ *                        (0, 1) and (2, 3), in each pair four elements at a time: two bytes of its first token, two of its second
+ *       4 P, 4 P         a word for each token's keys, and for its values: bits of the FP32 scale, whose low 12 are zero, with
+ *                        the zero point in the low 4
+ *     A vector x (a token's keys or values of one head) is stored as
+ *       lo = min(0, x), hi = max(0, x);  s = (hi - lo) / 15 rounded to 12 significant bits (ties to even), at least 2^-100;
+ *       z = rint(-lo / s);  code = clamp(rint(x / s) + z, 0, 15);  it stands for (code - z) * s
+ *     and is determined bit for bit.  A vector with an element that is not finite (or whose range overflows) stands for NaN.
+ * ------------------------------------------------------------------------------------ */
+
+#define LQ_F16 0
+#define LQ_BF16 1
+
+/* Host.  table [max_positions][rot_dim] FP32 for attn_qk_norm_rope: row p holds the cosines of p * f_i, then the sines, i < rot_dim/2,
+ * f_i = base^(-2i / rot_dim), computed in FP64 and rounded once.  `scaling` stretches the positions that a model was trained on:
+ *   LQ_ROPE_PLAIN    as above (factor and original_positions are not used)
+ *   LQ_ROPE_LINEAR   f_i / factor
+ *   LQ_ROPE_NTK      base * factor^(rot_dim / (rot_dim - 2)) in place of base
+ *   LQ_ROPE_YARN     f_i where a pair turns 32 times or more within original_positions, f_i / factor where once or less, in between
+ *                    a mixture, linear in i; cosines and sines times 0.1 ln(factor) + 1
+ * factor >= 1; rot_dim a multiple of 16 up to 1024 (NTK: at least 16); base > 1. */
+#define LQ_ROPE_PLAIN 0
+#define LQ_ROPE_LINEAR 1
+#define LQ_ROPE_NTK 2
+#define LQ_ROPE_YARN 3
+int attn_rope_table(int max_positions, int rot_dim, double base, int scaling, double factor, int original_positions, float *table);
+
+/* Norm (where the weights, FP32 [head_dim], are not NULL) and rotation of queries and keys:
+ *   y = x * rsqrt(mean(x^2) + eps) * weight;  for i < rot_dim/2 the pair (a, b) = (i, i + rot_dim/2), interleaved: (2i, 2i + 1),
+ *   becomes (y_a cos - y_b sin, y_b cos + y_a sin) with row positions[token] of the table; elements from rot_dim on are not turned.
+ * Products and sums are rounded one by one, the results once to the type.  A position outside 0 .. max_positions - 1 gives NaN in
+ * place of the turned elements.  rot_dim: a multiple of 16 up to head_dim.  q_out, k_out may be q, k themselves (same strides);
+ * other overlaps are not allowed.  tokens <= 2^24. */
+int attn_qk_norm_rope(int dtype, int tokens, int Hq, int Hkv, int head_dim, const void *q, long long q_token, long long q_head,
+                      const void *k, long long k_token, long long k_head, const int *positions, const float *table, int max_positions,
+                      int rot_dim, int interleaved, const float *q_norm, const float *k_norm, float eps, void *q_out,
+                      long long qo_token, long long qo_head, void *k_out, long long ko_token, long long ko_head, void *hip_stream);
+
+/* Bytes of a page; 0 where there is none (page_size: a power of two from 16 to 256; head_dim 64 or 128; Hkv 1 .. 4096). */
+size_t kv4_page_bytes(int page_size, int Hkv, int head_dim);
+
+/* Writes tokens' keys and values to their slots (int32 [tokens]; a token whose slot is outside the cache is left out; two tokens
+ * with one slot: undefined which is kept, piece by piece). */
+int kv4_write(int dtype, int tokens, int Hkv, int head_dim, const void *k, long long k_token, long long k_head, const void *v,
+              long long v_token, long long v_head, const int *slots, void *cache, int num_pages, int page_size, void *hip_stream);
+
+/* attn_qk_norm_rope and kv4_write in one launch: the turned queries to q_out, the turned keys (rounded to the type, as
+ * attn_qk_norm_rope returns them) and the values into the cache.  Same results as the two calls, bit for bit. */
+int kv4_append(int dtype, int tokens, int Hq, int Hkv, int head_dim, const void *q, long long q_token, long long q_head, const void *k,
+               long long k_token, long long k_head, const void *v, long long v_token, long long v_head, const int *positions,
+               const float *table, int max_positions, int rot_dim, int interleaved, const float *q_norm, const float *k_norm, float eps,
+               void *q_out, long long qo_token, long long qo_head, const int *slots, void *cache, int num_pages, int page_size,
+               void *hip_stream);
+
+/* What the slots hold, rounded to the type: k, v [tokens, Hkv, head_dim] (zeros for a slot outside the cache). */
+int kv4_read(int dtype, int tokens, int Hkv, int head_dim, const void *cache, int num_pages, int page_size, const int *slots, void *k,
+             void *v, void *hip_stream);
+
+/* Attention of n_new tokens for each of n_seqs sequences over the cache, out [n_seqs, n_new, Hq, head_dim]: head h reads kv head
+ * h / (Hq / Hkv), new token i the keys j < context[seq] - n_new + 1 + i (the cache holds the new tokens already).  Key j of a sequence is
+ * at place j % page_size of page block_table[seq][j / page_size] (int32 [n_seqs, table_width]; entries behind the context are not read).
+ * scale multiplies the scores.  A token that sees no key gets zeros; a page number outside the cache, or a context longer than
+ * the table, gives the sequence's kv heads that met it NaN.  workspace as for w4a8_gemm (kv4_attention_workspace_size() bytes, the
+ * first 32 KiB zeroed once, may be NULL: slower where there are few sequences; shared with w4a8_gemm calls on the same stream). */
+size_t kv4_attention_workspace_size(int n_seqs, int n_new, int Hq, int Hkv, int head_dim);
+int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, int head_dim, const void *q, long long q_seq, long long q_token,
+                  long long q_head, const void *cache, int num_pages, int page_size, const int *block_table, int table_width,
+                  const int *context, float scale, void *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Attention over packed prompts: queries starts_q[s] .. starts_q[s+1] - 1 of [total_q, Hq, head_dim] read keys and values starts_k[s] ..
+ * starts_k[s+1] - 1 of [total_k, Hkv, head_dim] (int32 [n_seqs + 1] each, on the device; what lies outside the tensors is cut off);
+ * causal: query i the keys j <= i + len_k - len_q, so that a chunk of a prompt sees what came before it.  out [total_q, Hq, head_dim];
+ * a query that sees no key gets zeros, rows that belong to no sequence are left alone.  Masked keys and values have no
+ * part in the result whatever they hold.  total_q <= 2^28. */
+int attn_prompt(int dtype, int n_seqs, int total_q, int total_k, int Hq, int Hkv, int head_dim, const void *q, long long q_token,
+                long long q_head, const void *k, long long k_token, long long k_head, const void *v, long long v_token, long long v_head,
+                const int *starts_q, const int *starts_k, float scale, int causal, void *out, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------
  * Calibration (measurement support): what this GPU delivers on the two resources of the
  * cost model of Sec. 3.2 with nothing else in the way.  Both only enqueue a kernel on
  * `hip_stream`; the caller times them.

@@ -98,6 +98,25 @@ def lib() -> ctypes.CDLL:
     L.w8a8_pack_weights.argtypes = [vp, i, i, vp]
     L.w8a8_gemm.restype = i
     L.w8a8_gemm.argtypes = [i, i, i, vp, vp, vp, vp, vp, vp, vp]
+    ll, f, d = ctypes.c_longlong, ctypes.c_float, ctypes.c_double
+    L.attn_rope_table.restype = i
+    L.attn_rope_table.argtypes = [i, i, d, i, d, i, vp]
+    L.attn_qk_norm_rope.restype = i
+    L.attn_qk_norm_rope.argtypes = [i] * 5 + [vp, ll, ll] * 2 + [vp, vp, i, i, i, vp, vp, f] + [vp, ll, ll] * 2 + [vp]
+    L.kv4_page_bytes.restype = sz
+    L.kv4_page_bytes.argtypes = [i, i, i]
+    L.kv4_write.restype = i
+    L.kv4_write.argtypes = [i] * 4 + [vp, ll, ll] * 2 + [vp, vp, i, i, vp]
+    L.kv4_append.restype = i
+    L.kv4_append.argtypes = [i] * 5 + [vp, ll, ll] * 3 + [vp, vp, i, i, i, vp, vp, f, vp, ll, ll, vp, vp, i, i, vp]
+    L.kv4_read.restype = i
+    L.kv4_read.argtypes = [i] * 4 + [vp, i, i, vp, vp, vp, vp]
+    L.kv4_attention_workspace_size.restype = sz
+    L.kv4_attention_workspace_size.argtypes = [i] * 5
+    L.kv4_attention.restype = i
+    L.kv4_attention.argtypes = [i] * 6 + [vp, ll, ll, ll, vp, i, i, vp, i, vp, f, vp, vp, sz, vp]
+    L.attn_prompt.restype = i
+    L.attn_prompt.argtypes = [i] * 7 + [vp, ll, ll] * 3 + [vp, vp, f, i, vp, vp]
     L.w4a8_calib_stream_read.restype = i
     L.w4a8_calib_stream_read.argtypes = [vp, sz, vp]
     L.w4a8_calib_mfma_i8.restype = i
@@ -273,16 +292,17 @@ def w4a8_workspace_init(workspace, stream=None) -> None:
                                      _stream(stream)))
 
 
-def _ws(workspace, M=0, N=0, K=0, group=64, device=None, stream=None):
+def _ws(workspace, M=0, N=0, K=0, group=64, device=None, stream=None, need=None):
     """Workspace pointer and size.  With workspace=None a zero-initialised buffer of the size
-    the library asks for is allocated once per (device, stream) and reused: calls on different
+    the library asks for (`need`: of another call than a GEMM) is allocated once per (device, stream) and reused: calls on different
     streams may overlap and must not share one (device memory plumbing, nothing else)."""
     import torch
 
     if workspace is None:
         if device is not None and torch.device(device).type != "cuda":
             raise TypeError("X must be a torch tensor on the GPU")
-        need = w4a8_gemm_workspace_size(M, N, K, group) if M > 0 else 0
+        if need is None:
+            need = w4a8_gemm_workspace_size(M, N, K, group) if M > 0 else 0
         if need == 0:
             return None, 0
         # (the native module looks buffers up by the same key)
@@ -538,3 +558,192 @@ def w4a8_describe_grouped(row_offsets, N: int, K: int, group: int) -> str:
     text = ctypes.create_string_buffer(320)
     _check(lib().w4a8_describe_grouped(len(offs) - 1, (ctypes.c_int * len(offs))(*offs), N, K, group, text, len(text)))
     return text.value.decode()
+
+
+# ------------------------------------------------------------------------------ attention
+LQ_F16, LQ_BF16 = 0, 1
+_ROPE_SCALING = {None: 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+def attn_rope_table(max_positions: int, rot_dim: int, base: float = 10000.0, scaling=None, factor: float = 1.0,
+                    original_positions: int = 0):
+    """Cosines and sines of positions 0 .. max_positions - 1, float32 numpy [max_positions, rot_dim]; `scaling`: None, "linear",
+    "ntk" or "yarn" stretch the positions by `factor` (yarn: from the `original_positions` of the training)."""
+    if scaling not in _ROPE_SCALING:
+        raise ValueError(f"scaling must be one of {list(_ROPE_SCALING)}, got {scaling!r}")
+    table = np.empty((max(max_positions, 0), max(rot_dim, 0)), dtype=np.float32)
+    _check(lib().attn_rope_table(max_positions, rot_dim, base, _ROPE_SCALING[scaling], factor, original_positions, _np(table)))
+    return table
+
+
+def _heads(t, name, dtype=None, shape=None):
+    """A [.., heads, head_dim] tensor on the GPU with strides of its own: its pointer and strides (the last one is 1)."""
+    import torch
+
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a torch tensor on the GPU")
+    if t.dtype not in (torch.float16, torch.bfloat16) or (dtype is not None and t.dtype != dtype):
+        raise TypeError(f"{name} must have dtype {dtype or 'float16 or bfloat16'}, got {t.dtype}")
+    if shape is None and t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, head_dim], got {tuple(t.shape)}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise ValueError(f"{name}: the elements of a head must be consecutive")
+    return (ctypes.c_void_p(t.data_ptr()), *t.stride()[:-1])
+
+
+def _dtype_code(t):
+    import torch
+
+    return LQ_F16 if t.dtype == torch.float16 else LQ_BF16
+
+
+def _kv4_shape(cache):
+    """(pages, kv heads, page size, head dimension) of a cache tensor made by kv4_cache."""
+    import torch
+
+    _dev(cache, torch.uint8, name="cache")
+    if cache.dim() == 3:
+        for dim in (64, 128):
+            page = cache.shape[2] // (dim + 8)
+            if page * (dim + 8) == cache.shape[2] and 16 <= page <= 256 and page & (page - 1) == 0:
+                return cache.shape[0], cache.shape[1], page, dim
+    raise ValueError(f"cache must be [pages, kv_heads, page_size * (head_dim + 8)] as kv4_cache makes it, got {tuple(cache.shape)}")
+
+
+def kv4_cache(num_pages: int, page_size: int, n_kv_heads: int, head_dim: int, device="cuda"):
+    """An empty 4-bit cache of keys and values: uint8 [num_pages, n_kv_heads, page_size * (head_dim + 8)], zeroed."""
+    import torch
+
+    nbytes = int(lib().kv4_page_bytes(page_size, n_kv_heads, head_dim))
+    if nbytes == 0 or not 1 <= num_pages <= (2**31 - 1) // page_size:
+        raise ValueError(f"no cache of {num_pages} pages of {page_size} tokens, {n_kv_heads} heads of {head_dim}: page_size is a power of two "
+                         "from 16 to 256, head_dim 64 or 128, num_pages * page_size below 2^31")
+    return torch.zeros((num_pages, n_kv_heads, nbytes // n_kv_heads), dtype=torch.uint8, device=device)
+
+
+def _norms(q_norm, k_norm, dim):
+    import torch
+
+    return _dev(q_norm, torch.float32, (dim,), "q_norm"), _dev(k_norm, torch.float32, (dim,), "k_norm")
+
+
+def _rotation(positions, table, tokens):
+    import torch
+
+    if table.dim() != 2:
+        raise ValueError(f"table must be [positions, rot_dim], got {tuple(table.shape)}")
+    return _dev(positions, torch.int32, (tokens,), "positions"), _dev(table, torch.float32, name="table"), table.shape[0], table.shape[1]
+
+
+def attn_qk_norm_rope(q, k, positions, table, interleaved=False, q_norm=None, k_norm=None, eps=1e-6, out_q=None, out_k=None, stream=None):
+    """Norm of each head (where there are weights, float32 [head_dim]) and rotation of queries [tokens, heads, head_dim] and keys
+    [tokens, kv_heads, head_dim], float16 or bfloat16, at `positions` (int32 [tokens]) of `table` (attn_rope_table's, on the GPU).
+    out_q, out_k may be q and k themselves.  Returns (out_q, out_k)."""
+    import torch
+
+    dq, dk = _heads(q, "q"), _heads(k, "k", q.dtype)
+    (T, Hq, D), Hkv = q.shape, k.shape[1]
+    if tuple(k.shape) != (T, Hkv, D):
+        raise ValueError(f"k must have shape {(T, Hkv, D)}, got {tuple(k.shape)}")
+    out_q = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device) if out_q is None else out_q
+    out_k = torch.empty((T, Hkv, D), dtype=q.dtype, device=q.device) if out_k is None else out_k
+    _check(lib().attn_qk_norm_rope(_dtype_code(q), T, Hq, Hkv, D, *dq, *dk, *_rotation(positions, table, T), int(bool(interleaved)),
+                                   *_norms(q_norm, k_norm, D), eps, *_heads(out_q, "out_q", q.dtype, (T, Hq, D)),
+                                   *_heads(out_k, "out_k", q.dtype, (T, Hkv, D)), _stream(stream)))
+    return out_q, out_k
+
+
+def kv4_write(k, v, slots, cache, stream=None):
+    """Quantises keys and values [tokens, kv_heads, head_dim] into the cache's slots (int32 [tokens]: page * page_size + place;
+    outside the cache: left out).  Returns the cache."""
+    import torch
+
+    dk, (T, Hkv, D) = _heads(k, "k"), k.shape
+    dv = _heads(v, "v", k.dtype, (T, Hkv, D))
+    pages, heads, page, dim = _kv4_shape(cache)
+    if (heads, dim) != (Hkv, D):
+        raise ValueError(f"the cache holds {heads} heads of {dim}, k has {Hkv} of {D}")
+    _check(lib().kv4_write(_dtype_code(k), T, Hkv, D, *dk, *dv, _dev(slots, torch.int32, (T,), "slots"),
+                           _dev(cache, torch.uint8, name="cache"), pages, page, _stream(stream)))
+    return cache
+
+
+def kv4_append(q, k, v, positions, table, slots, cache, interleaved=False, q_norm=None, k_norm=None, eps=1e-6, out_q=None, stream=None):
+    """attn_qk_norm_rope and kv4_write in one launch: returns the turned queries; keys and values are in the cache."""
+    import torch
+
+    dq, dk = _heads(q, "q"), _heads(k, "k", q.dtype)
+    (T, Hq, D), Hkv = q.shape, k.shape[1]
+    if tuple(k.shape) != (T, Hkv, D):
+        raise ValueError(f"k must have shape {(T, Hkv, D)}, got {tuple(k.shape)}")
+    dv = _heads(v, "v", q.dtype, (T, Hkv, D))
+    pages, heads, page, dim = _kv4_shape(cache)
+    if (heads, dim) != (Hkv, D):
+        raise ValueError(f"the cache holds {heads} heads of {dim}, k has {Hkv} of {D}")
+    out_q = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device) if out_q is None else out_q
+    _check(lib().kv4_append(_dtype_code(q), T, Hq, Hkv, D, *dq, *dk, *dv, *_rotation(positions, table, T), int(bool(interleaved)),
+                            *_norms(q_norm, k_norm, D), eps, *_heads(out_q, "out_q", q.dtype, (T, Hq, D)),
+                            _dev(slots, torch.int32, (T,), "slots"), _dev(cache, torch.uint8, name="cache"), pages, page, _stream(stream)))
+    return out_q
+
+
+def kv4_read(cache, slots, dtype=None, stream=None):
+    """Keys and values [tokens, kv_heads, head_dim] that the slots hold (zeros outside the cache), float16 or `dtype`."""
+    import torch
+
+    pages, Hkv, page, D = _kv4_shape(cache)
+    dtype, T = dtype or torch.float16, slots.shape[0]
+    k, v = (torch.empty((T, Hkv, D), dtype=dtype, device=cache.device) for _ in range(2))
+    _check(lib().kv4_read(_dtype_code(k), T, Hkv, D, _dev(cache, torch.uint8, name="cache"), pages, page,
+                          _dev(slots, torch.int32, (T,), "slots"), _heads(k, "k")[0], _heads(v, "v")[0], _stream(stream)))
+    return k, v
+
+
+def kv4_attention(q, cache, block_table, context, scale=None, out=None, workspace=None, stream=None):
+    """Attention of the newest tokens q [sequences, new, heads, head_dim] (or [sequences, heads, head_dim]: one each) over the
+    cache: `block_table` int32 [sequences, width] names each sequence's pages, `context` int32 [sequences] its tokens, the new ones among
+    them; new token i sees the first context - new + 1 + i.  scale: 1 / sqrt(head_dim) unless given.  Returns out, shaped as q."""
+    import torch
+
+    pages, Hkv, page, D = _kv4_shape(cache)
+    one = q.dim() == 3
+    if q.dim() not in (3, 4) or q.shape[-1] != D:
+        raise ValueError(f"q must be [sequences, new tokens, heads, {D}] or [sequences, heads, {D}], got {tuple(q.shape)}")
+    B, n, Hq = (q.shape[0], 1, q.shape[1]) if one else q.shape[:3]
+    dq = _heads(q, "q", shape=q.shape)
+    if one:
+        dq = (dq[0], dq[1], 0, dq[2])
+    if block_table.dim() != 2:
+        raise ValueError(f"block_table must be [sequences, width], got {tuple(block_table.shape)}")
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    need = int(lib().kv4_attention_workspace_size(B, n, Hq, Hkv, D))
+    wsp, wsb = _ws(workspace, device=q.device, stream=stream, need=need)
+    _check(lib().kv4_attention(_dtype_code(q), B, n, Hq, Hkv, D, *dq, _dev(cache, torch.uint8, name="cache"), pages, page,
+                               _dev(block_table, torch.int32, (B, block_table.shape[1]), "block_table"), block_table.shape[1],
+                               _dev(context, torch.int32, (B,), "context"), D ** -0.5 if scale is None else scale,
+                               _dev(out, q.dtype, q.shape, "out"), wsp, wsb, _stream(stream)))
+    return out
+
+
+def attn_prompt(q, k, v, starts_q, starts_k=None, scale=None, causal=True, out=None, stream=None):
+    """Attention over packed sequences: q [queries, heads, head_dim], k and v [keys, kv_heads, head_dim]; sequence s has the
+    queries starts_q[s] .. starts_q[s + 1] - 1 and the keys starts_k[s] .. (int32 on the GPU; starts_k: starts_q unless given).  causal: query
+    i sees the keys up to i + (keys - queries) of its sequence.  scale: 1 / sqrt(head_dim) unless given.  Returns out, shaped as q."""
+    import torch
+
+    dq, dk = _heads(q, "q"), _heads(k, "k", q.dtype)
+    (Tq, Hq, D), (Tk, Hkv, _) = q.shape, k.shape
+    if k.shape[2] != D:
+        raise ValueError(f"k must have heads of {D}, got {tuple(k.shape)}")
+    dv = _heads(v, "v", q.dtype, (Tk, Hkv, D))
+    starts_k = starts_q if starts_k is None else starts_k
+    if starts_q.dim() != 1 or starts_q.shape[0] < 1:
+        raise ValueError(f"starts_q must be [sequences + 1], got {tuple(starts_q.shape)}")
+    S = starts_q.shape[0] - 1
+    out = torch.empty((Tq, Hq, D), dtype=q.dtype, device=q.device) if out is None else out
+    _check(lib().attn_prompt(_dtype_code(q), S, Tq, Tk, Hq, Hkv, D, *dq, *dk, *dv, _dev(starts_q, torch.int32, (S + 1,), "starts_q"),
+                             _dev(starts_k, torch.int32, (S + 1,), "starts_k"), D ** -0.5 if scale is None else scale, int(bool(causal)),
+                             _dev(out, q.dtype, (Tq, Hq, D), "out"), _stream(stream)))
+    return out
