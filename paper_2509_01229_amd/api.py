@@ -138,7 +138,7 @@ class _NoNative:
             warnings.warn(f"no native module for this Python and torch ({why}): calls go through ctypes, 20 us more each; "
                           "build it with `python -m paper_2509_01229_amd.build`", RuntimeWarning, stacklevel=3)
 
-    gemm = quantize = grouped = _decline
+    gemm = quantize = grouped = rope = write = append = read = decode = prompt = _decline
 
 
 def native_built_for() -> str:
@@ -163,6 +163,8 @@ def _bind(L) -> None:
     address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
     _binding.bind(address(L.w4a8_gemm), address(L.w4a8_gemm_workspace_size), address(L.w4a8_quantize_activations),
                   address(L.w4a8_grouped_gemm), address(L.liquidquant_packed_size))
+    _binding.bind_attention(address(L.attn_qk_norm_rope), address(L.kv4_write), address(L.kv4_append), address(L.kv4_read),
+                            address(L.kv4_attention_workspace_size), address(L.kv4_attention), address(L.attn_prompt))
     _native = _binding
 
 
@@ -641,6 +643,11 @@ def attn_qk_norm_rope(q, k, positions, table, interleaved=False, q_norm=None, k_
     """Norm of each head (where there are weights, float32 [head_dim]) and rotation of queries [tokens, heads, head_dim] and keys
     [tokens, kv_heads, head_dim], float16 or bfloat16, at `positions` (int32 [tokens]) of `table` (attn_rope_table's, on the GPU).
     out_q, out_k may be q and k themselves.  Returns (out_q, out_k)."""
+    if _native is None:
+        lib()
+    done = _native.rope(q, k, positions, table, interleaved, q_norm, k_norm, eps, out_q, out_k, stream)
+    if done is not None:
+        return _result(done)
     import torch
 
     dq, dk = _heads(q, "q"), _heads(k, "k", q.dtype)
@@ -658,6 +665,11 @@ def attn_qk_norm_rope(q, k, positions, table, interleaved=False, q_norm=None, k_
 def kv4_write(k, v, slots, cache, stream=None):
     """Quantises keys and values [tokens, kv_heads, head_dim] into the cache's slots (int32 [tokens]: page * page_size + place;
     outside the cache: left out).  Returns the cache."""
+    if _native is None:
+        lib()
+    done = _native.write(k, v, slots, cache, stream)
+    if done is not None:
+        return _result(done)
     import torch
 
     dk, (T, Hkv, D) = _heads(k, "k"), k.shape
@@ -672,6 +684,11 @@ def kv4_write(k, v, slots, cache, stream=None):
 
 def kv4_append(q, k, v, positions, table, slots, cache, interleaved=False, q_norm=None, k_norm=None, eps=1e-6, out_q=None, stream=None):
     """attn_qk_norm_rope and kv4_write in one launch: returns the turned queries; keys and values are in the cache."""
+    if _native is None:
+        lib()
+    done = _native.append(q, k, v, positions, table, slots, cache, interleaved, q_norm, k_norm, eps, out_q, stream)
+    if done is not None:
+        return _result(done)
     import torch
 
     dq, dk = _heads(q, "q"), _heads(k, "k", q.dtype)
@@ -693,8 +710,16 @@ def kv4_read(cache, slots, dtype=None, stream=None):
     """Keys and values [tokens, kv_heads, head_dim] that the slots hold (zeros outside the cache), float16 or `dtype`."""
     import torch
 
+    dtype = dtype or torch.float16
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"dtype must be float16 or bfloat16, got {dtype}")
+    if _native is None:
+        lib()
+    done = _native.read(cache, slots, dtype is torch.bfloat16, stream)
+    if done is not None:
+        return _result(done)
     pages, Hkv, page, D = _kv4_shape(cache)
-    dtype, T = dtype or torch.float16, slots.shape[0]
+    T = slots.shape[0]
     k, v = (torch.empty((T, Hkv, D), dtype=dtype, device=cache.device) for _ in range(2))
     _check(lib().kv4_read(_dtype_code(k), T, Hkv, D, _dev(cache, torch.uint8, name="cache"), pages, page,
                           _dev(slots, torch.int32, (T,), "slots"), _heads(k, "k")[0], _heads(v, "v")[0], _stream(stream)))
@@ -705,6 +730,11 @@ def kv4_attention(q, cache, block_table, context, scale=None, out=None, workspac
     """Attention of the newest tokens q [sequences, new, heads, head_dim] (or [sequences, heads, head_dim]: one each) over the
     cache: `block_table` int32 [sequences, width] names each sequence's pages, `context` int32 [sequences] its tokens, the new ones among
     them; new token i sees the first context - new + 1 + i.  scale: 1 / sqrt(head_dim) unless given.  Returns out, shaped as q."""
+    if _native is None:
+        lib()
+    done = _native.decode(q, cache, block_table, context, scale, out, workspace, stream, _ws_cache)
+    if done is not None:
+        return _result(done)
     import torch
 
     pages, Hkv, page, D = _kv4_shape(cache)
@@ -731,6 +761,11 @@ def attn_prompt(q, k, v, starts_q, starts_k=None, scale=None, causal=True, out=N
     """Attention over packed sequences: q [queries, heads, head_dim], k and v [keys, kv_heads, head_dim]; sequence s has the
     queries starts_q[s] .. starts_q[s + 1] - 1 and the keys starts_k[s] .. (int32 on the GPU; starts_k: starts_q unless given).  causal: query
     i sees the keys up to i + (keys - queries) of its sequence.  scale: 1 / sqrt(head_dim) unless given.  Returns out, shaped as q."""
+    if _native is None:
+        lib()
+    done = _native.prompt(q, k, v, starts_q, starts_q if starts_k is None else starts_k, scale, causal, out, stream)
+    if done is not None:
+        return _result(done)
     import torch
 
     dq, dk = _heads(q, "q"), _heads(k, "k", q.dtype)
