@@ -12,6 +12,8 @@
 //     nothing moves between lanes; the keys of a 16-byte piece of values are those of the lane's scores.
 // Weights are rounded to FP16 (2^-11 of each; the sums are FP32), as 2^6 .. 2^14 where they count most, times the value's
 // scale over a power of two that is at least the largest one so far.
+#include <algorithm>
+
 #include "attn_common.h"
 
 namespace lqq {
@@ -24,7 +26,9 @@ struct DecodeArgs {
     const uint8_t *cache;
     const int *table, *context;
     void *out;
-    int n_new, Hq, Hkv, group, rows, row_tiles, width, pages, lg_page;
+    unsigned *tickets;
+    float *parts;
+    int n_seqs, n_new, Hq, Hkv, group, rows, row_tiles, width, pages, lg_page, split, target;
     float scale_log2;  // softmax scale / ln 2
 };
 
@@ -32,15 +36,22 @@ __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b)
 {
     return __builtin_bit_cast(uint32_t, (f16x2v)(__builtin_bit_cast(f16x2v, a) - __builtin_bit_cast(f16x2v, b)));
 }
+// (w & mask) | bits in one instruction (the compiler takes two: it keeps both constants as literals)
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits)
+{
+    uint32_t r;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(w), "s"(mask), "v"(bits));
+    return r;
+}
 // 8 nibbles of a dword as 4 pairs of FP16 integers, the zero points taken off: pair r = nibbles r and r + 4.
 // even = 0x6400 + z in both halves (1024 + z), odd = 0x5400 + (z << 4) (64 + z)
 __device__ __forceinline__ void integers8(uint32_t w, uint32_t even, uint32_t odd, uint32_t (&o)[4])
 {
     const uint32_t w8 = w >> 8;
-    o[0] = sub_f16x2((w & 0x000f000fu) | 0x64006400u, even);
-    o[1] = sub_f16x2((w & 0x00f000f0u) | 0x54005400u, odd);
-    o[2] = sub_f16x2((w8 & 0x000f000fu) | 0x64006400u, even);
-    o[3] = sub_f16x2((w8 & 0x00f000f0u) | 0x54005400u, odd);
+    o[0] = sub_f16x2(and_or(w, 0x000f000fu, 0x64006400u), even);
+    o[1] = sub_f16x2(and_or(w, 0x00f000f0u, 0x54005400u), odd);
+    o[2] = sub_f16x2(and_or(w8, 0x000f000fu, 0x64006400u), even);
+    o[3] = sub_f16x2(and_or(w8, 0x00f000f0u, 0x54005400u), odd);
 }
 
 // over the four groups of 16 lanes: every lane gets the result of its column
@@ -53,230 +64,459 @@ __device__ __forceinline__ float across_groups(float x, F f)
     return f(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
 }
 
-// What a wave loads for 32 keys (two tiles of 16)
+// What a wave loads for 32 keys (two tiles of 16): the keys' part and the values'.  `head`: the kv head's bytes of the tile's page as a
+// buffer, of length zero where nothing is to be loaded (so that a load is never behind a branch, and the compiler can count those in flight).
+typedef __amdgpu_buffer_rsrc_t buf_t;
+template <int N>
+__device__ __forceinline__ void load_dwords(uint32_t (&x)[N], buf_t b, int lane_offset, int offset)
+{
+    if constexpr (N == 4) {
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, lane_offset, offset, 0);
+        x[0] = v[0], x[1] = v[1], x[2] = v[2], x[3] = v[3];
+    } else {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(b, lane_offset, offset, 0);
+        x[0] = v[0], x[1] = v[1];
+    }
+}
 template <int D>
-struct Loaded {
-    uint32_t k[2][D / 32], v[2][D / 32];  // this lane's key (row), this lane's four keys of its column group
-    u32x4 kw[2], vw[2];                   // words of the lane's four keys
-    uint32_t kz[2];                       // word of the lane's key
-    __device__ __forceinline__ void load(const uint8_t *head, int P, int j, int t, int lane)
+struct Keys {
+    uint32_t k[2][D / 32];  // this lane's key (row)
+    u32x4 w[2];             // words of the lane's four keys
+    uint32_t z[2];          // word of the lane's key
+    __device__ __forceinline__ void load(buf_t head, int P, int j, int t, int lane)
     {
         const int n = lane & 15, g = lane >> 4;
-        typedef uint32_t piece __attribute__((ext_vector_type(D / 32)));
-        const piece a = *reinterpret_cast<const piece *>(head + (j + n) * (D / 2) + g * (D / 8));
-        const piece b = *reinterpret_cast<const piece *>(head + P * (D / 2) + ((j >> 2) + g) * (2 * D) + n * (D / 8));
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) k[t][i] = a[i], v[t][i] = b[i];
-        const uint8_t *words = head + P * D + 4 * j;
-        kw[t] = *reinterpret_cast<const u32x4 *>(words + 16 * g);
-        vw[t] = *reinterpret_cast<const u32x4 *>(words + 4 * P + 16 * g);
-        kz[t] = *reinterpret_cast<const uint32_t *>(words + 4 * n);
+        load_dwords(k[t], head, n * (D / 2) + g * (D / 8), j * (D / 2));
+        w[t] = __builtin_amdgcn_raw_buffer_load_b128(head, 16 * g, P * D + 4 * j, 0);
+        z[t] = __builtin_amdgcn_raw_buffer_load_b32(head, 4 * n, P * D + 4 * j, 0);
+    }
+};
+template <int D>
+struct Values {
+    uint32_t v[2][D / 32];  // the lane's four keys of its column group
+    u32x4 w[2];             // their words
+    __device__ __forceinline__ void load(buf_t head, int P, int j, int t, int lane)
+    {
+        const int n = lane & 15, g = lane >> 4;
+        w[t] = __builtin_amdgcn_raw_buffer_load_b128(head, 16 * g, P * (D + 4) + 4 * j, 0);
+        load_dwords(v[t], head, g * (2 * D) + n * (D / 8), (P + j) * (D / 2));
     }
 };
 
 constexpr int kDecodeWaves = 4;
-constexpr float kWeightBits = 6.0f;  // a row's largest weight is 2^6 when its maximum is up to date
+constexpr int kUnit = 32 * kDecodeWaves;  // keys that a block goes through at once
+constexpr float kWeightBits = 6.0f;       // a row's largest weight is 2^6 when its maximum is up to date
 
-template <int D, class T>
-__global__ __launch_bounds__(64 * kDecodeWaves) void kv4_attention_kernel(const DecodeArgs a)
+// The work is units of kUnit keys.  With split = 1 an item (sequence, kv head, tile of rows) is cut into chunks of the same number of
+// units for all sequences, so many that about `target` blocks have work, and a block takes a chunk.  The chunks of an item are joined by the
+// last of its blocks to arrive at its ticket: each leaves its maxima, sums and unscaled results in the workspace (written and read past
+// the L2s, which the XCDs do not share), in the order of the split chunks of all items; the ticket is that of the item's first.
+// A sequence without keys has one unit all the same (its zeros are written there).  With split = 0 a block is an item.
+#ifndef KV4_OCC1
+#define KV4_OCC1 4
+#endif
+#ifndef KV4_MIN_UNITS
+#define KV4_MIN_UNITS 1
+#endif
+#ifndef KV4_ROUNDS
+#define KV4_ROUNDS 1
+#endif
+constexpr int kMaxParts = 64, kMinUnits = KV4_MIN_UNITS;
+constexpr size_t kTickets = 32768;  // bytes at the head of the workspace, those of the GEMM's
+__host__ __device__ constexpr int part_floats(int rows, int D) { return rows * (D + 4); }
+
+__device__ __forceinline__ int units_of(int ctx) { return max(1, (ctx + kUnit - 1) / kUnit); }
+// 16 bytes past the L2 (device scope)
+constexpr int kShared = 16;  // sc1
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t shared_buffer(float *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(p, 0, bytes, 0x00027000); }
+
+// (RT: tiles of 16 rows that share a pass over the keys)
+template <int D, class T, int RT>
+__global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? KV4_OCC1 : 2) void kv4_attention_kernel(const DecodeArgs a)
 {
     constexpr int W = D / 16, STEPS = D / 32;  // elements of a column group; MFMAs of a key tile
-    __shared__ float s_o[kDecodeWaves][16][D + 4], s_m[kDecodeWaves][16], s_l[kDecodeWaves][16];
+    constexpr int ROWS = 16 * RT;
+    __shared__ float s_o[kDecodeWaves][16][D + 4], s_m[kDecodeWaves][ROWS], s_l[kDecodeWaves][ROWS];
+    __shared__ int s_last;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    int item = (int)blockIdx.x;
-    const int rt = item % a.row_tiles;
-    item /= a.row_tiles;
-    const int hk = item % a.Hkv, seq = item / a.Hkv;
-    const int P = 1 << a.lg_page;
+    const int P = 1 << a.lg_page, items = a.Hkv * a.row_tiles;
     const size_t page_bytes = (size_t)a.Hkv * kv4_head_bytes(P, D);
-    const uint8_t *const cache = a.cache + (size_t)hk * kv4_head_bytes(P, D);
+    const int longest = a.width << a.lg_page;
+    // (integers that no kernel writes meanwhile: scalar loads)
+    typedef const __attribute__((address_space(4))) int *ints;
+    const ints table = (ints)(uintptr_t)a.table, contexts = (ints)(uintptr_t)a.context;
+    const auto context = [&](int s) { return min(max(contexts[s], 0), longest); };
 
-    int ctx = a.context[seq];
-    bool bad = ctx > a.width * P;  // more than the table has pages for
-    ctx = min(max(ctx, 0), a.width * P);
-    const int row = rt * 16 + n, token = min(row / a.group, a.n_new - 1), head = hk * a.group + row % a.group;
-    const bool real = row < a.rows;
-    const int limit = real ? ctx - a.n_new + 1 + token : 0;  // keys that this lane's row sees
-
-    // queries: operand order of the keys (see integers8)
-    vec<f16, 8> q[STEPS];
-    float q_scale = a.scale_log2;
-    {
-        float f[STEPS][8];
-        const T *src = static_cast<const T *>(a.q) + seq * a.q_seq + token * a.q_token + (real ? head : hk * a.group) * a.q_head + g * (D / 4);
-        float most = 0.0f;
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            const vec<T, 8> x = *reinterpret_cast<const vec<T, 8> *>(src + 8 * i);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[i][e] = real ? (float)x[e] : 0.0f, most = fmaxf(most, fabsf(f[i][e]));
+    // this block's sequence, item and units; the item's chunks, and where they are among the split ones
+    int seq, item, unit = 0, count, chunks = 1, chunk = 0, first_part = 0;
+    if (a.split) {
+        int total = 0, most = 0;
+        for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+            const int s = s0 + lane, u = s < a.n_seqs ? units_of(context(s)) : 0;
+            int sum = u, top = u;
+            for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d), top = max(top, __shfl_xor(top, d));
+            total += sum;
+            most = max(most, top);
         }
-        if (sizeof(T) == 2 && !__is_same(T, f16)) {
-            // BF16: times a power of two that brings the row below 2 (exact down to 2^-14 of its largest element)
-            most = across_groups(most, [](float x, float y) { return fmaxf(x, y); });
-            const int e = min(max((int)(__builtin_bit_cast(uint32_t, most) >> 23), 27), 227) - 127;
-            q_scale *= __builtin_ldexpf(1.0f, e);
+        total = __builtin_amdgcn_readfirstlane(total) * items;
+        most = __builtin_amdgcn_readfirstlane(most);
+        const int size = max(max((total + a.target - 1) / a.target, kMinUnits), (most + kMaxParts - 1) / kMaxParts);  // units of a chunk
+        int before = 0, parts = 0;  // chunks, split chunks of the sequences that come before
+        seq = -1;
+        for (int s0 = 0; seq < 0 && s0 < a.n_seqs; s0 += 64) {
+            const int s = s0 + lane, c = s < a.n_seqs ? (units_of(context(s)) + size - 1) / size : 0;
+            int sum = c, split = c > 1 ? c : 0;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int x = __shfl_up(sum, d), y = __shfl_up(split, d);
+                if (lane >= d) sum += x, split += y;
+            }
+            const uint64_t past = __ballot((before + sum) * items > (int)blockIdx.x);
+            const int at = past ? __builtin_ctzll(past) : 63;
+            before += __builtin_amdgcn_readlane(sum, at);
+            parts += __builtin_amdgcn_readlane(split, at);
+            if (past) {
+                seq = s0 + at;
+                chunks = __builtin_amdgcn_readlane(c, at);
+                before -= chunks;
+                if (chunks > 1) parts -= chunks;
+            }
+        }
+        if (seq < 0) return;
+        const int inside = (int)blockIdx.x - before * items;
+        item = inside / chunks;
+        chunk = inside % chunks;
+        first_part = parts * items + item * chunks;
+        unit = chunk * size;
+        count = min(size, units_of(context(seq)) - unit);
+    } else {
+        seq = (int)blockIdx.x / items;
+        item = (int)blockIdx.x % items;
+        count = units_of(context(seq));
+    }
+
+    {
+        const int rt = item % a.row_tiles, hk = item / a.row_tiles;
+        const uint8_t *const cache = a.cache + (size_t)hk * kv4_head_bytes(P, D);
+        bool bad = contexts[seq] > longest;  // more than the table has pages for
+        const int ctx = context(seq), end = min(ctx, (unit + count) * kUnit);
+        int limit[RT];                        // keys that this lane's rows see
+
+        // queries: operand order of the keys (see integers8)
+        vec<f16, 8> q[RT][STEPS];
+        float q_scale[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int row = rt * ROWS + r * 16 + n, token = min(row / a.group, a.n_new - 1), head = hk * a.group + row % a.group;
+            const bool real = row < a.rows;
+            limit[r] = real ? ctx - a.n_new + 1 + token : 0;
+            q_scale[r] = fmaxf(fabsf(a.scale_log2), 0x1p-126f);  // (its sign goes with the queries)
+            float f[STEPS][8];
+            const T *src = static_cast<const T *>(a.q) + seq * a.q_seq + token * a.q_token + (real ? head : hk * a.group) * a.q_head + g * (D / 4);
+            const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;
+            float most = 0.0f;
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                const vec<T, 8> x = *reinterpret_cast<const vec<T, 8> *>(src + 8 * i);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[i][e] = real ? (float)x[e] * sign : 0.0f, most = fmaxf(most, fabsf(f[i][e]));
+            }
+            if constexpr (!__is_same(T, f16)) {
+                // BF16: times a power of two that brings the row below 2 (exact down to 2^-14 of its largest element)
+                most = across_groups(most, [](float x, float y) { return fmaxf(x, y); });
+                const int e = min(max((int)(__builtin_bit_cast(uint32_t, most) >> 23), 27), 227) - 127;
+                q_scale[r] *= __builtin_ldexpf(1.0f, e);
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[i][j] = __builtin_ldexpf(f[i][j], -e);
+            }
 #pragma unroll
             for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[i][j] = __builtin_ldexpf(f[i][j], -e);
+                for (int j = 0; j < 4; ++j) q[r][i][2 * j] = (f16)f[i][j], q[r][i][2 * j + 1] = (f16)f[i][j + 4];
         }
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) q[i][2 * r] = (f16)f[i][r], q[i][2 * r + 1] = (f16)f[i][r + 4];
-    }
 
-    v4f o[W] = {};
-    float m = -__builtin_inff(), l = 0.0f;  // the row's maximum (of scores / ln 2), this lane's part of its sum
-    float v_top = 0x1p-126f, v_inv = 0.0f;  // power of two that no value's scale so far is above, and 2^-.. of it
-    const int last_page = max((ctx - 1) >> a.lg_page, 0);
+        v4f o[RT][W] = {};
+        float m[RT], l[RT] = {};  // a row's maximum (as sc), this lane's part of its sum
+        float m_up[RT], base[RT] = {};  // the score from which the maximum moves; kWeightBits less the maximum times q_scale
+#pragma unroll
+        for (int r = 0; r < RT; ++r) m[r] = m_up[r] = -__builtin_inff();
+        float v_top = 0x1p-126f, v_inv = 0.0f;  // power of two that no value's scale so far is above, and 2^-.. of it
+        const int last_page = max((ctx - 1) >> a.lg_page, 0);
 
-    auto fetch = [&](Loaded<D> &x, int key) {
+        // the pages of 32 keys: numbers first, then addresses
+        struct Place {
+            int page[2];
+        };
+        const auto pages_of = [&](int key) {
+            Place p;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int k0 = key + 16 * t;
-            int page = a.table[(size_t)seq * a.width + min(k0 >> a.lg_page, last_page)];
-            const bool out_of_range = page < 0 || page >= a.pages;
-            bad |= out_of_range;
-            page = out_of_range ? 0 : page;
-            x.load(cache + (size_t)page * page_bytes, P, k0 & (P - 1), t, lane);
-        }
-    };
-    auto step = [&](const Loaded<D> &x, int key) {
-        float sc[2][4];  // scores
-        float sv[2][4];  // scales of the values
+            for (int t = 0; t < 2; ++t) p.page[t] = table[(size_t)seq * a.width + min((key + 16 * t) >> a.lg_page, last_page)];
+            return p;
+        };
+        buf_t head[2];
+        const auto go_to = [&](Place p, bool any) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const uint32_t z = x.kz[t] & 15u, zz = z | z << 16, even = 0x64006400u | zz, odd = 0x54005400u | zz << 4;
-            v4f acc = {};
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                uint32_t k8[4];
-                integers8(x.k[t][i], even, odd, k8);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec<f16, 8>, u32x4{k8[0], k8[1], k8[2], k8[3]}), q[i], acc, 0, 0, 0);
+            for (int t = 0; t < 2; ++t) {
+                const bool out_of_range = p.page[t] < 0 || p.page[t] >= a.pages;
+                bad |= out_of_range;
+                head[t] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(cache + (size_t)(out_of_range ? 0 : p.page[t]) * page_bytes), 0,
+                                                            any ? kv4_head_bytes(P, D) : 0, 0x00027000);
             }
+        };
+        const auto load = [&](auto &x, int key) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sc[t][i] = acc[i] * (__builtin_bit_cast(float, x.kw[t][i] & kScaleMask) * q_scale);
-                sv[t][i] = __builtin_bit_cast(float, x.vw[t][i] & kScaleMask);
+            for (int t = 0; t < 2; ++t) x.load(head[t], P, (key + 16 * t) & (P - 1), t, lane);
+        };
+        Keys<D> xk;
+        Values<D> xv;
+        // a step takes 32 keys; the next ones' registers are those that it has just used
+        const auto step = [&](int key, bool more, Place &next) {
+            float sc[RT][2][4];  // scores over q_scale
+            float sv[2][4];      // scales of the values (with the zero points still in their last bits: 2^-19 of them)
+            float vt = 0.0f;
+            const bool tail = key + 32 > ctx - a.n_new + 1;  // some row does not see all of these keys
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const uint32_t z = xk.z[t] & 15u, zz = z | z << 16, even = 0x64006400u | zz, odd = 0x54005400u | zz << 4;
+                v4f acc[RT] = {};
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i) {
+                    uint32_t k8[4];
+                    integers8(xk.k[t][i], even, odd, k8);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+                        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec<f16, 8>, u32x4{k8[0], k8[1], k8[2], k8[3]}), q[r][i],
+                                                                        acc[r], 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float sk = __builtin_bit_cast(float, xk.w[t][i] & kScaleMask);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) sc[r][t][i] = acc[r][i] * sk;
+                }
             }
-        }
-        const bool tail = key + 32 > ctx - a.n_new + 1;  // some row does not see all of these keys
-        if (tail) {
+            go_to(next, more);
+            load(xk, key + kUnit);
+            next = pages_of(key + 2 * kUnit);
+            __builtin_amdgcn_sched_barrier(0);
+            asm("" : "+v"(xv.w[0]), "+v"(xv.w[1]));  // (nothing of the values is looked at before)
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int j = key + 16 * t + 4 * g + i;
-                    sc[t][i] = j < limit ? sc[t][i] : -__builtin_inff();
-                    sv[t][i] = j < ctx ? sv[t][i] : 0.0f;
+                    const uint32_t word = xv.w[t][i];  // (a bit cast of a vector's element takes its first)
+                    sv[t][i] = __builtin_bit_cast(float, word);
                 }
-        }
-        float top = sc[0][0], vt = sv[0][0];
+            if (tail) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i >> 2][i & 3]), vt = fmaxf(vt, sv[i >> 2][i & 3]);
-        if (__any(top > m + (14.0f - kWeightBits))) {  // (first of all: m is minus infinity)
-            top = across_groups(top, [](float u, float w) { return fmaxf(u, w); });
-            const float now = fmaxf(m, top), by = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - now);
-            m = now;
-            l *= by;
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int e = 0; e < W; ++e) o[e] *= by;
-        }
-        if (__any(vt > v_top)) {
-            for (int d = 1; d < 64; d <<= 1) vt = fmaxf(vt, __shfl_xor(vt, d));
-            // (the next power of two; scales above 2^126 keep it there and reach FP16's largest weights)
-            const uint32_t e = min((__builtin_bit_cast(uint32_t, vt) >> 23) + 1u, 253u);
-            const float next = __builtin_bit_cast(float, e << 23), by = v_top / next;
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = key + 16 * t + 4 * g + i;
 #pragma unroll
-            for (int i = 0; i < W; ++i) o[i] *= by;
-            v_top = next;
-            v_inv = 1.0f / next;
-        }
-        const float base = m == -__builtin_inff() ? 0.0f : m - kWeightBits;
-        uint32_t w[4];
-        float p[2][4];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                p[t][i] = __builtin_amdgcn_exp2f(sc[t][i] - base);
-                l += p[t][i];
-                p[t][i] *= sv[t][i] * v_inv;
-                if (tail) p[t][i] = key + 16 * t + 4 * g + i < limit ? p[t][i] : 0.0f;  // (whatever the scale there is)
+                        for (int r = 0; r < RT; ++r) sc[r][t][i] = j < limit[r] ? sc[r][t][i] : -__builtin_inff();
+                        sv[t][i] = j < ctx ? sv[t][i] : 0.0f;
+                    }
             }
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+            for (int i = 0; i < 8; ++i) vt = fmaxf(vt, sv[i >> 2][i & 3]);
+            float top[RT];
+            bool up = false;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                w[2 * t + i] = __builtin_bit_cast(uint32_t, f16x2v{(f16)p[t][2 * i], (f16)p[t][2 * i + 1]});
-        const auto weights = __builtin_bit_cast(vec<f16, 8>, u32x4{w[0], w[1], w[2], w[3]});
-        uint32_t zz[4];  // zero points of the pairs of keys
+            for (int r = 0; r < RT; ++r) {
+                top[r] = sc[r][0][0];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+                for (int i = 1; i < 8; ++i) top[r] = fmaxf(top[r], sc[r][i >> 2][i & 3]);
+                up |= top[r] > m_up[r];
+            }
+            if (__any(up)) {  // (first of all: m is minus infinity)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) zz[2 * t + i] = (x.vw[t][2 * i] & 15u) | (x.vw[t][2 * i + 1] & 15u) << 16;
+                for (int r = 0; r < RT; ++r) {
+                    top[r] = across_groups(top[r], [](float u, float w) { return fmaxf(u, w); });
+                    const float now = fmaxf(m[r], top[r]), by = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m[r] - now) * q_scale[r]);
+                    m[r] = now;
+                    m_up[r] = now + (14.0f - kWeightBits) / q_scale[r];
+                    base[r] = now == -__builtin_inff() ? 0.0f : kWeightBits - now * q_scale[r];
+                    l[r] *= by;
 #pragma unroll
-        for (int h = 0; h < W / 4; ++h) {
-            uint32_t v8[4][4];  // [pair][element of the four]
+                    for (int e = 0; e < W; ++e) o[r][e] *= by;
+                }
+            }
+            if (__any(vt > v_top)) {
+                for (int d = 1; d < 64; d <<= 1) vt = fmaxf(vt, __shfl_xor(vt, d));
+                const uint32_t e = min((__builtin_bit_cast(uint32_t, vt) >> 23) + 1u, 253u);  // the next power of two
+                const float next = __builtin_bit_cast(float, e << 23), by = v_top / next;
 #pragma unroll
-            for (int p2 = 0; p2 < 4; ++p2)
-                integers8(x.v[p2 >> 1][(p2 & 1) * (W / 4) + h], 0x64006400u | zz[p2], 0x54005400u | zz[p2] << 4, v8[p2]);
+                for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                o[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                    __builtin_bit_cast(vec<f16, 8>, u32x4{v8[0][e], v8[1][e], v8[2][e], v8[3][e]}), weights, o[4 * h + e], 0, 0, 0);
-        }
-    };
+                    for (int i = 0; i < W; ++i) o[r][i] *= by;
+                v_top = next;
+                v_inv = 1.0f / next;
+            }
+            vec<f16, 8> weights[RT];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                uint32_t w[4];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    float p[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r][t][i], q_scale[r], base[r]));
+                        l[r] += p[i];
+                        p[i] *= sv[t][i] * v_inv;
+                    }
+                    if (tail) {  // (whatever the scale there is)
+                        asm volatile("");
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) p[i] = sc[r][t][i] == -__builtin_inff() ? 0.0f : p[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) w[2 * t + i] = __builtin_bit_cast(uint32_t, f16x2v{(f16)p[2 * i], (f16)p[2 * i + 1]});
+                }
+                weights[r] = __builtin_bit_cast(vec<f16, 8>, u32x4{w[0], w[1], w[2], w[3]});
+            }
+            uint32_t zz[4];  // zero points of the pairs of keys (the low bytes of their words)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) zz[2 * t + i] = __builtin_amdgcn_perm(xv.w[t][2 * i + 1], xv.w[t][2 * i], 0x0c040c00u) & 0x000f000fu;
+#pragma unroll
+            for (int h = 0; h < W / 4; ++h) {
+                uint32_t v8[4][4];  // [pair][element of the four]
+#pragma unroll
+                for (int p2 = 0; p2 < 4; ++p2)
+                    integers8(xv.v[p2 >> 1][(p2 & 1) * (W / 4) + h], 0x64006400u | zz[p2], 0x54005400u | zz[p2] << 4, v8[p2]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+                        o[r][4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                            __builtin_bit_cast(vec<f16, 8>, u32x4{v8[0][e], v8[1][e], v8[2][e], v8[3][e]}), weights[r], o[r][4 * h + e], 0, 0, 0);
+            }
+            load(xv, key + kUnit);
+            __builtin_amdgcn_sched_barrier(0);
+        };
 
-    Loaded<D> x[2];
-    int key = 32 * wave;
-    constexpr int STRIDE = 32 * kDecodeWaves;
-    if (key < ctx) {
-        fetch(x[0], key);
-        for (;; key += 2 * STRIDE) {
-            const bool more = key + STRIDE < ctx;
-            if (more) fetch(x[1], key + STRIDE);
-            step(x[0], key);
-            if (!more) break;
-            const bool more2 = key + 2 * STRIDE < ctx;
-            if (more2) fetch(x[0], key + 2 * STRIDE);
-            step(x[1], key + STRIDE);
-            if (!more2) break;
+        int key = unit * kUnit + 32 * wave;
+        if (key < end) {
+            go_to(pages_of(key), true);
+            load(xk, key);
+            __builtin_amdgcn_sched_barrier(0);  // (in the order of the loop's)
+            load(xv, key);
+            __builtin_amdgcn_sched_barrier(0);
+            Place next = pages_of(key + kUnit);
+            for (; key < end; key += kUnit) step(key, key + kUnit < end, next);
         }
-    }
-    l = across_groups(l, [](float u, float w) { return u + w; });
-    if (bad) l = __builtin_nanf("");
-    // the waves' parts: sums of weights relative to 2^(m - kWeightBits), both over 2^16 so that values near the end of FP32's range stay in it
-    if (g == 0) s_m[wave][n] = m, s_l[wave][n] = l * 0x1p-16f;
+        // the waves' parts: sums of weights relative to 2^(m - kWeightBits), both over 2^16 so that values near the end of FP32's range stay in it
 #pragma unroll
-    for (int e = 0; e < W; ++e)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s_o[wave][n][(4 * g + i) * W + e] = o[e][i] * 0x1p-16f * v_top;
-    __syncthreads();
-    // thread: 8 elements of a row
-    constexpr int PIECES = 16 * D / 8;
-    for (int i = threadIdx.x; i < PIECES; i += 64 * kDecodeWaves) {
-        const int r = i / (D / 8), c = i % (D / 8) * 8, to = rt * 16 + r;
-        if (to >= a.rows) continue;
-        float most = s_m[0][r];
-#pragma unroll
-        for (int w = 1; w < kDecodeWaves; ++w) most = fmaxf(most, s_m[w][r]);
-        float sum = 0.0f, f[8] = {};
-#pragma unroll
-        for (int w = 0; w < kDecodeWaves; ++w) {
-            const float by = s_m[w][r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(s_m[w][r] - most);
-            sum += s_l[w][r] * by;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] += s_o[w][r][c + e] * by;
+        for (int r = 0; r < RT; ++r) {
+            l[r] = across_groups(l[r], [](float u, float w) { return u + w; });
+            if (bad) l[r] = __builtin_nanf("");
+            if (g == 0) s_m[wave][16 * r + n] = m[r] * q_scale[r], s_l[wave][16 * r + n] = l[r] * 0x1p-16f;
         }
-        vec<T, 8> y;
+        // thread: 8 elements of a row of each tile; the waves' results one tile at a time
+        float most[RT], sum[RT], f[RT][8];
+        constexpr int STEP = 64 * kDecodeWaves;
+        static_assert(16 * D / 8 <= STEP, "");
+        const int r16 = (int)threadIdx.x / (D / 8), c = (int)threadIdx.x % (D / 8) * 8;
+        const bool mine = threadIdx.x < 16 * D / 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = (T)(sum == 0.0f ? 0.0f : f[e] / sum);
-        T *dst = static_cast<T *>(a.out) + (((size_t)seq * a.n_new + to / a.group) * a.Hq + hk * a.group + to % a.group) * D + c;
-        *reinterpret_cast<vec<T, 8> *>(dst) = y;
+        for (int r = 0; r < RT; ++r) {
+            if (r) __syncthreads();
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s_o[wave][n][(4 * g + i) * W + e] = o[r][e][i] * 0x1p-16f * v_top;
+            __syncthreads();
+            if (!mine) continue;
+            most[r] = s_m[0][16 * r + r16];
+#pragma unroll
+            for (int w = 1; w < kDecodeWaves; ++w) most[r] = fmaxf(most[r], s_m[w][16 * r + r16]);
+            sum[r] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[r][e] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kDecodeWaves; ++w) {
+                const float mw = s_m[w][16 * r + r16], by = mw == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mw - most[r]);
+                sum[r] += s_l[w][16 * r + r16] * by;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[r][e] += s_o[w][r16][c + e] * by;
+            }
+        }
+        if (chunks > 1) {
+            float *const parts = a.parts + (size_t)first_part * part_floats(ROWS, D);
+            const auto mine_at = shared_buffer(parts + (size_t)chunk * part_floats(ROWS, D), part_floats(ROWS, D) * 4);
+            if (mine) {
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    const int at = ((16 * r + r16) * D + c) * 4;
+                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__builtin_bit_cast(u32x4, v4f{f[r][0], f[r][1], f[r][2], f[r][3]})}, mine_at, at, 0, kShared);
+                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__builtin_bit_cast(u32x4, v4f{f[r][4], f[r][5], f[r][6], f[r][7]})}, mine_at, at + 16, 0, kShared);
+                    if (c == 0)
+                        __builtin_amdgcn_raw_buffer_store_b128(u32x4{__builtin_bit_cast(u32x4, v4f{most[r], sum[r], 0.0f, 0.0f})}, mine_at,
+                                                               (ROWS * D + (16 * r + r16) * 4) * 4, 0, kShared);
+                }
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                const unsigned before = __hip_atomic_fetch_add(a.tickets + first_part, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                s_last = before == (unsigned)chunks - 1;
+                if (before == (unsigned)chunks - 1) __hip_atomic_store(a.tickets + first_part, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            __syncthreads();
+            if (!s_last) return;
+            if (mine) {
+                constexpr int U = 4;  // parts whose loads are in flight together
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    most[r] = -__builtin_inff();
+                    sum[r] = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[r][e] = 0.0f;
+                    for (int w = 0; w < chunks; w += U) {
+                        v4f x[U][2], ml[U];
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {  // (past the last: the last once more, without weight)
+                            const auto from = shared_buffer(parts + (size_t)min(w + u, chunks - 1) * part_floats(ROWS, D), part_floats(ROWS, D) * 4);
+                            const int at = ((16 * r + r16) * D + c) * 4;
+                            ml[u] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, (ROWS * D + (16 * r + r16) * 4) * 4, 0, kShared));
+                            x[u][0] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at, 0, kShared));
+                            x[u][1] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at + 16, 0, kShared));
+                        }
+                        float now = most[r];
+#pragma unroll
+                        for (int u = 0; u < U; ++u) now = fmaxf(now, ml[u][0]);
+                        const float old = most[r] == now ? 1.0f : __builtin_amdgcn_exp2f(most[r] - now);
+                        most[r] = now;
+                        sum[r] *= old;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[r][e] *= old;
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            if (w + u >= chunks) break;  // (uniform)
+                            const float by = ml[u][0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ml[u][0] - now);
+                            sum[r] += ml[u][1] * by;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) f[r][e] += x[u][e >> 2][e & 3] * by;
+                        }
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int to = rt * ROWS + 16 * r + r16;
+            if (!mine || to >= a.rows) continue;
+            vec<T, 8> y;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = (T)(sum[r] == 0.0f ? 0.0f : f[r][e] / sum[r]);
+            T *dst = static_cast<T *>(a.out) + (((size_t)seq * a.n_new + to / a.group) * a.Hq + hk * a.group + to % a.group) * D + c;
+            *reinterpret_cast<vec<T, 8> *>(dst) = y;
+        }
     }
 }
 
@@ -284,10 +524,17 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void kv4_attention_kernel(const 
 
 using namespace lqq;
 
+// Rows that share a pass: one tile of 16, or two
+static int row_tiles_of(int rows) { return rows <= 16 ? 1 : 2; }
+// Blocks that have work where the keys can be split: as many as the CUs hold at a time (KV4_ROUNDS times)
+static int target_of(int row_tiles) { return KV4_ROUNDS * 256 * (row_tiles == 1 ? KV4_OCC1 : 2); }
+
 extern "C" size_t kv4_attention_workspace_size(int n_seqs, int n_new, int Hq, int Hkv, int head_dim)
 {
-    (void)n_seqs, (void)n_new, (void)Hq, (void)Hkv, (void)head_dim;
-    return 0;
+    if (n_seqs < 1 || n_new < 1 || Hkv < 1 || Hq < 1 || Hq % Hkv || !head_dim_ok(head_dim)) return 0;
+    const long long rows = (long long)n_new * (Hq / Hkv);
+    const int RT = row_tiles_of((int)std::min(rows, 1LL << 20));
+    return kTickets + sizeof(float) * 2 * target_of(RT) * part_floats(16 * RT, head_dim);
 }
 
 extern "C" int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, int head_dim, const void *q, long long q_seq,
@@ -301,29 +548,40 @@ extern "C" int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, 
         return fail(LQ_ERR_INVALID, "bad shape: %d sequences, %d new tokens, %d heads, %d kv heads (heads a multiple of kv heads, up to 4096)",
                     n_seqs, n_new, Hq, Hkv);
     if (!page_ok(page_size)) return fail(LQ_ERR_INVALID, "page_size must be a power of two from 16 to 256, got %d", page_size);
-    if (num_pages < 1 || num_pages > INT32_MAX / page_size || table_width < 1 || table_width > INT32_MAX / page_size)
-        return fail(LQ_ERR_INVALID, "num_pages and table_width times page_size must be from 1 to 2^31 - 1, got %d and %d times %d", num_pages,
+    if (num_pages < 1 || num_pages > INT32_MAX / page_size || table_width < 1 || table_width > INT32_MAX / page_size - 1)
+        return fail(LQ_ERR_INVALID, "num_pages and table_width times page_size must be from 1 to below 2^31, got %d and %d times %d", num_pages,
                     table_width, page_size);
     if (!(scale > -1e30f && scale < 1e30f)) return fail(LQ_ERR_INVALID, "scale must be finite");
-    const long long rows = (long long)n_new * (Hq / Hkv), tiles = (rows + 15) / 16;
-    if (rows > (1 << 20) || tiles * Hkv * n_seqs > (1 << 22))
-        return fail(LQ_ERR_INVALID, "too many rows: %d sequences, %d new tokens, %d heads", n_seqs, n_new, Hq);
+    const long long rows = (long long)n_new * (Hq / Hkv);
+    if (rows > (1 << 20)) return fail(LQ_ERR_INVALID, "too many rows: %d new tokens, %d heads a kv head", n_new, Hq / Hkv);
+    const int RT = row_tiles_of((int)rows);
+    const long long tiles = (rows + 16 * RT - 1) / (16 * RT), items = tiles * Hkv;
+    if (items * n_seqs > (1 << 22)) return fail(LQ_ERR_INVALID, "too many rows: %d sequences, %d new tokens, %d heads", n_seqs, n_new, Hq);
     if (n_seqs == 0) return LQ_OK;
     if (!q || !cache || !block_table || !context || !out) return fail(LQ_ERR_INVALID, "null pointer");
-    if (((uintptr_t)q | (uintptr_t)cache | (uintptr_t)out) & 15) return fail(LQ_ERR_ALIGN, "q, cache and out must be 16-byte aligned");
+    if (((uintptr_t)q | (uintptr_t)cache | (uintptr_t)out | (uintptr_t)workspace) & 15)
+        return fail(LQ_ERR_ALIGN, "q, cache, out and workspace must be 16-byte aligned");
     if (((uintptr_t)block_table | (uintptr_t)context) & 3) return fail(LQ_ERR_ALIGN, "block_table and context must be 4-byte aligned");
     if ((n_seqs > 1 && q_seq % 8) || (n_new > 1 && q_token % 8) || (Hq > 1 && q_head % 8))
         return fail(LQ_ERR_ALIGN, "q: strides must be multiples of 8 elements, got %lld, %lld and %lld", q_seq, q_token, q_head);
-    (void)workspace, (void)workspace_bytes;
-    const DecodeArgs a{q, q_seq, q_token, q_head, static_cast<const uint8_t *>(cache), block_table, context, out, n_new, Hq, Hkv, Hq / Hkv,
-                       (int)rows, (int)tiles, table_width, num_pages, log2_of(page_size), scale * 1.44269504f};
-    const dim3 grid((unsigned)(tiles * Hkv * n_seqs));
+    // units are counted in 32 bits; no more of them than this
+    const long long most = items * n_seqs * (((long long)table_width * page_size + kUnit - 1) / kUnit);
+    const bool split = workspace && workspace_bytes >= kv4_attention_workspace_size(n_seqs, n_new, Hq, Hkv, head_dim) && most < (1LL << 31);
+    const DecodeArgs a{q, q_seq, q_token, q_head, static_cast<const uint8_t *>(cache), block_table, context, out,
+                       static_cast<unsigned *>(workspace), split ? reinterpret_cast<float *>(static_cast<char *>(workspace) + kTickets) : nullptr,
+                       n_seqs, n_new, Hq, Hkv, Hq / Hkv, (int)rows, (int)tiles, table_width, num_pages, log2_of(page_size), split,
+                       target_of(RT), scale * 1.44269504f};
+    const dim3 grid((unsigned)(split ? std::min<long long>(target_of(RT) + items * n_seqs, most) : items * n_seqs));
     (void)hipGetLastError();
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kDecodeWaves), 0, static_cast<hipStream_t>(hip_stream), a); };
-    if (dtype == LQ_F16)
-        head_dim == 128 ? go(kv4_attention_kernel<128, f16>) : go(kv4_attention_kernel<64, f16>);
-    else
-        head_dim == 128 ? go(kv4_attention_kernel<128, bf16>) : go(kv4_attention_kernel<64, bf16>);
+    auto by_dim = [&](auto x) {
+        using T = decltype(x);
+        if (head_dim == 128)
+            RT == 1 ? go(kv4_attention_kernel<128, T, 1>) : go(kv4_attention_kernel<128, T, 2>);
+        else
+            RT == 1 ? go(kv4_attention_kernel<64, T, 1>) : go(kv4_attention_kernel<64, T, 2>);
+    };
+    dtype == LQ_F16 ? by_dim(f16{}) : by_dim(bf16{});
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? LQ_OK : fail(LQ_ERR_HIP, "attention launch failed: %s", hipGetErrorString(e));
 }
