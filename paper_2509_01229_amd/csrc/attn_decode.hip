@@ -64,6 +64,19 @@ __device__ __forceinline__ float across_groups(float x, F f)
     return f(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
 }
 
+// lane i: f over lanes 0 .. i (f with 0 has to leave a value as it is)
+template <class F>
+__device__ __forceinline__ int lanes_up_to(int x, F f)
+{
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));  // row_shr 1, 2, 4, 8
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));  // row_bcast 15, 31
+    return f(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+}
+__device__ __forceinline__ int sums_up_to(int x) { return lanes_up_to(x, [](int a, int b) { return a + b; }); }
+
 // What a wave loads for 32 keys (two tiles of 16): the keys' part and the values'.  `head`: the kv head's bytes of the tile's page as a
 // buffer, of length zero where nothing is to be loaded (so that a load is never behind a branch, and the compiler can count those in flight).
 typedef __amdgpu_buffer_rsrc_t buf_t;
@@ -112,16 +125,11 @@ constexpr float kWeightBits = 6.0f;       // a row's largest weight is 2^6 when 
 // last of its blocks to arrive at its ticket: each leaves its maxima, sums and unscaled results in the workspace (written and read past
 // the L2s, which the XCDs do not share), in the order of the split chunks of all items; the ticket is that of the item's first.
 // A sequence without keys has one unit all the same (its zeros are written there).  With split = 0 a block is an item.
-#ifndef KV4_OCC1
-#define KV4_OCC1 4
+constexpr int kMaxParts = 32;
+#ifndef KV4_OCC2
+#define KV4_OCC2 3
 #endif
-#ifndef KV4_MIN_UNITS
-#define KV4_MIN_UNITS 1
-#endif
-#ifndef KV4_ROUNDS
-#define KV4_ROUNDS 1
-#endif
-constexpr int kMaxParts = 64, kMinUnits = KV4_MIN_UNITS;
+__host__ __device__ constexpr int blocks_per_cu(int row_tiles) { return row_tiles == 1 ? 4 : KV4_OCC2; }
 constexpr size_t kTickets = 32768;  // bytes at the head of the workspace, those of the GEMM's
 __host__ __device__ constexpr int part_floats(int rows, int D) { return rows * (D + 4); }
 
@@ -132,12 +140,13 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t shared_buffer(float *p, int by
 
 // (RT: tiles of 16 rows that share a pass over the keys)
 template <int D, class T, int RT>
-__global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? KV4_OCC1 : 2) void kv4_attention_kernel(const DecodeArgs a)
+__global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_attention_kernel(const DecodeArgs a)
 {
     constexpr int W = D / 16, STEPS = D / 32;  // elements of a column group; MFMAs of a key tile
     constexpr int ROWS = 16 * RT;
     __shared__ float s_o[kDecodeWaves][16][D + 4], s_m[kDecodeWaves][ROWS], s_l[kDecodeWaves][ROWS];
     __shared__ int s_last;
+    __shared__ vec<f16, 8> s_q[RT > 1 ? RT : 1][RT > 1 ? STEPS : 1][RT > 1 ? 64 : 1];  // (the waves have the same queries)
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int P = 1 << a.lg_page, items = a.Hkv * a.row_tiles;
@@ -149,34 +158,31 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? KV4_OCC1 : 2) void kv4
     const auto context = [&](int s) { return min(max(contexts[s], 0), longest); };
 
     // this block's sequence, item and units; the item's chunks, and where they are among the split ones
-    int seq, item, unit = 0, count, chunks = 1, chunk = 0, first_part = 0;
+    int seq, item, unit = 0, units = 1, count, chunks = 1, chunk = 0, first_part = 0;
     if (a.split) {
         int total = 0, most = 0;
+        const int first64 = lane < a.n_seqs ? units_of(context(lane)) : 0;
+        const auto units64 = [&](int s0) { return s0 == 0 ? first64 : s0 + lane < a.n_seqs ? units_of(context(s0 + lane)) : 0; };
         for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-            const int s = s0 + lane, u = s < a.n_seqs ? units_of(context(s)) : 0;
-            int sum = u, top = u;
-            for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d), top = max(top, __shfl_xor(top, d));
-            total += sum;
-            most = max(most, top);
+            const int u = units64(s0);
+            total += __builtin_amdgcn_readlane(sums_up_to(u), 63);
+            most = max(most, __builtin_amdgcn_readlane(lanes_up_to(u, [](int x, int y) { return max(x, y); }), 63));
         }
-        total = __builtin_amdgcn_readfirstlane(total) * items;
-        most = __builtin_amdgcn_readfirstlane(most);
-        const int size = max(max((total + a.target - 1) / a.target, kMinUnits), (most + kMaxParts - 1) / kMaxParts);  // units of a chunk
+        total *= items;
+        // Units of a chunk: as many as make a.target chunks, but joining a part costs the last block about a quarter of a unit where there
+        // are few, and more than kMaxParts of them are never ahead.
+        const int size = max(max((total + a.target - 1) / a.target, (int)__builtin_sqrtf(0.25f * (float)most)), (most + kMaxParts - 1) / kMaxParts);
         int before = 0, parts = 0;  // chunks, split chunks of the sequences that come before
         seq = -1;
         for (int s0 = 0; seq < 0 && s0 < a.n_seqs; s0 += 64) {
-            const int s = s0 + lane, c = s < a.n_seqs ? (units_of(context(s)) + size - 1) / size : 0;
-            int sum = c, split = c > 1 ? c : 0;
-            for (int d = 1; d < 64; d <<= 1) {
-                const int x = __shfl_up(sum, d), y = __shfl_up(split, d);
-                if (lane >= d) sum += x, split += y;
-            }
+            const int u = units64(s0), c = (u + size - 1) / size, sum = sums_up_to(c), split = sums_up_to(c > 1 ? c : 0);
             const uint64_t past = __ballot((before + sum) * items > (int)blockIdx.x);
             const int at = past ? __builtin_ctzll(past) : 63;
             before += __builtin_amdgcn_readlane(sum, at);
             parts += __builtin_amdgcn_readlane(split, at);
             if (past) {
                 seq = s0 + at;
+                units = __builtin_amdgcn_readlane(u, at);
                 chunks = __builtin_amdgcn_readlane(c, at);
                 before -= chunks;
                 if (chunks > 1) parts -= chunks;
@@ -187,8 +193,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? KV4_OCC1 : 2) void kv4
         item = inside / chunks;
         chunk = inside % chunks;
         first_part = parts * items + item * chunks;
-        unit = chunk * size;
-        count = min(size, units_of(context(seq)) - unit);
+        unit = (int)((unsigned)chunk * (unsigned)units / (unsigned)chunks);
+        count = (int)((unsigned)(chunk + 1) * (unsigned)units / (unsigned)chunks) - unit;
     } else {
         seq = (int)blockIdx.x / items;
         item = (int)blockIdx.x % items;
@@ -203,7 +209,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? KV4_OCC1 : 2) void kv4
         int limit[RT];                        // keys that this lane's rows see
 
         // queries: operand order of the keys (see integers8)
-        vec<f16, 8> q[RT][STEPS];
+        vec<f16, 8> q[STEPS];
         float q_scale[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
@@ -234,7 +240,10 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? KV4_OCC1 : 2) void kv4
 #pragma unroll
             for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) q[r][i][2 * j] = (f16)f[i][j], q[r][i][2 * j + 1] = (f16)f[i][j + 4];
+                for (int j = 0; j < 4; ++j) q[i][2 * j] = (f16)f[i][j], q[i][2 * j + 1] = (f16)f[i][j + 4];
+            if constexpr (RT > 1)
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i) s_q[r][i][lane] = q[i];  // (each wave writes all of them, the same)
         }
 
         v4f o[RT][W] = {};
@@ -287,7 +296,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? KV4_OCC1 : 2) void kv4
                     integers8(xk.k[t][i], even, odd, k8);
 #pragma unroll
                     for (int r = 0; r < RT; ++r)
-                        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec<f16, 8>, u32x4{k8[0], k8[1], k8[2], k8[3]}), q[r][i],
+                        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec<f16, 8>, u32x4{k8[0], k8[1], k8[2], k8[3]}), RT > 1 ? s_q[RT > 1 ? r : 0][RT > 1 ? i : 0][RT > 1 ? lane : 0] : q[i],
                                                                         acc[r], 0, 0, 0);
                 }
 #pragma unroll
@@ -421,8 +430,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? KV4_OCC1 : 2) void kv4
         float most[RT], sum[RT], f[RT][8];
         constexpr int STEP = 64 * kDecodeWaves;
         static_assert(16 * D / 8 <= STEP, "");
-        const int r16 = (int)threadIdx.x / (D / 8), c = (int)threadIdx.x % (D / 8) * 8;
-        const bool mine = threadIdx.x < 16 * D / 8;
+        const int c = (int)threadIdx.x % (D / 8) * 8;
+        int r16 = (int)threadIdx.x / (D / 8);
+        bool mine = threadIdx.x < 16 * D / 8;
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             if (r) __syncthreads();
@@ -449,9 +459,10 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? KV4_OCC1 : 2) void kv4
         if (chunks > 1) {
             float *const parts = a.parts + (size_t)first_part * part_floats(ROWS, D);
             const auto mine_at = shared_buffer(parts + (size_t)chunk * part_floats(ROWS, D), part_floats(ROWS, D) * 4);
-            if (mine) {
+            {
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
+                    if (!mine || rt * ROWS + 16 * r + r16 >= a.rows) continue;
                     const int at = ((16 * r + r16) * D + c) * 4;
                     __builtin_amdgcn_raw_buffer_store_b128(u32x4{__builtin_bit_cast(u32x4, v4f{f[r][0], f[r][1], f[r][2], f[r][3]})}, mine_at, at, 0, kShared);
                     __builtin_amdgcn_raw_buffer_store_b128(u32x4{__builtin_bit_cast(u32x4, v4f{f[r][4], f[r][5], f[r][6], f[r][7]})}, mine_at, at + 16, 0, kShared);
@@ -469,43 +480,60 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? KV4_OCC1 : 2) void kv4
             }
             __syncthreads();
             if (!s_last) return;
-            if (mine) {
-                constexpr int U = 4;  // parts whose loads are in flight together
+            // threads: piece (8 elements) of a real row, and as many groups of threads as there are for the parts
+            const int left = a.rows - rt * ROWS, rows16 = left >= 9 ? 16 : left >= 5 ? 8 : left >= 3 ? 4 : left;  // (a power of two)
+            const int pieces = rows16 * (D / 8), groups = 64 * kDecodeWaves / pieces, group = (int)threadIdx.x / pieces;
+            r16 = (int)threadIdx.x / (D / 8) % rows16;
+            float *const s_f = &s_o[0][0][0];
+            constexpr int U = 4;  // parts whose loads are in flight together
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    most[r] = -__builtin_inff();
-                    sum[r] = 0.0f;
+            for (int r = 0; r < RT; ++r) {
+                most[r] = -__builtin_inff();
+                sum[r] = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) f[r][e] = 0.0f;
-                    for (int w = 0; w < chunks; w += U) {
-                        v4f x[U][2], ml[U];
+                for (int e = 0; e < 8; ++e) f[r][e] = 0.0f;
+                const auto add = [&](float m, float l, const float (&x)[8]) {
+                    const float now = fmaxf(most[r], m);
+                    const float old = most[r] == now ? 1.0f : __builtin_amdgcn_exp2f(most[r] - now);
+                    const float by = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - now);
+                    most[r] = now;
+                    sum[r] = sum[r] * old + l * by;
 #pragma unroll
-                        for (int u = 0; u < U; ++u) {  // (past the last: the last once more, without weight)
-                            const auto from = shared_buffer(parts + (size_t)min(w + u, chunks - 1) * part_floats(ROWS, D), part_floats(ROWS, D) * 4);
-                            const int at = ((16 * r + r16) * D + c) * 4;
-                            ml[u] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, (ROWS * D + (16 * r + r16) * 4) * 4, 0, kShared));
-                            x[u][0] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at, 0, kShared));
-                            x[u][1] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at + 16, 0, kShared));
-                        }
-                        float now = most[r];
+                    for (int e = 0; e < 8; ++e) f[r][e] = f[r][e] * old + x[e] * by;
+                };
+                for (int w = group; w < chunks; w += U * groups) {
+                    v4f x[U][2], ml[U];
 #pragma unroll
-                        for (int u = 0; u < U; ++u) now = fmaxf(now, ml[u][0]);
-                        const float old = most[r] == now ? 1.0f : __builtin_amdgcn_exp2f(most[r] - now);
-                        most[r] = now;
-                        sum[r] *= old;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) f[r][e] *= old;
-#pragma unroll
-                        for (int u = 0; u < U; ++u) {
-                            if (w + u >= chunks) break;  // (uniform)
-                            const float by = ml[u][0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ml[u][0] - now);
-                            sum[r] += ml[u][1] * by;
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) f[r][e] += x[u][e >> 2][e & 3] * by;
-                        }
+                    for (int u = 0; u < U; ++u) {  // (past the last: the last once more, not added)
+                        const auto from = shared_buffer(parts, chunks * part_floats(ROWS, D) * 4);
+                        const int at = min(w + u * groups, chunks - 1) * part_floats(ROWS, D) * 4;
+                        ml[u] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at + (ROWS * D + (16 * r + r16) * 4) * 4, 0, kShared));
+                        x[u][0] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at + ((16 * r + r16) * D + c) * 4, 0, kShared));
+                        x[u][1] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at + ((16 * r + r16) * D + c) * 4 + 16, 0, kShared));
                     }
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (w + u * groups < chunks) {
+                            const float x8[8] = {x[u][0][0], x[u][0][1], x[u][0][2], x[u][0][3], x[u][1][0], x[u][1][1], x[u][1][2], x[u][1][3]};
+                            add(ml[u][0], ml[u][1], x8);
+                        }
+                }
+                if (groups > 1) {  // (one tile of rows, then: the last)
+                    float *const to = s_f + threadIdx.x * 10;
+                    to[0] = most[r], to[1] = sum[r];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) to[2 + e] = f[r][e];
+                    __syncthreads();
+                    if (group == 0)
+                        for (int w = 1; w < groups; ++w) {
+                            const float *const from = s_f + (threadIdx.x + w * pieces) * 10;
+                            const float x8[8] = {from[2], from[3], from[4], from[5], from[6], from[7], from[8], from[9]};
+                            add(from[0], from[1], x8);
+                        }
+                    __syncthreads();
                 }
             }
+            mine = group == 0;
         }
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
@@ -526,8 +554,8 @@ using namespace lqq;
 
 // Rows that share a pass: one tile of 16, or two
 static int row_tiles_of(int rows) { return rows <= 16 ? 1 : 2; }
-// Blocks that have work where the keys can be split: as many as the CUs hold at a time (KV4_ROUNDS times)
-static int target_of(int row_tiles) { return KV4_ROUNDS * 256 * (row_tiles == 1 ? KV4_OCC1 : 2); }
+// Blocks that have work where the keys can be split: as many as the CUs hold at a time
+static int target_of(int row_tiles) { return 256 * blocks_per_cu(row_tiles); }
 
 extern "C" size_t kv4_attention_workspace_size(int n_seqs, int n_new, int Hq, int Hkv, int head_dim)
 {
