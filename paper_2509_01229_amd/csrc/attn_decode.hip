@@ -6,8 +6,10 @@
 //
 // What is read is 17/16 of 4 bits an element, so the arithmetic has to stay small: 3.2 instruction slots of a lane for each code at the
 // rate of memory.  Both products run on 16x16x32 MFMAs with the cache as the first operand (S^T = K Q^T, O^T = V^T P^T):
-//   - codes become FP16 integers in 9 instructions for 8 (and-or into 1024 + code or 64 + code, subtract 1024 + z or 64 + z: all
-//     exact); the scales stay out of the operands, a key's is applied to its scores, a value's to its weights;
+//   - the codes go into them as they are: masked out of their dword (5 instructions for 8), they are subnormal FP16 numbers, which the matrix
+//     cores multiply exactly; the scales are applied to the scores (keys) and to the weights (values).  The keys' zero points take an
+//     MFMA of their own (with the sum of a query's elements); the values' are taken off the codes (4 more instructions), as their
+//     sums may cancel;
 //   - the scores come out with 4 keys of one row in a lane, which is the order in which the weights go into the second product, so
 //     nothing moves between lanes; the keys of a 16-byte piece of values are those of the lane's scores.
 // Weights are rounded to FP16 (2^-11 of each; the sums are FP32), as 2^6 .. 2^14 where they count most, times the value's
@@ -32,27 +34,35 @@ struct DecodeArgs {
     float scale_log2;  // softmax scale / ln 2
 };
 
-__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b)
-{
-    return __builtin_bit_cast(uint32_t, (f16x2v)(__builtin_bit_cast(f16x2v, a) - __builtin_bit_cast(f16x2v, b)));
-}
-// (w & mask) | bits in one instruction (the compiler takes two: it keeps both constants as literals)
-__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits)
-{
-    uint32_t r;
-    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(w), "s"(mask), "v"(bits));
-    return r;
-}
-// 8 nibbles of a dword as 4 pairs of FP16 integers, the zero points taken off: pair r = nibbles r and r + 4.
-// even = 0x6400 + z in both halves (1024 + z), odd = 0x5400 + (z << 4) (64 + z)
-__device__ __forceinline__ void integers8(uint32_t w, uint32_t even, uint32_t odd, uint32_t (&o)[4])
+// 8 nibbles of a dword as 4 pairs of FP16 numbers: pair r = nibbles r and r + 4, which as subnormal numbers are 2^-24 of the code (r
+// even) or 2^-20 of it (r odd)
+__device__ __forceinline__ void halves8(uint32_t w, uint32_t (&o)[4])
 {
     const uint32_t w8 = w >> 8;
-    o[0] = sub_f16x2(and_or(w, 0x000f000fu, 0x64006400u), even);
-    o[1] = sub_f16x2(and_or(w, 0x00f000f0u, 0x54005400u), odd);
-    o[2] = sub_f16x2(and_or(w8, 0x000f000fu, 0x64006400u), even);
-    o[3] = sub_f16x2(and_or(w8, 0x00f000f0u, 0x54005400u), odd);
+    o[0] = w & 0x000f000fu;
+    o[1] = w & 0x00f000f0u;
+    o[2] = w8 & 0x000f000fu;
+    o[3] = w8 & 0x00f000f0u;
 }
+// the same with the zero points of both halves taken off: exact, subnormal numbers all of them
+__device__ __forceinline__ void halves8(uint32_t w, uint32_t zz, uint32_t (&o)[4])
+{
+    halves8(w, o);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        o[r] = __builtin_bit_cast(uint32_t, (f16x2v)(__builtin_bit_cast(f16x2v, o[r]) - __builtin_bit_cast(f16x2v, r & 1 ? zz << 4 : zz)));
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));  // (a NaN is left out)
+    return r;
+}
+__device__ __forceinline__ v4f mfma16(const uint32_t (&a)[4], vec<f16, 8> b, v4f c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec<f16, 8>, u32x4{a[0], a[1], a[2], a[3]}), b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
 
 // over the four groups of 16 lanes: every lane gets the result of its column
 template <class F>
@@ -79,15 +89,18 @@ __device__ __forceinline__ int sums_up_to(int x) { return lanes_up_to(x, [](int 
 
 // What a wave loads for 32 keys (two tiles of 16): the keys' part and the values'.  `head`: the kv head's bytes of the tile's page as a
 // buffer, of length zero where nothing is to be loaded (so that a load is never behind a branch, and the compiler can count those in flight).
+#ifndef KV4_AUX
+#define KV4_AUX 2
+#endif
 typedef __amdgpu_buffer_rsrc_t buf_t;
 template <int N>
 __device__ __forceinline__ void load_dwords(uint32_t (&x)[N], buf_t b, int lane_offset, int offset)
 {
     if constexpr (N == 4) {
-        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, lane_offset, offset, 0);
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, lane_offset, offset, KV4_AUX);
         x[0] = v[0], x[1] = v[1], x[2] = v[2], x[3] = v[3];
     } else {
-        const auto v = __builtin_amdgcn_raw_buffer_load_b64(b, lane_offset, offset, 0);
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(b, lane_offset, offset, KV4_AUX);
         x[0] = v[0], x[1] = v[1];
     }
 }
@@ -125,9 +138,12 @@ constexpr float kWeightBits = 6.0f;       // a row's largest weight is 2^6 when 
 // last of its blocks to arrive at its ticket: each leaves its maxima, sums and unscaled results in the workspace (written and read past
 // the L2s, which the XCDs do not share), in the order of the split chunks of all items; the ticket is that of the item's first.
 // A sequence without keys has one unit all the same (its zeros are written there).  With split = 0 a block is an item.
-constexpr int kMaxParts = 32;
+#ifndef KV4_PARTS
+#define KV4_PARTS 32
+#endif
+constexpr int kMaxParts = KV4_PARTS;
 #ifndef KV4_OCC2
-#define KV4_OCC2 3
+#define KV4_OCC2 2
 #endif
 __host__ __device__ constexpr int blocks_per_cu(int row_tiles) { return row_tiles == 1 ? 4 : KV4_OCC2; }
 constexpr size_t kTickets = 32768;  // bytes at the head of the workspace, those of the GEMM's
@@ -146,7 +162,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
     constexpr int ROWS = 16 * RT;
     __shared__ float s_o[kDecodeWaves][16][D + 4], s_m[kDecodeWaves][ROWS], s_l[kDecodeWaves][ROWS];
     __shared__ int s_last;
-    __shared__ vec<f16, 8> s_q[RT > 1 ? RT : 1][RT > 1 ? STEPS : 1][RT > 1 ? 64 : 1];  // (the waves have the same queries)
+    __shared__ vec<f16, 8> s_q[RT][STEPS + 1][64];  // (the waves have the same queries)
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int P = 1 << a.lg_page, items = a.Hkv * a.row_tiles;
@@ -208,50 +224,6 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
         const int ctx = context(seq), end = min(ctx, (unit + count) * kUnit);
         int limit[RT];                        // keys that this lane's rows see
 
-        // queries: operand order of the keys (see integers8)
-        vec<f16, 8> q[STEPS];
-        float q_scale[RT];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const int row = rt * ROWS + r * 16 + n, token = min(row / a.group, a.n_new - 1), head = hk * a.group + row % a.group;
-            const bool real = row < a.rows;
-            limit[r] = real ? ctx - a.n_new + 1 + token : 0;
-            q_scale[r] = fmaxf(fabsf(a.scale_log2), 0x1p-126f);  // (its sign goes with the queries)
-            float f[STEPS][8];
-            const T *src = static_cast<const T *>(a.q) + seq * a.q_seq + token * a.q_token + (real ? head : hk * a.group) * a.q_head + g * (D / 4);
-            const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;
-            float most = 0.0f;
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                const vec<T, 8> x = *reinterpret_cast<const vec<T, 8> *>(src + 8 * i);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[i][e] = real ? (float)x[e] * sign : 0.0f, most = fmaxf(most, fabsf(f[i][e]));
-            }
-            if constexpr (!__is_same(T, f16)) {
-                // BF16: times a power of two that brings the row below 2 (exact down to 2^-14 of its largest element)
-                most = across_groups(most, [](float x, float y) { return fmaxf(x, y); });
-                const int e = min(max((int)(__builtin_bit_cast(uint32_t, most) >> 23), 27), 227) - 127;
-                q_scale[r] *= __builtin_ldexpf(1.0f, e);
-#pragma unroll
-                for (int i = 0; i < STEPS; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f[i][j] = __builtin_ldexpf(f[i][j], -e);
-            }
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) q[i][2 * j] = (f16)f[i][j], q[i][2 * j + 1] = (f16)f[i][j + 4];
-            if constexpr (RT > 1)
-#pragma unroll
-                for (int i = 0; i < STEPS; ++i) s_q[r][i][lane] = q[i];  // (each wave writes all of them, the same)
-        }
-
-        v4f o[RT][W] = {};
-        float m[RT], l[RT] = {};  // a row's maximum (as sc), this lane's part of its sum
-        float m_up[RT], base[RT] = {};  // the score from which the maximum moves; kWeightBits less the maximum times q_scale
-#pragma unroll
-        for (int r = 0; r < RT; ++r) m[r] = m_up[r] = -__builtin_inff();
-        float v_top = 0x1p-126f, v_inv = 0.0f;  // power of two that no value's scale so far is above, and 2^-.. of it
         const int last_page = max((ctx - 1) >> a.lg_page, 0);
 
         // the pages of 32 keys: numbers first, then addresses
@@ -280,32 +252,112 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
         };
         Keys<D> xk;
         Values<D> xv;
+        // the queries, then the first keys and values: in flight together
+        vec<T, 8> raw[RT][STEPS];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int row = rt * ROWS + r * 16 + n, token = min(row / a.group, a.n_new - 1), head = hk * a.group + row % a.group;
+            const bool real = row < a.rows;
+            limit[r] = real ? ctx - a.n_new + 1 + token : 0;
+            const T *src = static_cast<const T *>(a.q) + seq * a.q_seq + token * a.q_token + (real ? head : hk * a.group) * a.q_head + g * (D / 4);
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) raw[r][i] = *reinterpret_cast<const vec<T, 8> *>(src + 8 * i);
+        }
+        int key = unit * kUnit + 32 * wave;
+        Place next{};
+        if (key < end) {
+            go_to(pages_of(key), true);
+            __builtin_amdgcn_sched_barrier(0);
+            load(xk, key);
+            __builtin_amdgcn_sched_barrier(0);  // (in the order of the loop's)
+            load(xv, key);
+            __builtin_amdgcn_sched_barrier(0);
+            next = pages_of(key + kUnit);
+        }
+        // Queries in the keys' operand order, times a power of two that brings the row's largest element to 4 .. 8 (exact down to 2^-16 of
+        // it), those that meet even pairs (halves8) times 16.  A last operand holds what the zero points are multiplied with, minus 16 times
+        // the sum of the row's elements, as three numbers (33 bits of it).
+        constexpr int Q = STEPS + 1;
+        float q_scale[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const bool real = rt * ROWS + r * 16 + n < a.rows;
+            float f[STEPS][8];
+            const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;  // (the scale's)
+            float most = 0.0f;
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[i][e] = real ? (float)raw[r][i][e] * sign : 0.0f, most = fmaxf(most, fabsf(f[i][e]));
+            }
+            most = across_groups(most, [](float x, float y) { return fmaxf(x, y); });
+            const int e = min(max((int)(__builtin_bit_cast(uint32_t, most) >> 23), 29), 227) - 129;
+            q_scale[r] = fmaxf(fabsf(a.scale_log2), 0x1p-126f) * 0x1p20f * power_of_two(e);
+            vec<f16, 8> q[Q];
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const f16 x = (f16)(f[i][j] * power_of_two(-e));
+                    sum += (float)x;
+                    q[i][2 * (j & 3) + (j >> 2)] = j & 1 ? x : x * (f16)16.0f;
+                }
+            sum = -16.0f * across_groups(sum, [](float x, float y) { return x + y; });
+            const f16 s0 = (f16)sum, s1 = (f16)(sum - (float)s0), s2 = (f16)(sum - (float)s0 - (float)s1);
+            q[STEPS] = vec<f16, 8>{};
+            if (g == 0) q[STEPS][0] = s0, q[STEPS][1] = s1, q[STEPS][2] = s2;
+#pragma unroll
+            for (int i = 0; i < Q; ++i) s_q[r][i][lane] = q[i];  // (each wave writes all of them, the same)
+        }
+        const auto query = [&](int r, int i) { return s_q[r][i][lane]; };
+
+        v4f o[RT][W] = {};
+        float m[RT], l[RT] = {};   // a row's maximum (as sc), this lane's part of its sum
+        float m_up[RT], base[RT];  // the score from which the maximum moves; see below
+#pragma unroll
+        for (int r = 0; r < RT; ++r) m[r] = m_up[r] = -__builtin_inff(), base[r] = 0.0f;
+        // Weights are over 2^v_exp, a power of two that no value's scale so far is above: 2^v_in of it in the exponent (and in l), the rest,
+        // where v_exp is very far from 0, by a factor.
+        int v_exp = -126, v_in = -90;
+        float v_top = power_of_two(v_exp);
+        const auto base_of = [&](int r) { return m[r] == -__builtin_inff() ? 0.0f : kWeightBits - (float)v_in - m[r] * q_scale[r]; };
         // a step takes 32 keys; the next ones' registers are those that it has just used
         const auto step = [&](int key, bool more, Place &next) {
             float sc[RT][2][4];  // scores over q_scale
             float sv[2][4];      // scales of the values (with the zero points still in their last bits: 2^-19 of them)
             float vt = 0.0f;
             const bool tail = key + 32 > ctx - a.n_new + 1;  // some row does not see all of these keys
+            v4f acc[2][RT];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const uint32_t z = xk.z[t] & 15u, zz = z | z << 16, even = 0x64006400u | zz, odd = 0x54005400u | zz << 4;
-                v4f acc[RT] = {};
+            for (int r = 0; r < RT; ++r) {
+                const auto qi = query(r, STEPS);
 #pragma unroll
-                for (int i = 0; i < STEPS; ++i) {
-                    uint32_t k8[4];
-                    integers8(xk.k[t][i], even, odd, k8);
-#pragma unroll
-                    for (int r = 0; r < RT; ++r)
-                        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec<f16, 8>, u32x4{k8[0], k8[1], k8[2], k8[3]}), RT > 1 ? s_q[RT > 1 ? r : 0][RT > 1 ? i : 0][RT > 1 ? lane : 0] : q[i],
-                                                                        acc[r], 0, 0, 0);
+                for (int t = 0; t < 2; ++t) {
+                    const uint32_t z = xk.z[t] & 15u, zz = z | z << 16, zeros[4] = {zz, zz, 0, 0};
+                    acc[t][r] = mfma16(zeros, qi, v4f{});
                 }
+            }
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                uint32_t k8[2][4];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) halves8(xk.k[t][i], k8[t]);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    const auto qi = query(r, i);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) acc[t][r] = mfma16(k8[t], qi, acc[t][r]);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float sk = __builtin_bit_cast(float, xk.w[t][i] & kScaleMask);
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) sc[r][t][i] = acc[r][i] * sk;
+                    for (int r = 0; r < RT; ++r) sc[r][t][i] = acc[t][r][i] * sk;
                 }
-            }
             go_to(next, more);
             load(xk, key + kUnit);
             next = pages_of(key + 2 * kUnit);
@@ -330,24 +382,24 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
                     }
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) vt = fmaxf(vt, sv[i >> 2][i & 3]);
+            for (int i = 0; i < 8; i += 2) vt = max3(vt, sv[i >> 2][i & 3], sv[i >> 2][(i & 3) + 1]);
             float top[RT];
             bool up = false;
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                top[r] = sc[r][0][0];
+                top[r] = m[r];
 #pragma unroll
-                for (int i = 1; i < 8; ++i) top[r] = fmaxf(top[r], sc[r][i >> 2][i & 3]);
+                for (int i = 0; i < 8; i += 2) top[r] = max3(top[r], sc[r][i >> 2][i & 3], sc[r][i >> 2][(i & 3) + 1]);
                 up |= top[r] > m_up[r];
             }
             if (__any(up)) {  // (first of all: m is minus infinity)
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
                     top[r] = across_groups(top[r], [](float u, float w) { return fmaxf(u, w); });
-                    const float now = fmaxf(m[r], top[r]), by = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m[r] - now) * q_scale[r]);
+                    const float now = top[r], by = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m[r] - now) * q_scale[r]);
                     m[r] = now;
                     m_up[r] = now + (14.0f - kWeightBits) / q_scale[r];
-                    base[r] = now == -__builtin_inff() ? 0.0f : kWeightBits - now * q_scale[r];
+                    base[r] = base_of(r);
                     l[r] *= by;
 #pragma unroll
                     for (int e = 0; e < W; ++e) o[r][e] *= by;
@@ -355,14 +407,19 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
             }
             if (__any(vt > v_top)) {
                 for (int d = 1; d < 64; d <<= 1) vt = fmaxf(vt, __shfl_xor(vt, d));
-                const uint32_t e = min((__builtin_bit_cast(uint32_t, vt) >> 23) + 1u, 253u);  // the next power of two
-                const float next = __builtin_bit_cast(float, e << 23), by = v_top / next;
+                const int e = __builtin_amdgcn_readfirstlane(min((int)(__builtin_bit_cast(uint32_t, vt) >> 23) - 126, 126));  // the next power of two
+                const int in = min(max(e, -90), 90);
+                const float by = power_of_two(max(v_exp - e, -126)), by_l = power_of_two(max(v_in - in, -126));
+                v_exp = e;
+                v_in = in;
+                v_top = power_of_two(e);
 #pragma unroll
-                for (int r = 0; r < RT; ++r)
+                for (int r = 0; r < RT; ++r) {
+                    base[r] = base_of(r);
+                    l[r] *= by_l;
 #pragma unroll
                     for (int i = 0; i < W; ++i) o[r][i] *= by;
-                v_top = next;
-                v_inv = 1.0f / next;
+                }
             }
             vec<f16, 8> weights[RT];
 #pragma unroll
@@ -375,7 +432,12 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
                     for (int i = 0; i < 4; ++i) {
                         p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r][t][i], q_scale[r], base[r]));
                         l[r] += p[i];
-                        p[i] *= sv[t][i] * v_inv;
+                        p[i] *= sv[t][i];
+                    }
+                    if (v_exp != v_in) {
+                        asm volatile("");
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) p[i] *= power_of_two(v_in - v_exp);
                     }
                     if (tail) {  // (whatever the scale there is)
                         asm volatile("");
@@ -394,37 +456,27 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
                 for (int i = 0; i < 2; ++i) zz[2 * t + i] = __builtin_amdgcn_perm(xv.w[t][2 * i + 1], xv.w[t][2 * i], 0x0c040c00u) & 0x000f000fu;
 #pragma unroll
             for (int h = 0; h < W / 4; ++h) {
-                uint32_t v8[4][4];  // [pair][element of the four]
+                uint32_t v8[4][4];  // [pair of keys][element of the four]
 #pragma unroll
-                for (int p2 = 0; p2 < 4; ++p2)
-                    integers8(xv.v[p2 >> 1][(p2 & 1) * (W / 4) + h], 0x64006400u | zz[p2], 0x54005400u | zz[p2] << 4, v8[p2]);
+                for (int p2 = 0; p2 < 4; ++p2) halves8(xv.v[p2 >> 1][(p2 & 1) * (W / 4) + h], zz[p2], v8[p2]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t x[4] = {v8[0][e], v8[1][e], v8[2][e], v8[3][e]};
 #pragma unroll
-                    for (int r = 0; r < RT; ++r)
-                        o[r][4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                            __builtin_bit_cast(vec<f16, 8>, u32x4{v8[0][e], v8[1][e], v8[2][e], v8[3][e]}), weights[r], o[r][4 * h + e], 0, 0, 0);
+                    for (int r = 0; r < RT; ++r) o[r][4 * h + e] = mfma16(x, weights[r], o[r][4 * h + e]);
+                }
             }
             load(xv, key + kUnit);
             __builtin_amdgcn_sched_barrier(0);
         };
 
-        int key = unit * kUnit + 32 * wave;
-        if (key < end) {
-            go_to(pages_of(key), true);
-            load(xk, key);
-            __builtin_amdgcn_sched_barrier(0);  // (in the order of the loop's)
-            load(xv, key);
-            __builtin_amdgcn_sched_barrier(0);
-            Place next = pages_of(key + kUnit);
-            for (; key < end; key += kUnit) step(key, key + kUnit < end, next);
-        }
+        for (; key < end; key += kUnit) step(key, key + kUnit < end, next);
         // the waves' parts: sums of weights relative to 2^(m - kWeightBits), both over 2^16 so that values near the end of FP32's range stay in it
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             l[r] = across_groups(l[r], [](float u, float w) { return u + w; });
             if (bad) l[r] = __builtin_nanf("");
-            if (g == 0) s_m[wave][16 * r + n] = m[r] * q_scale[r], s_l[wave][16 * r + n] = l[r] * 0x1p-16f;
+            if (g == 0) s_m[wave][16 * r + n] = m[r] * q_scale[r], s_l[wave][16 * r + n] = l[r] * (0x1p-16f * power_of_two(v_in));
         }
         // thread: 8 elements of a row of each tile; the waves' results one tile at a time
         float most[RT], sum[RT], f[RT][8];
@@ -439,7 +491,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
 #pragma unroll
             for (int e = 0; e < W; ++e)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s_o[wave][n][(4 * g + i) * W + e] = o[r][e][i] * 0x1p-16f * v_top;
+                for (int i = 0; i < 4; ++i) s_o[wave][n][(4 * g + i) * W + e] = o[r][e][i] * (e & 1 ? 0x1p4f : 0x1p8f) * v_top;
             __syncthreads();
             if (!mine) continue;
             most[r] = s_m[0][16 * r + r16];
@@ -485,39 +537,47 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
             const int pieces = rows16 * (D / 8), groups = 64 * kDecodeWaves / pieces, group = (int)threadIdx.x / pieces;
             r16 = (int)threadIdx.x / (D / 8) % rows16;
             float *const s_f = &s_o[0][0][0];
-            constexpr int U = 4;  // parts whose loads are in flight together
+            constexpr int U = 8 / RT;  // parts whose loads are in flight together
+            const auto add = [&](int r, float m, float l, const float (&x)[8]) {
+                const float now = fmaxf(most[r], m);
+                const float old = most[r] == now ? 1.0f : __builtin_amdgcn_exp2f(most[r] - now);
+                const float by = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - now);
+                most[r] = now;
+                sum[r] = sum[r] * old + l * by;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[r][e] = f[r][e] * old + x[e] * by;
+            };
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 most[r] = -__builtin_inff();
                 sum[r] = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[r][e] = 0.0f;
-                const auto add = [&](float m, float l, const float (&x)[8]) {
-                    const float now = fmaxf(most[r], m);
-                    const float old = most[r] == now ? 1.0f : __builtin_amdgcn_exp2f(most[r] - now);
-                    const float by = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - now);
-                    most[r] = now;
-                    sum[r] = sum[r] * old + l * by;
+            }
+            const auto from = shared_buffer(parts, chunks * part_floats(ROWS, D) * 4);
+            for (int w = group; w < chunks; w += U * groups) {
+                v4f x[U][RT][2], ml[U][RT];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) f[r][e] = f[r][e] * old + x[e] * by;
-                };
-                for (int w = group; w < chunks; w += U * groups) {
-                    v4f x[U][2], ml[U];
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {  // (past the last: the last once more, not added)
-                        const auto from = shared_buffer(parts, chunks * part_floats(ROWS, D) * 4);
-                        const int at = min(w + u * groups, chunks - 1) * part_floats(ROWS, D) * 4;
-                        ml[u] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at + (ROWS * D + (16 * r + r16) * 4) * 4, 0, kShared));
-                        x[u][0] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at + ((16 * r + r16) * D + c) * 4, 0, kShared));
-                        x[u][1] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at + ((16 * r + r16) * D + c) * 4 + 16, 0, kShared));
+                    for (int r = 0; r < RT; ++r) {  // (past the last: nothing is loaded)
+                        const int at = w + u * groups < chunks ? (w + u * groups) * part_floats(ROWS, D) * 4 : chunks * part_floats(ROWS, D) * 4;
+                        ml[u][r] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at + (ROWS * D + (16 * r + r16) * 4) * 4, 0, kShared));
+                        x[u][r][0] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at + ((16 * r + r16) * D + c) * 4, 0, kShared));
+                        x[u][r][1] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, at + ((16 * r + r16) * D + c) * 4 + 16, 0, kShared));
                     }
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
-                        if (w + u * groups < chunks) {
-                            const float x8[8] = {x[u][0][0], x[u][0][1], x[u][0][2], x[u][0][3], x[u][1][0], x[u][1][1], x[u][1][2], x[u][1][3]};
-                            add(ml[u][0], ml[u][1], x8);
+                for (int u = 0; u < U; ++u)
+                    if (w + u * groups < chunks)
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) {
+                            const v4f a = x[u][r][0], b = x[u][r][1];
+                            const float x8[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+                            add(r, ml[u][r][0], ml[u][r][1], x8);
                         }
-                }
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
                 if (groups > 1) {  // (one tile of rows, then: the last)
                     float *const to = s_f + threadIdx.x * 10;
                     to[0] = most[r], to[1] = sum[r];
@@ -525,10 +585,10 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
                     for (int e = 0; e < 8; ++e) to[2 + e] = f[r][e];
                     __syncthreads();
                     if (group == 0)
-                        for (int w = 1; w < groups; ++w) {
-                            const float *const from = s_f + (threadIdx.x + w * pieces) * 10;
-                            const float x8[8] = {from[2], from[3], from[4], from[5], from[6], from[7], from[8], from[9]};
-                            add(from[0], from[1], x8);
+                        for (int w = 1; w < min(groups, chunks); ++w) {
+                            const float *const o = s_f + (threadIdx.x + w * pieces) * 10;
+                            const float x8[8] = {o[2], o[3], o[4], o[5], o[6], o[7], o[8], o[9]};
+                            add(r, o[0], o[1], x8);
                         }
                     __syncthreads();
                 }
@@ -555,7 +615,10 @@ using namespace lqq;
 // Rows that share a pass: one tile of 16, or two
 static int row_tiles_of(int rows) { return rows <= 16 ? 1 : 2; }
 // Blocks that have work where the keys can be split: as many as the CUs hold at a time
-static int target_of(int row_tiles) { return 256 * blocks_per_cu(row_tiles); }
+#ifndef KV4_TARGET
+#define KV4_TARGET 1024
+#endif
+static int target_of(int row_tiles) { return row_tiles == 1 ? KV4_TARGET : 512; }
 
 extern "C" size_t kv4_attention_workspace_size(int n_seqs, int n_new, int Hq, int Hkv, int head_dim)
 {
