@@ -89,18 +89,16 @@ __device__ __forceinline__ int sums_up_to(int x) { return lanes_up_to(x, [](int 
 
 // What a wave loads for 32 keys (two tiles of 16): the keys' part and the values'.  `head`: the kv head's bytes of the tile's page as a
 // buffer, of length zero where nothing is to be loaded (so that a load is never behind a branch, and the compiler can count those in flight).
-#ifndef KV4_AUX
-#define KV4_AUX 2
-#endif
+constexpr int kReadOnce = 2;  // (non-temporal)
 typedef __amdgpu_buffer_rsrc_t buf_t;
 template <int N>
 __device__ __forceinline__ void load_dwords(uint32_t (&x)[N], buf_t b, int lane_offset, int offset)
 {
     if constexpr (N == 4) {
-        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, lane_offset, offset, KV4_AUX);
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, lane_offset, offset, kReadOnce);
         x[0] = v[0], x[1] = v[1], x[2] = v[2], x[3] = v[3];
     } else {
-        const auto v = __builtin_amdgcn_raw_buffer_load_b64(b, lane_offset, offset, KV4_AUX);
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(b, lane_offset, offset, kReadOnce);
         x[0] = v[0], x[1] = v[1];
     }
 }
@@ -138,14 +136,8 @@ constexpr float kWeightBits = 6.0f;       // a row's largest weight is 2^6 when 
 // last of its blocks to arrive at its ticket: each leaves its maxima, sums and unscaled results in the workspace (written and read past
 // the L2s, which the XCDs do not share), in the order of the split chunks of all items; the ticket is that of the item's first.
 // A sequence without keys has one unit all the same (its zeros are written there).  With split = 0 a block is an item.
-#ifndef KV4_PARTS
-#define KV4_PARTS 32
-#endif
-constexpr int kMaxParts = KV4_PARTS;
-#ifndef KV4_OCC2
-#define KV4_OCC2 2
-#endif
-__host__ __device__ constexpr int blocks_per_cu(int row_tiles) { return row_tiles == 1 ? 4 : KV4_OCC2; }
+constexpr int kMaxParts = 32, kLongChunk = 8;
+__host__ __device__ constexpr int blocks_per_cu(int row_tiles) { return row_tiles == 1 ? 4 : 2; }
 constexpr size_t kTickets = 32768;  // bytes at the head of the workspace, those of the GEMM's
 __host__ __device__ constexpr int part_floats(int rows, int D) { return rows * (D + 4); }
 
@@ -185,9 +177,12 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
             most = max(most, __builtin_amdgcn_readlane(lanes_up_to(u, [](int x, int y) { return max(x, y); }), 63));
         }
         total *= items;
-        // Units of a chunk: as many as make a.target chunks, but joining a part costs the last block about a quarter of a unit where there
-        // are few, and more than kMaxParts of them are never ahead.
-        const int size = max(max((total + a.target - 1) / a.target, (int)__builtin_sqrtf(0.25f * (float)most)), (most + kMaxParts - 1) / kMaxParts);
+        // Units of a chunk: as many as make a.target chunks, half as many chunks while they have at most kLongChunk units (a block's start
+        // and end cost as much as some units); and joining a part costs the last block about a quarter of a unit where there are few,
+        // more than kMaxParts of them are never ahead.  (16 contexts of 4096, 64/8 heads: 8 units 21.3 us, 4 units 24.2; two of 131072: 32 units
+        // 56.8, 16 units 71.5.)
+        const int size = max(max(max((total + a.target - 1) / a.target, min((2 * total + a.target - 1) / a.target, kLongChunk)),
+                                 (int)__builtin_sqrtf(0.25f * (float)most)), (most + kMaxParts - 1) / kMaxParts);
         int before = 0, parts = 0;  // chunks, split chunks of the sequences that come before
         seq = -1;
         for (int s0 = 0; seq < 0 && s0 < a.n_seqs; s0 += 64) {
@@ -615,10 +610,7 @@ using namespace lqq;
 // Rows that share a pass: one tile of 16, or two
 static int row_tiles_of(int rows) { return rows <= 16 ? 1 : 2; }
 // Blocks that have work where the keys can be split: as many as the CUs hold at a time
-#ifndef KV4_TARGET
-#define KV4_TARGET 1024
-#endif
-static int target_of(int row_tiles) { return row_tiles == 1 ? KV4_TARGET : 512; }
+static int target_of(int row_tiles) { return 256 * blocks_per_cu(row_tiles); }
 
 extern "C" size_t kv4_attention_workspace_size(int n_seqs, int n_new, int Hq, int Hkv, int head_dim)
 {
