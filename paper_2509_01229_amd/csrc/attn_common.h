@@ -58,4 +58,26 @@ __device__ __forceinline__ float reduce_lanes(float x, F f)
     return x;
 }
 
+// ----------------------------------------------------------------------------------- over the lanes of a wave
+// lane i: f over lanes 0 .. i (f with 0 has to leave a value as it is)
+template <class F>
+__device__ __forceinline__ int lanes_up_to(int x, F f)
+{
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));  // row_shr 1, 2, 4, 8
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));  // row_bcast 15, 31
+    return f(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+}
+__device__ __forceinline__ int sums_up_to(int x) { return lanes_up_to(x, [](int a, int b) { return a + b; }); }
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));  // (a NaN is left out)
+    return r;
+}
+__device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
+
 }  // namespace lqq

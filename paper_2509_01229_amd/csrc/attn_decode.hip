@@ -52,18 +52,10 @@ __device__ __forceinline__ void halves8(uint32_t w, uint32_t zz, uint32_t (&o)[4
     for (int r = 0; r < 4; ++r)
         o[r] = __builtin_bit_cast(uint32_t, (f16x2v)(__builtin_bit_cast(f16x2v, o[r]) - __builtin_bit_cast(f16x2v, r & 1 ? zz << 4 : zz)));
 }
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));  // (a NaN is left out)
-    return r;
-}
 __device__ __forceinline__ v4f mfma16(const uint32_t (&a)[4], vec<f16, 8> b, v4f c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec<f16, 8>, u32x4{a[0], a[1], a[2], a[3]}), b, c, 0, 0, 0);
 }
-__device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
-
 // over the four groups of 16 lanes: every lane gets the result of its column
 template <class F>
 __device__ __forceinline__ float across_groups(float x, F f)
@@ -73,19 +65,6 @@ __device__ __forceinline__ float across_groups(float x, F f)
     const auto b = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
     return f(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
 }
-
-// lane i: f over lanes 0 .. i (f with 0 has to leave a value as it is)
-template <class F>
-__device__ __forceinline__ int lanes_up_to(int x, F f)
-{
-    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));  // row_shr 1, 2, 4, 8
-    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
-    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
-    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
-    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));  // row_bcast 15, 31
-    return f(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
-}
-__device__ __forceinline__ int sums_up_to(int x) { return lanes_up_to(x, [](int a, int b) { return a + b; }); }
 
 // What a wave loads for 32 keys (two tiles of 16): the keys' part and the values'.  `head`: the kv head's bytes of the tile's page as a
 // buffer, of length zero where nothing is to be loaded (so that a load is never behind a branch, and the compiler can count those in flight).

@@ -3,13 +3,15 @@
 //     o_i = sum_j softmax_j(scale * q_i . k_j) v_j,   j < len_k,   causal: j <= i + len_k - len_q
 //
 // One pass over the keys with a running maximum and sum (FP32).  A block takes 128 queries of one head (a wave 32 of them, held as
-// MFMA operands) through the keys, 64 at a time, in LDS; both products on 32x32x16 MFMAs with the keys' side as the first operand
+// MFMA operands) through the keys, 64 at a time, which go straight into LDS while the 64 before them are worked on; both products on 32x32x16 MFMAs with the keys' side as the first operand
 // (S^T = K Q^T, O^T = V^T P^T): a lane's scores are 32 keys of one query, and they are in the order in which the weights enter the
 // second product.  The values are read from LDS transposed (ds_read_b64_tr_b16).  Weights are rounded to the type of the values.
 //
 // Keys are taken from the last to the first: the tiles that the causal mask cuts come first.  What is masked has no
 // part in the result, whatever it holds: scores by selection, and values, where a masked one is not finite, by taking
 // the tile's values that are not finite out of the product and adding them to the rows that see them.
+#include <type_traits>
+
 #include "attn_common.h"
 
 namespace lqq {
@@ -19,11 +21,12 @@ struct PromptArgs {
     long long q_token, q_head, k_token, k_head, v_token, v_head;
     const int *starts_q, *starts_k;
     void *out;
-    int n_seqs, total_q, total_k, Hq, group, causal;
+    int n_seqs, total_q, total_k, Hq, group, causal, tiles;
     float scale_log2;
 };
 
 constexpr int kQueries = 128, kKeys = 64, kPromptWaves = 4;
+constexpr float kWeightBits = 6.0f;  // a row's largest weight is 2^6 when its maximum is up to date (2^14 at most)
 
 template <class T>
 __device__ __forceinline__ v16f mfma32(vec<T, 8> a, vec<T, 8> b, v16f c)
@@ -49,131 +52,191 @@ __device__ __forceinline__ uint32_t not_finite2(uint32_t x)
     return ((x & e) + one) & 0x80008000u;
 }
 
+// 16 bytes for each lane straight into LDS, from a wave-uniform base plus the lane's offset to a wave-uniform place plus 16 * lane.  Written in
+// assembly, so that the compiler does not wait for all of them before each LDS read; the kernel waits for them itself.
+__device__ __forceinline__ void load_to_lds(uint32_t lane_offset, const char *base, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_offset), "s"(base), "s"(lds) : "memory", "m0");
+}
+__device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 template <int D, class T>
 __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const PromptArgs a)
 {
-    constexpr int CHUNKS = D / 8;  // 16-byte pieces of a row
-    __shared__ __attribute__((aligned(16))) u32x4 s_k[kKeys][CHUNKS], s_v[kKeys][CHUNKS];
-    __shared__ int s_odd;  // a value of the tile is not finite
+    constexpr int CHUNKS = D / 8;                          // 16-byte pieces of a row
+    constexpr int ROWS = 64 / CHUNKS, LOADS = kKeys / kPromptWaves / ROWS;  // rows that a load of a wave brings; loads of a wave's share of a tile
+    __shared__ __attribute__((aligned(16))) u32x4 s_k[2][kKeys][CHUNKS], s_v[2][kKeys][CHUNKS];
+    __shared__ int s_odd;  // the tile (plus 1) in which a value is not finite
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int head = (int)blockIdx.y, hk = head / a.group;
 
-    // the tile's sequence
-    int tile = (int)blockIdx.x, seq = 0, q0 = 0, len_q = 0;
-    for (; seq < a.n_seqs; ++seq) {
-        q0 = min(max(a.starts_q[seq], 0), a.total_q);
-        len_q = max(min(a.starts_q[seq + 1], a.total_q) - q0, 0);
-        const int tiles = (len_q + kQueries - 1) / kQueries;
-        if (tile < tiles) break;
-        tile -= tiles;
+    // Blocks with ids 8 apart run on one XCD: each XCD gets consecutive heads, and goes through a head's tiles from the last
+    // (the longest rows of keys) to the first, so that what runs at a time shares keys and values in the XCD's L2.
+    const int per = (a.tiles * a.Hq + 7) >> 3, id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+    if ((int)blockIdx.x >> 3 >= per || id >= a.tiles * a.Hq) return;
+    const int head = id / a.tiles, hk = head / a.group;
+    int tile = a.tiles - 1 - id % a.tiles;
+
+    // the tile's sequence (tiles past the last: none)
+    int seq = -1, q0 = 0, len_q = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+        const int s = s0 + lane;
+        int from = 0, len = 0;
+        if (s < a.n_seqs) {
+            from = min(max(a.starts_q[s], 0), a.total_q);
+            len = max(min(a.starts_q[s + 1], a.total_q) - from, 0);
+        }
+        const int tiles = (len + kQueries - 1) / kQueries, upto = sums_up_to(tiles);
+        const uint64_t past = __ballot(upto > tile);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            seq = s0 + at;
+            q0 = __builtin_amdgcn_readlane(from, at);
+            len_q = __builtin_amdgcn_readlane(len, at);
+            tile -= __builtin_amdgcn_readlane(upto - tiles, at);
+            break;
+        }
+        tile -= __builtin_amdgcn_readlane(upto, 63);
     }
-    if (seq == a.n_seqs) return;
+    if (seq < 0) return;
     const int k0 = min(max(a.starts_k[seq], 0), a.total_k), len_k = max(min(a.starts_k[seq + 1], a.total_k) - k0, 0);
     const int first = tile * kQueries, before = len_k - len_q;  // of the block's rows; keys that every row sees, and one more each
     const int row = first + 32 * wave + n;
     const int limit = a.causal ? min(len_k, row + before + 1) : len_k;  // keys that this lane's row sees
     const int until = a.causal ? min(len_k, min(first + kQueries, len_q) + before) : len_k;  // that some row of the block sees
-    // keys that all rows of the wave (of the block) see
+    // keys that all rows of the wave (some row of it, all rows of the block) see
     const int wave_all = a.causal ? min(len_k, first + 32 * wave + before + 1) : len_k;
     const int wave_any = a.causal ? min(len_k, first + 32 * wave + 32 + before) : len_k;
     const int block_all = a.causal ? min(len_k, first + before + 1) : len_k;
 
+    // A wave loads 16 rows of a tile of keys and of values.  A row's pieces lie at their number XOR the row (keys; the lanes that read together
+    // have 16 rows) or XOR twice the row (values: 4 rows, two pieces), so that none of them meet in a bank.
+    const char *const k_head = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + k0 * a.k_token + hk * a.k_head);
+    const char *const v_head = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + k0 * a.v_token + hk * a.v_head);
+    const uint32_t lds_k = (uint32_t)(size_t)(__attribute__((address_space(3))) void *)s_k, lds_v = (uint32_t)(size_t)(__attribute__((address_space(3))) void *)s_v;
+    constexpr uint32_t TILE = kKeys * D * 2;  // bytes
+    const uint32_t k_row = (uint32_t)a.k_token * 2, v_row = (uint32_t)a.v_token * 2;
+    uint32_t k_at[LOADS], v_at[LOADS];
+    const auto lane_offsets = [&](int last) {  // (rows behind `last`: that one once more; they are masked)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = 16 * wave + ROWS * i + lane / CHUNKS, p = lane % CHUNKS, from = min(r, last);
+            k_at[i] = (uint32_t)from * k_row + 16 * (p ^ (r & (CHUNKS - 1)));
+            v_at[i] = (uint32_t)from * v_row + 16 * (p ^ ((r & (CHUNKS / 2 - 1)) << 1));
+        }
+    };
+    const auto issue = [&](int t, int buf) {
+        const char *const k = k_head + (long long)t * kKeys * a.k_token * 2, *const v = v_head + (long long)t * kKeys * a.v_token * 2;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load_to_lds(k_at[i], k, lds_k + buf * TILE + (16 * wave + ROWS * i) * (D * 2));
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load_to_lds(v_at[i], v, lds_v + buf * TILE + (16 * wave + ROWS * i) * (D * 2));
+    };
+
+    int t = (until + kKeys - 1) / kKeys - 1, buf = 0;
+    if (t >= 0) {
+        lane_offsets(len_k - 1 - t * kKeys);
+        issue(t, 0);
+        lane_offsets(kKeys);
+    }
+    if (threadIdx.x == 0) s_odd = 0;
+
     vec<T, 8> q[D / 16];
     {
         const T *src = static_cast<const T *>(a.q) + (long long)(q0 + min(row, len_q - 1)) * a.q_token + head * a.q_head + 8 * h;
+        const uint32_t sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u;  // (the scale's)
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const vec<T, 8> *>(src + 16 * i);
-    }
-    v16f o[D / 32] = {};
-    float m = -__builtin_inff(), l = 0.0f;
-
-    for (int tile_k = (until + kKeys - 1) / kKeys - 1; tile_k >= 0; --tile_k) {
-        const int key = tile_k * kKeys;
-        const bool masked = key + kKeys > block_all;
-        __syncthreads();
-        if (threadIdx.x == 0) s_odd = 0;
-        __syncthreads();
-        uint32_t odd = 0;
-        for (int i = threadIdx.x; i < kKeys * CHUNKS; i += 64 * kPromptWaves) {
-            const int j = i / CHUNKS, c = i % CHUNKS;
-            u32x4 kk = {}, vv = {};
-            if (key + j < len_k) {
-                const long long at = k0 + key + j;
-                kk = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.k) + at * a.k_token + hk * a.k_head + 8 * c);
-                vv = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.v) + at * a.v_token + hk * a.v_head + 8 * c);
-            }
-            s_k[j][c ^ (j & (CHUNKS - 1))] = kk;
-            s_v[j][c ^ ((j & (CHUNKS / 2 - 1)) << 1)] = vv;
-            if (masked)
+        for (int i = 0; i < D / 16; ++i) {
+            u32x4 x = *reinterpret_cast<const u32x4 *>(src + 16 * i);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) odd |= not_finite2<T>(vv[e]);
+            for (int e = 0; e < 4; ++e) x[e] ^= sign;
+            q[i] = __builtin_bit_cast(vec<T, 8>, x);
         }
-        if (odd) s_odd = 1;
-        __syncthreads();
+    }
+    const float scale = fmaxf(fabsf(a.scale_log2), 0x1p-126f);
+    v16f o[D / 32] = {};
+    float m = -__builtin_inff(), m_up = m, base = 0.0f, l = 0.0f;  // maximum (over scale), from where it moves, kWeightBits - m * scale; this lane's part of the sum
+
+    for (; t >= 0; --t, buf ^= 1) {
+        const int key = t * kKeys;
+        const bool masked = key + kKeys > block_all;
+        wait_and_meet();  // (the tile is there, and all waves have read the one before it)
+        if (masked) {
+            uint32_t odd = 0;
+#pragma unroll
+            for (int i = 0; i < kKeys * CHUNKS / (64 * kPromptWaves); ++i) {
+                const u32x4 x = (&s_v[buf][0][0])[i * 64 * kPromptWaves + (int)threadIdx.x];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) odd |= not_finite2<T>(x[e]);
+            }
+            if (odd) s_odd = t + 1;
+            wait_and_meet();
+        }
+        if (t > 0) issue(t - 1, buf ^ 1);
         if (key >= wave_any) continue;  // (no row of the wave sees any of them)
 
-        float sc[2][16];
+        v16f s[2] = {};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            v16f acc = {};
+        for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-                const int j = 32 * t + n, c = 2 * i + h;
-                acc = mfma32<T>(__builtin_bit_cast(vec<T, 8>, s_k[j][c ^ (j & (CHUNKS - 1))]), q[i], acc);
+            for (int u = 0; u < 2; ++u) {
+                const int j = 32 * u + n, c = 2 * i + h;
+                s[u] = mfma32<T>(__builtin_bit_cast(vec<T, 8>, s_k[buf][j][c ^ (j & (CHUNKS - 1))]), q[i], s[u]);
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[t][i] = acc[i] * a.scale_log2;
-        }
         if (key + kKeys > wave_all) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int j = key + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3);
-                    sc[t][i] = j < limit ? sc[t][i] : -__builtin_inff();
+                    const int j = key + 32 * u + 8 * (i >> 2) + 4 * h + (i & 3);
+                    s[u][i] = j < limit ? s[u][i] : -__builtin_inff();
                 }
         }
-        float top = sc[0][0];
+        float top = m;
 #pragma unroll
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i >> 4][i & 15]);
-        const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, top), __builtin_bit_cast(unsigned, top), false, false);
-        top = fmaxf(__builtin_bit_cast(float, (unsigned)both[0]), __builtin_bit_cast(float, (unsigned)both[1]));
-        if (__any(top > m)) {
-            const float now = fmaxf(m, top), by = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - now);
-            m = now;
+        for (int i = 0; i < 32; i += 2) top = max3(top, s[i >> 4][i & 15], s[i >> 4][(i & 15) + 1]);
+        if (__any(top > m_up)) {  // (first of all: m is minus infinity)
+            const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, top), __builtin_bit_cast(unsigned, top), false, false);
+            top = fmaxf(__builtin_bit_cast(float, (unsigned)both[0]), __builtin_bit_cast(float, (unsigned)both[1]));
+            const float by = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m - top) * scale);
+            m = top;
+            m_up = top + (14.0f - kWeightBits) / scale;
+            base = top == -__builtin_inff() ? 0.0f : kWeightBits - top * scale;
             l *= by;
 #pragma unroll
             for (int e = 0; e < D / 32; ++e) o[e] *= by;
         }
-        const float base = m == -__builtin_inff() ? 0.0f : m;
         vec<T, 8> p[4];
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            const float x = __builtin_amdgcn_exp2f(sc[i >> 4][i & 15] - base);
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][i & 15], scale, base));
             l += x;
             p[i >> 3][i & 7] = (T)x;
         }
-        const bool careful = masked && s_odd;
+        const bool careful = masked && s_odd == t + 1;
+        const auto values = [&](int e, int u, auto clean) {  // 32 elements (from 32 e) of 16 keys (from 16 u)
+            uint2 half[2];
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                uint2 half[2];
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    const int i = lane & 15, j = 16 * u + 8 * w + 4 * h + (i >> 2);
-                    const int c = 4 * e + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-                    half[w] = read_transposed(reinterpret_cast<const char *>(&s_v[j][c ^ ((j & (CHUNKS / 2 - 1)) << 1)]) + 8 * (i & 1));
-                    if (careful) {
-                        const uint32_t bx = not_finite2<T>(half[w].x), by = not_finite2<T>(half[w].y);
-                        half[w].x &= ~((bx >> 15) * 0xffffu);
-                        half[w].y &= ~((by >> 15) * 0xffffu);
-                    }
+            for (int w = 0; w < 2; ++w) {
+                const int i = lane & 15, j = 16 * u + 8 * w + 4 * h + (i >> 2), c = 4 * e + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+                half[w] = read_transposed(reinterpret_cast<const char *>(&s_v[buf][j][c ^ ((j & (CHUNKS / 2 - 1)) << 1)]) + 8 * (i & 1));
+                if constexpr (clean) {
+                    half[w].x &= ~((not_finite2<T>(half[w].x) >> 15) * 0xffffu);
+                    half[w].y &= ~((not_finite2<T>(half[w].y) >> 15) * 0xffffu);
                 }
-                o[e] = mfma32<T>(__builtin_bit_cast(vec<T, 8>, u32x4{half[0].x, half[0].y, half[1].x, half[1].y}), p[u], o[e]);
             }
-        if (careful) {
+            return __builtin_bit_cast(vec<T, 8>, u32x4{half[0].x, half[0].y, half[1].x, half[1].y});
+        };
+        if (!careful) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) o[e] = mfma32<T>(values(e, u, std::false_type{}), p[u], o[e]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) o[e] = mfma32<T>(values(e, u, std::true_type{}), p[u], o[e]);
             for (int j = 0; j < kKeys; ++j) {
                 const bool sees = key + j < limit;
 #pragma unroll
@@ -181,7 +244,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int d = 32 * e + 8 * (i >> 2) + 4 * h + (i & 3);
-                        const T x = reinterpret_cast<const T *>(&s_v[j][(d >> 3) ^ ((j & (CHUNKS / 2 - 1)) << 1)])[d & 7];
+                        const T x = reinterpret_cast<const T *>(&s_v[buf][j][(d >> 3) ^ ((j & (CHUNKS / 2 - 1)) << 1)])[d & 7];
                         const float f = (float)x;
                         if (sees && !(fabsf(f) < __builtin_inff())) o[e][i] += f;
                     }
@@ -224,9 +287,14 @@ extern "C" int attn_prompt(int dtype, int n_seqs, int total_q, int total_k, int 
     if (((uintptr_t)starts_q | (uintptr_t)starts_k) & 3) return fail(LQ_ERR_ALIGN, "starts_q and starts_k must be 4-byte aligned");
     if ((total_q > 1 && q_token % 8) || (Hq > 1 && q_head % 8) || (total_k > 1 && (k_token % 8 || v_token % 8)) || (Hkv > 1 && (k_head % 8 || v_head % 8)))
         return fail(LQ_ERR_ALIGN, "strides must be multiples of 8 elements");
+    if (total_k > 1 && (k_token < 0 || v_token < 0 || k_token > (1 << 24) || v_token > (1 << 24)))
+        return fail(LQ_ERR_INVALID, "k and v: strides from token to token must be from 0 to 2^24 elements, got %lld and %lld", k_token, v_token);
+    if (total_k <= 1) k_token = v_token = 0;
+    const long long tiles = total_q / kQueries + n_seqs;  // at most
+    if (tiles * Hq > (1 << 24)) return fail(LQ_ERR_INVALID, "too many rows: %d queries of %d sequences, %d heads", total_q, n_seqs, Hq);
     const PromptArgs a{q, k, v, q_token, q_head, k_token, k_head, v_token, v_head, starts_q, starts_k, out, n_seqs, total_q, total_k, Hq,
-                       Hq / Hkv, causal != 0, scale * 1.44269504f};
-    const dim3 grid((unsigned)(total_q / kQueries + n_seqs), (unsigned)Hq);
+                       Hq / Hkv, causal != 0, (int)tiles, scale * 1.44269504f};
+    const dim3 grid((unsigned)((tiles * Hq + 7) / 8 * 8));
     (void)hipGetLastError();
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kPromptWaves), 0, static_cast<hipStream_t>(hip_stream), a); };
     if (dtype == LQ_F16)
