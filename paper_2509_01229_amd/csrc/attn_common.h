@@ -72,10 +72,13 @@ __device__ __forceinline__ int lanes_up_to(int x, F f)
 }
 __device__ __forceinline__ int sums_up_to(int x) { return lanes_up_to(x, [](int a, int b) { return a + b; }); }
 
-__device__ __forceinline__ float max3(float a, float b, float c)
+// The largest of three in one instruction: a NaN stays one
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
+// or is left out.  (Not for results of a matrix product: the compiler does not count their wait states into assembly.)
+__device__ __forceinline__ float max3_numbers(float a, float b, float c)
 {
     float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));  // (a NaN is left out)
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
 __device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }  // -126 <= e <= 127

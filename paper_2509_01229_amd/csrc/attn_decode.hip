@@ -356,21 +356,22 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
                     }
             }
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) vt = max3(vt, sv[i >> 2][i & 3], sv[i >> 2][(i & 3) + 1]);
+            for (int i = 0; i < 8; i += 2) vt = max3_numbers(vt, sv[i >> 2][i & 3], sv[i >> 2][(i & 3) + 1]);
             float top[RT];
             bool up = false;
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 top[r] = m[r];
 #pragma unroll
-                for (int i = 0; i < 8; i += 2) top[r] = max3(top[r], sc[r][i >> 2][i & 3], sc[r][i >> 2][(i & 3) + 1]);
+                for (int i = 0; i < 8; i += 2) top[r] = max3_numbers(top[r], sc[r][i >> 2][i & 3], sc[r][i >> 2][(i & 3) + 1]);
                 up |= top[r] > m_up[r];
             }
             if (__any(up)) {  // (first of all: m is minus infinity)
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
                     top[r] = across_groups(top[r], [](float u, float w) { return fmaxf(u, w); });
-                    const float now = top[r], by = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m[r] - now) * q_scale[r]);
+                    const float now = top[r] > m_up[r] ? top[r] : m[r];  // (a row's results go by its own scores alone)
+                    const float by = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m[r] - now) * q_scale[r]);
                     m[r] = now;
                     m_up[r] = now + (14.0f - kWeightBits) / q_scale[r];
                     base[r] = base_of(r);

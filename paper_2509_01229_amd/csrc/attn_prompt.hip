@@ -157,33 +157,29 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
     v16f o[D / 32] = {};
     float m = -__builtin_inff(), m_up = m, base = 0.0f, l = 0.0f;  // maximum (over scale), from where it moves, kWeightBits - m * scale; this lane's part of the sum
 
-    for (; t >= 0; --t, buf ^= 1) {
-        const int key = t * kKeys;
-        const bool masked = key + kKeys > block_all;
-        wait_and_meet();  // (the tile is there, and all waves have read the one before it)
-        if (masked) {
-            uint32_t odd = 0;
+    // K fragment of 32 keys (u) for elements 16 i ..; V fragment of 16 keys (u) and elements 32 e ..
+    const auto keys = [&](int u, int i) {
+        const int j = 32 * u + n, c = 2 * i + h;
+        return __builtin_bit_cast(vec<T, 8>, s_k[buf][j][c ^ (j & (CHUNKS - 1))]);
+    };
+    const auto values = [&](int u, int e) {
+        uint2 half[2];
 #pragma unroll
-            for (int i = 0; i < kKeys * CHUNKS / (64 * kPromptWaves); ++i) {
-                const u32x4 x = (&s_v[buf][0][0])[i * 64 * kPromptWaves + (int)threadIdx.x];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) odd |= not_finite2<T>(x[e]);
-            }
-            if (odd) s_odd = t + 1;
-            wait_and_meet();
+        for (int w = 0; w < 2; ++w) {
+            const int i = lane & 15, j = 16 * u + 8 * w + 4 * h + (i >> 2), c = 4 * e + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+            half[w] = read_transposed(reinterpret_cast<const char *>(&s_v[buf][j][c ^ ((j & (CHUNKS / 2 - 1)) << 1)]) + 8 * (i & 1));
         }
-        if (t > 0) issue(t - 1, buf ^ 1);
-        if (key >= wave_any) continue;  // (no row of the wave sees any of them)
-
+        return __builtin_bit_cast(vec<T, 8>, u32x4{half[0].x, half[0].y, half[1].x, half[1].y});
+    };
+    // One tile.  CUT: some row of the block does not see all of its keys.
+    const auto step = [&](auto cut, int key, bool careful) {
+        constexpr bool CUT = decltype(cut)::value;
         v16f s[2] = {};
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int j = 32 * u + n, c = 2 * i + h;
-                s[u] = mfma32<T>(__builtin_bit_cast(vec<T, 8>, s_k[buf][j][c ^ (j & (CHUNKS - 1))]), q[i], s[u]);
-            }
-        if (key + kKeys > wave_all) {
+            for (int u = 0; u < 2; ++u) s[u] = mfma32<T>(keys(u, i), q[i], s[u]);
+        if (CUT && key + kKeys > wave_all) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -198,6 +194,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
         if (__any(top > m_up)) {  // (first of all: m is minus infinity)
             const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, top), __builtin_bit_cast(unsigned, top), false, false);
             top = fmaxf(__builtin_bit_cast(float, (unsigned)both[0]), __builtin_bit_cast(float, (unsigned)both[1]));
+            top = top > m_up ? top : m;  // (a row's results go by its own scores alone)
             const float by = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m - top) * scale);
             m = top;
             m_up = top + (14.0f - kWeightBits) / scale;
@@ -213,30 +210,21 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
             l += x;
             p[i >> 3][i & 7] = (T)x;
         }
-        const bool careful = masked && s_odd == t + 1;
-        const auto values = [&](int e, int u, auto clean) {  // 32 elements (from 32 e) of 16 keys (from 16 u)
-            uint2 half[2];
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                const int i = lane & 15, j = 16 * u + 8 * w + 4 * h + (i >> 2), c = 4 * e + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-                half[w] = read_transposed(reinterpret_cast<const char *>(&s_v[buf][j][c ^ ((j & (CHUNKS / 2 - 1)) << 1)]) + 8 * (i & 1));
-                if constexpr (clean) {
-                    half[w].x &= ~((not_finite2<T>(half[w].x) >> 15) * 0xffffu);
-                    half[w].y &= ~((not_finite2<T>(half[w].y) >> 15) * 0xffffu);
-                }
-            }
-            return __builtin_bit_cast(vec<T, 8>, u32x4{half[0].x, half[0].y, half[1].x, half[1].y});
-        };
-        if (!careful) {
+        if (!CUT || !careful) {
 #pragma unroll
             for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int e = 0; e < D / 32; ++e) o[e] = mfma32<T>(values(e, u, std::false_type{}), p[u], o[e]);
+                for (int e = 0; e < D / 32; ++e) o[e] = mfma32<T>(values(u, e), p[u], o[e]);
         } else {
 #pragma unroll
             for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int e = 0; e < D / 32; ++e) o[e] = mfma32<T>(values(e, u, std::true_type{}), p[u], o[e]);
+                for (int e = 0; e < D / 32; ++e) {
+                    u32x4 x = __builtin_bit_cast(u32x4, values(u, e));
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) x[w] &= ~((not_finite2<T>(x[w]) >> 15) * 0xffffu);
+                    o[e] = mfma32<T>(__builtin_bit_cast(vec<T, 8>, x), p[u], o[e]);
+                }
             for (int j = 0; j < kKeys; ++j) {
                 const bool sees = key + j < limit;
 #pragma unroll
@@ -250,6 +238,27 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
                     }
             }
         }
+    };
+
+    // the tiles that are cut, with a look at their values
+    for (; t >= 0 && (t + 1) * kKeys > block_all; --t, buf ^= 1) {
+        wait_and_meet();  // (the tile is there, and all waves have read the one before it)
+        uint32_t odd = 0;
+#pragma unroll
+        for (int i = 0; i < kKeys * CHUNKS / (64 * kPromptWaves); ++i) {
+            const u32x4 x = (&s_v[buf][0][0])[i * 64 * kPromptWaves + (int)threadIdx.x];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd |= not_finite2<T>(x[e]);
+        }
+        if (odd) s_odd = t + 1;
+        wait_and_meet();
+        if (t > 0) issue(t - 1, buf ^ 1);
+        if (t * kKeys < wave_any) step(std::true_type{}, t * kKeys, s_odd == t + 1);  // (else: no row of the wave sees any of them)
+    }
+    for (; t >= 0; --t, buf ^= 1) {
+        wait_and_meet();
+        if (t > 0) issue(t - 1, buf ^ 1);
+        step(std::false_type{}, t * kKeys, false);
     }
     const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, l), __builtin_bit_cast(unsigned, l), false, false);
     l = __builtin_bit_cast(float, (unsigned)both[0]) + __builtin_bit_cast(float, (unsigned)both[1]);
