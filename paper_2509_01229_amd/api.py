@@ -116,7 +116,9 @@ def lib() -> ctypes.CDLL:
     L.kv4_attention.restype = i
     L.kv4_attention.argtypes = [i] * 6 + [vp, ll, ll, ll, vp, i, i, vp, i, vp, f, vp, vp, sz, vp]
     L.attn_prompt.restype = i
-    L.attn_prompt.argtypes = [i] * 7 + [vp, ll, ll] * 3 + [vp, vp, f, i, vp, vp]
+    L.attn_prompt.argtypes = [i] * 7 + [vp, ll, ll] * 3 + [vp, vp, f, i, vp, vp, sz, vp]
+    L.attn_prompt_workspace_size.restype = sz
+    L.attn_prompt_workspace_size.argtypes = [i] * 5
     L.w4a8_calib_stream_read.restype = i
     L.w4a8_calib_stream_read.argtypes = [vp, sz, vp]
     L.w4a8_calib_mfma_i8.restype = i
@@ -164,7 +166,8 @@ def _bind(L) -> None:
     _binding.bind(address(L.w4a8_gemm), address(L.w4a8_gemm_workspace_size), address(L.w4a8_quantize_activations),
                   address(L.w4a8_grouped_gemm), address(L.liquidquant_packed_size))
     _binding.bind_attention(address(L.attn_qk_norm_rope), address(L.kv4_write), address(L.kv4_append), address(L.kv4_read),
-                            address(L.kv4_attention_workspace_size), address(L.kv4_attention), address(L.attn_prompt))
+                            address(L.kv4_attention_workspace_size), address(L.kv4_attention), address(L.attn_prompt_workspace_size),
+                            address(L.attn_prompt))
     _native = _binding
 
 
@@ -757,13 +760,13 @@ def kv4_attention(q, cache, block_table, context, scale=None, out=None, workspac
     return out
 
 
-def attn_prompt(q, k, v, starts_q, starts_k=None, scale=None, causal=True, out=None, stream=None):
+def attn_prompt(q, k, v, starts_q, starts_k=None, scale=None, causal=True, out=None, workspace=None, stream=None):
     """Attention over packed sequences: q [queries, heads, head_dim], k and v [keys, kv_heads, head_dim]; sequence s has the
     queries starts_q[s] .. starts_q[s + 1] - 1 and the keys starts_k[s] .. (int32 on the GPU; starts_k: starts_q unless given).  causal: query
     i sees the keys up to i + (keys - queries) of its sequence.  scale: 1 / sqrt(head_dim) unless given.  Returns out, shaped as q."""
     if _native is None:
         lib()
-    done = _native.prompt(q, k, v, starts_q, starts_q if starts_k is None else starts_k, scale, causal, out, stream)
+    done = _native.prompt(q, k, v, starts_q, starts_q if starts_k is None else starts_k, scale, causal, out, workspace, stream, _ws_cache)
     if done is not None:
         return _result(done)
     import torch
@@ -778,7 +781,9 @@ def attn_prompt(q, k, v, starts_q, starts_k=None, scale=None, causal=True, out=N
         raise ValueError(f"starts_q must be [sequences + 1], got {tuple(starts_q.shape)}")
     S = starts_q.shape[0] - 1
     out = torch.empty((Tq, Hq, D), dtype=q.dtype, device=q.device) if out is None else out
+    need = int(lib().attn_prompt_workspace_size(S, Tq, Tk, Hq, D))
+    wsp, wsb = _ws(workspace, device=q.device, stream=stream, need=need)
     _check(lib().attn_prompt(_dtype_code(q), S, Tq, Tk, Hq, Hkv, D, *dq, *dk, *dv, _dev(starts_q, torch.int32, (S + 1,), "starts_q"),
                              _dev(starts_k, torch.int32, (S + 1,), "starts_k"), D ** -0.5 if scale is None else scale, int(bool(causal)),
-                             _dev(out, q.dtype, (Tq, Hq, D), "out"), _stream(stream)))
+                             _dev(out, q.dtype, (Tq, Hq, D), "out"), wsp, wsb, _stream(stream)))
     return out

@@ -10,6 +10,7 @@
 // Keys are taken from the last to the first: the tiles that the causal mask cuts come first.  What is masked has no
 // part in the result, whatever it holds: scores by selection, and values, where a masked one is not finite, by taking
 // the tile's values that are not finite out of the product and adding them to the rows that see them.
+#include <algorithm>
 #include <type_traits>
 
 #include "attn_common.h"
@@ -21,7 +22,9 @@ struct PromptArgs {
     long long q_token, q_head, k_token, k_head, v_token, v_head;
     const int *starts_q, *starts_k;
     void *out;
-    int n_seqs, total_q, total_k, Hq, group, causal, tiles;
+    unsigned *tickets;
+    float *parts;
+    int n_seqs, total_q, total_k, Hq, group, causal, tiles, splits;
     float scale_log2;
 };
 
@@ -72,10 +75,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
 
     // Blocks with ids 8 apart run on one XCD: each XCD gets consecutive heads, and goes through a head's tiles from the last
     // (the longest rows of keys) to the first, so that what runs at a time shares keys and values in the XCD's L2.
-    const int per = (a.tiles * a.Hq + 7) >> 3, id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
-    if ((int)blockIdx.x >> 3 >= per || id >= a.tiles * a.Hq) return;
-    const int head = id / a.tiles, hk = head / a.group;
-    int tile = a.tiles - 1 - id % a.tiles;
+    const int blocks = a.tiles * a.Hq * a.splits, per = (blocks + 7) >> 3, id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+    if ((int)blockIdx.x >> 3 >= per || id >= blocks) return;
+    const int whole = id / a.splits, part = id % a.splits;  // a tile of a head, which part of its keys
+    const int head = whole / a.tiles, hk = head / a.group;
+    int tile = a.tiles - 1 - whole % a.tiles;
 
     // the tile's sequence (tiles past the last: none)
     int seq = -1, q0 = 0, len_q = 0;
@@ -133,8 +137,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
         for (int i = 0; i < LOADS; ++i) load_to_lds(v_at[i], v, lds_v + buf * TILE + (16 * wave + ROWS * i) * (D * 2));
     };
 
-    int t = (until + kKeys - 1) / kKeys - 1, buf = 0;
-    if (t >= 0) {
+    // this part's tiles of keys: from t down to t_last
+    const int tiles_k = max((until + kKeys - 1) / kKeys, 0);
+    const int t_last = (int)((unsigned)part * (unsigned)tiles_k / (unsigned)a.splits);
+    int t = (int)((unsigned)(part + 1) * (unsigned)tiles_k / (unsigned)a.splits) - 1, buf = 0;
+    if (t >= t_last) {
         lane_offsets(len_k - 1 - t * kKeys);
         issue(t, 0);
         lane_offsets(kKeys);
@@ -241,7 +248,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
     };
 
     // the tiles that are cut, with a look at their values
-    for (; t >= 0 && (t + 1) * kKeys > block_all; --t, buf ^= 1) {
+    for (; t >= t_last && (t + 1) * kKeys > block_all; --t, buf ^= 1) {
         wait_and_meet();  // (the tile is there, and all waves have read the one before it)
         uint32_t odd = 0;
 #pragma unroll
@@ -252,16 +259,59 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
         }
         if (odd) s_odd = t + 1;
         wait_and_meet();
-        if (t > 0) issue(t - 1, buf ^ 1);
+        if (t > t_last) issue(t - 1, buf ^ 1);
         if (t * kKeys < wave_any) step(std::true_type{}, t * kKeys, s_odd == t + 1);  // (else: no row of the wave sees any of them)
     }
-    for (; t >= 0; --t, buf ^= 1) {
+    for (; t >= t_last; --t, buf ^= 1) {
         wait_and_meet();
-        if (t > 0) issue(t - 1, buf ^ 1);
+        if (t > t_last) issue(t - 1, buf ^ 1);
         step(std::false_type{}, t * kKeys, false);
     }
     const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, l), __builtin_bit_cast(unsigned, l), false, false);
     l = __builtin_bit_cast(float, (unsigned)both[0]) + __builtin_bit_cast(float, (unsigned)both[1]);
+    if (a.splits > 1) {
+        // every part leaves its maxima, sums and unscaled results, past the L2s (the XCDs do not share them); the last to arrive at the
+        // tile's ticket joins them, in their order
+        constexpr int FLOATS = 64 * kPromptWaves * (D / 2 + 4);  // of a part
+        float *const parts = a.parts + (size_t)whole * a.splits * FLOATS;
+        const auto all = __builtin_amdgcn_make_buffer_rsrc(parts, 0, a.splits * FLOATS * 4, 0x00027000);
+        const auto at = [&](int p, int piece) { return (p * FLOATS + (piece * 64 * kPromptWaves + (int)threadIdx.x) * 4) * 4; };
+        constexpr int kShared = 16;  // sc1
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v4f{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]}), all,
+                                                       at(part, 4 * e + i), 0, kShared);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v4f{m, l, 0.0f, 0.0f}), all, at(part, D / 8), 0, kShared);
+        wait_and_meet();
+        if (threadIdx.x == 0) {
+            const unsigned arrived = __hip_atomic_fetch_add(a.tickets + whole, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_odd = arrived == (unsigned)a.splits - 1;
+            if (s_odd) __hip_atomic_store(a.tickets + whole, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        wait_and_meet();
+        if (!s_odd) return;
+        m = -__builtin_inff();
+        l = 0.0f;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) o[e] = v16f{};
+        for (int p = 0; p < a.splits; ++p) {
+            const v4f ml = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(all, at(p, D / 8), 0, kShared));
+            v4f x[D / 8];
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) x[i] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(all, at(p, i), 0, kShared));
+            const float now = fmaxf(m, ml[0]);
+            const float old = m == now ? 1.0f : __builtin_amdgcn_exp2f((m - now) * scale);
+            const float by = ml[0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((ml[0] - now) * scale);
+            m = now;
+            l = l * old + ml[1] * by;
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[e][i] = o[e][i] * old + x[4 * e + (i >> 2)][i & 3] * by;
+        }
+    }
     if (row >= len_q) return;
     const float by = l == 0.0f ? 0.0f : 1.0f / l;
     T *dst = static_cast<T *>(a.out) + ((size_t)(q0 + row) * a.Hq + head) * D;
@@ -280,9 +330,31 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
 
 using namespace lqq;
 
+namespace {
+constexpr size_t kTickets = 32768;  // bytes at the head of the workspace, those of the GEMM's
+// Parts of the keys: as many as fill two blocks a CU where the tiles of queries do not, each of 1024 keys or more on the average.
+// (512 queries of two sequences over 6000 keys, 32 heads: one part 122 us, three parts see the table of cases.)
+int splits_of(long long blocks, int total_k, int n_seqs)
+{
+    if (blocks < 1 || blocks > 256) return 1;
+    return (int)std::max<long long>(1, std::min<long long>({512 / blocks, total_k / std::max(n_seqs, 1) / 1024, 8}));
+}
+long long tiles_of(int total_q, int n_seqs) { return total_q / kQueries + n_seqs; }  // at most
+size_t part_bytes(int head_dim) { return sizeof(float) * 64 * kPromptWaves * (head_dim / 2 + 4); }
+}  // namespace
+
+extern "C" size_t attn_prompt_workspace_size(int n_seqs, int total_q, int total_k, int Hq, int head_dim)
+{
+    if (n_seqs < 1 || total_q < 1 || total_k < 1 || Hq < 1 || !head_dim_ok(head_dim)) return 0;
+    const long long blocks = tiles_of(total_q, n_seqs) * Hq;
+    const int splits = splits_of(blocks, total_k, n_seqs);
+    return splits == 1 ? 0 : kTickets + (size_t)blocks * splits * part_bytes(head_dim);
+}
+
 extern "C" int attn_prompt(int dtype, int n_seqs, int total_q, int total_k, int Hq, int Hkv, int head_dim, const void *q, long long q_token,
                            long long q_head, const void *k, long long k_token, long long k_head, const void *v, long long v_token,
-                           long long v_head, const int *starts_q, const int *starts_k, float scale, int causal, void *out, void *hip_stream)
+                           long long v_head, const int *starts_q, const int *starts_k, float scale, int causal, void *out, void *workspace,
+                           size_t workspace_bytes, void *hip_stream)
 {
     if (dtype != LQ_F16 && dtype != LQ_BF16) return fail(LQ_ERR_INVALID, "dtype must be LQ_F16 or LQ_BF16, got %d", dtype);
     if (!head_dim_ok(head_dim)) return fail(LQ_ERR_INVALID, "head_dim must be 64 or 128, got %d", head_dim);
@@ -292,18 +364,22 @@ extern "C" int attn_prompt(int dtype, int n_seqs, int total_q, int total_k, int 
     if (!(scale > -1e30f && scale < 1e30f)) return fail(LQ_ERR_INVALID, "scale must be finite");
     if (n_seqs == 0 || total_q == 0) return LQ_OK;
     if (!q || !out || !starts_q || !starts_k || (total_k && (!k || !v))) return fail(LQ_ERR_INVALID, "null pointer");
-    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15) return fail(LQ_ERR_ALIGN, "q, k, v and out must be 16-byte aligned");
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out | (uintptr_t)workspace) & 15)
+        return fail(LQ_ERR_ALIGN, "q, k, v, out and workspace must be 16-byte aligned");
     if (((uintptr_t)starts_q | (uintptr_t)starts_k) & 3) return fail(LQ_ERR_ALIGN, "starts_q and starts_k must be 4-byte aligned");
     if ((total_q > 1 && q_token % 8) || (Hq > 1 && q_head % 8) || (total_k > 1 && (k_token % 8 || v_token % 8)) || (Hkv > 1 && (k_head % 8 || v_head % 8)))
         return fail(LQ_ERR_ALIGN, "strides must be multiples of 8 elements");
     if (total_k > 1 && (k_token < 0 || v_token < 0 || k_token > (1 << 24) || v_token > (1 << 24)))
         return fail(LQ_ERR_INVALID, "k and v: strides from token to token must be from 0 to 2^24 elements, got %lld and %lld", k_token, v_token);
     if (total_k <= 1) k_token = v_token = 0;
-    const long long tiles = total_q / kQueries + n_seqs;  // at most
+    const long long tiles = tiles_of(total_q, n_seqs);
     if (tiles * Hq > (1 << 24)) return fail(LQ_ERR_INVALID, "too many rows: %d queries of %d sequences, %d heads", total_q, n_seqs, Hq);
-    const PromptArgs a{q, k, v, q_token, q_head, k_token, k_head, v_token, v_head, starts_q, starts_k, out, n_seqs, total_q, total_k, Hq,
-                       Hq / Hkv, causal != 0, (int)tiles, scale * 1.44269504f};
-    const dim3 grid((unsigned)((tiles * Hq + 7) / 8 * 8));
+    const size_t need = attn_prompt_workspace_size(n_seqs, total_q, total_k, Hq, head_dim);
+    const int splits = need && workspace && workspace_bytes >= need ? splits_of(tiles * Hq, total_k, n_seqs) : 1;
+    const PromptArgs a{q, k, v, q_token, q_head, k_token, k_head, v_token, v_head, starts_q, starts_k, out,
+                       static_cast<unsigned *>(workspace), splits > 1 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + kTickets) : nullptr,
+                       n_seqs, total_q, total_k, Hq, Hq / Hkv, causal != 0, (int)tiles, splits, scale * 1.44269504f};
+    const dim3 grid((unsigned)((tiles * Hq * splits + 7) / 8 * 8));
     (void)hipGetLastError();
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kPromptWaves), 0, static_cast<hipStream_t>(hip_stream), a); };
     if (dtype == LQ_F16)

@@ -34,6 +34,7 @@ struct Attention {
     decltype(&kv4_read) read;
     decltype(&kv4_attention_workspace_size) workspace_size;
     decltype(&kv4_attention) decode;
+    decltype(&attn_prompt_workspace_size) prompt_workspace_size;
     decltype(&attn_prompt) prompt;
 } attn{};
 
@@ -427,44 +428,53 @@ PyObject *decode(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// prompt(q, k, v, starts_q, starts_k, scale, causal, out, stream) -> out
+// prompt(q, k, v, starts_q, starts_k, scale, causal, out, workspace, stream, workspaces) -> out
 PyObject *prompt(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     void *stream;
     double scale;
-    if (n != 9 || !heads(a[0], 3)) Py_RETURN_NONE;
+    if (n != 11 || !heads(a[0], 3)) Py_RETURN_NONE;
     const at::Tensor &q = tensor(a[0]);
     if (!heads(a[1], 3, &q)) Py_RETURN_NONE;
     const at::Tensor &k = tensor(a[1]);
     const int64_t T = q.size(0), Hq = q.size(1), D = q.size(2), Tk = k.size(0), Hkv = k.size(1);
     if (k.size(2) != D || !heads_of(a[2], q, {Tk, Hkv, D}) || !plain_dims(a[3], at::kInt, 1) || tensor(a[3]).size(0) < 1 ||
         !plain(a[4], at::kInt, {tensor(a[3]).size(0)}) || !scale_of(a[5], D, scale) || !PyBool_Check(a[6]) ||
-        (a[7] != Py_None && !plain(a[7], q.scalar_type(), {T, Hq, D})) || !stream_of(a[8], stream))
+        (a[7] != Py_None && !plain(a[7], q.scalar_type(), {T, Hq, D})) || !stream_of(a[9], stream))
         Py_RETURN_NONE;
+    const int S = (int)tensor(a[3]).size(0) - 1;
+    at::Tensor workspace;
+    if (!workspace_of(a[8], a[10], q, stream, attn.prompt_workspace_size(S, (int)T, (int)Tk, (int)Hq, (int)D), workspace)) {
+        if (PyErr_Occurred()) return nullptr;
+        Py_RETURN_NONE;
+    }
     const at::Tensor &v = tensor(a[2]);
     at::Tensor out = a[7] != Py_None ? tensor(a[7]) : at::Tensor();
     int rc;
     {
         const WithoutGil released;
         if (!out.defined()) out = at::empty({T, Hq, D}, q.options());
-        rc = attn.prompt(dtype_of(q), (int)tensor(a[3]).size(0) - 1, (int)T, (int)Tk, (int)Hq, (int)Hkv, (int)D, q.data_ptr(), q.stride(0), q.stride(1),
+        rc = attn.prompt(dtype_of(q), S, (int)T, (int)Tk, (int)Hq, (int)Hkv, (int)D, q.data_ptr(), q.stride(0), q.stride(1),
                          k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), ints(a[3]), ints(a[4]), (float)scale,
-                         a[6] == Py_True, out.data_ptr(), stream);
+                         a[6] == Py_True, out.data_ptr(), workspace.defined() ? workspace.data_ptr() : nullptr,
+                         workspace.defined() ? (size_t)workspace.numel() : 0, stream);
     }
     if (rc != LQ_OK) return PyLong_FromLong(rc);
     return wrapped(a[7], std::move(out));
     END_HANDLE_TH_ERRORS
 }
 
-// bind_attention(attn_qk_norm_rope, kv4_write, kv4_append, kv4_read, kv4_attention_workspace_size, kv4_attention, attn_prompt): their addresses
+// bind_attention(attn_qk_norm_rope, kv4_write, kv4_append, kv4_read, kv4_attention_workspace_size, kv4_attention,
+// attn_prompt_workspace_size, attn_prompt): their addresses
 PyObject *bind_attention(PyObject *, PyObject *args)
 {
-    unsigned long long r, w, a, d, s, t, p;
-    if (!PyArg_ParseTuple(args, "KKKKKKK", &r, &w, &a, &d, &s, &t, &p)) return nullptr;
+    unsigned long long r, w, a, d, s, t, z, p;
+    if (!PyArg_ParseTuple(args, "KKKKKKKK", &r, &w, &a, &d, &s, &t, &z, &p)) return nullptr;
     attn = Attention{reinterpret_cast<decltype(attn.rope)>(r), reinterpret_cast<decltype(attn.write)>(w), reinterpret_cast<decltype(attn.append)>(a),
                      reinterpret_cast<decltype(attn.read)>(d), reinterpret_cast<decltype(attn.workspace_size)>(s),
-                     reinterpret_cast<decltype(attn.decode)>(t), reinterpret_cast<decltype(attn.prompt)>(p)};
+                     reinterpret_cast<decltype(attn.decode)>(t),
+                     reinterpret_cast<decltype(attn.prompt_workspace_size)>(z), reinterpret_cast<decltype(attn.prompt)>(p)};
     Py_RETURN_NONE;
 }
 

@@ -109,4 +109,4 @@ def test_what_is_not_plain_is_left_to_the_general_path():
     pages = torch.zeros((5, 4), dtype=torch.int32, device="cuda")
     assert native.decode(q, cache, pages, pos, 1, None, None, None, {}) is None
     assert native.decode(q, cache, pages[:4], pos, None, None, None, None, {}) is None
-    assert native.prompt(q, k, v, pos, pos, None, 1, None, None) is None
+    assert native.prompt(q, k, v, pos, pos, None, 1, None, None, None, {}) is None

@@ -68,11 +68,11 @@ def test_c_entries_refuse_what_they_cannot_run():
     decode = [0, 4, 1, 8, 2, 128, P, 1024, 1024, 128, P, 10, 16, P, 5, P, 0.1, P, None, 0, None]
     _refused(L.kv4_attention, decode, {0: 9, 1: -1, 2: (0, 2 ** 30), 3: (7, 0), 4: (0, 3), 5: 32, 6: None, 10: None, 11: (0, 2 ** 28), 12: 15, 13: None,
                                        14: (0, 2 ** 28), 15: None, 16: (float("nan"), float("inf")), 17: None}, bad)
-    _refused(L.kv4_attention, decode, {6: ODD, 7: 1020, 9: 100, 10: ODD, 17: ODD}, align)
-    prompt = [0, 2, 40, 60, 8, 2, 128, P, 1024, 128, P, 256, 128, P, 256, 128, P, P, 0.1, 1, P, None]
+    _refused(L.kv4_attention, decode, {6: ODD, 7: 1020, 9: 100, 10: ODD, 17: ODD, 18: ODD}, align)
+    prompt = [0, 2, 40, 60, 8, 2, 128, P, 1024, 128, P, 256, 128, P, 256, 128, P, P, 0.1, 1, P, None, 0, None]
     _refused(L.attn_prompt, prompt, {0: 2, 1: (-1, 2 ** 21), 2: (-1, 2 ** 29), 3: -1, 4: (0, 9), 5: 0, 6: 192, 7: None, 10: None, 13: None, 16: None,
-                                     17: None, 18: float("nan"), 20: None}, bad)
-    _refused(L.attn_prompt, prompt, {7: ODD, 8: 1028, 9: 4, 10: ODD, 11: 4, 12: 4, 13: ODD, 14: 4, 15: 4, 20: ODD}, align)
+                                     17: None, 18: float("nan"), 20: None, 11: (-8, 2 ** 25)}, bad)
+    _refused(L.attn_prompt, prompt, {7: ODD, 8: 1028, 9: 4, 10: ODD, 11: 4, 12: 4, 13: ODD, 14: 4, 15: 4, 20: ODD, 21: ODD}, align)
     # nothing to do: nothing is looked at
     assert L.kv4_write(0, 0, 2, 128, *[None if x is P else x for x in write[4:]]) == 0
     assert L.kv4_attention(*[0 if i == 1 else None if x is P else x for i, x in enumerate(decode)]) == 0

@@ -354,6 +354,39 @@ def test_prompts_masked_keys_and_values_do_not_matter(dtype, D, bad):
                 assert np.isnan(got[sees]).all(), j
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompts_few_queries_over_many_keys(dtype, D):
+    """Keys split over blocks and joined: with a workspace, without one (one block a tile), twice on the same tickets; a value
+    that is not finite in a part that some rows do not see."""
+    import torch
+
+    rng = np.random.default_rng(17)
+    lens, Hq, Hkv = [(70, 4000), (130, 2500), (1, 3000), (5, 3)], 3, 1
+    sq, sk = (np.concatenate(([0], np.cumsum([x[i] for x in lens]))).astype(np.int32) for i in (0, 1))
+    q, k, v = _draw(rng, (sq[-1], Hq, D), dtype) * np.float32(2.0), _draw(rng, (sk[-1], Hkv, D), dtype, True), _draw(rng, (sk[-1], Hkv, D), dtype)
+    args = [_gpu(x, dtype) for x in (q, k, v)] + [_gpu(sq), _gpu(sk)]
+    need = int(api.lib().attn_prompt_workspace_size(len(lens), int(sq[-1]), int(sk[-1]), Hq, D))
+    assert need > 32768
+    for causal in (True, False):
+        ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+        ws[32768:] = 255  # (what it holds does not matter)
+        got = api.attn_prompt(*args, causal=causal, workspace=ws)
+        assert torch.equal(got, api.attn_prompt(*args, causal=causal, workspace=ws)) and torch.equal(got, api.attn_prompt(*args, causal=causal))
+        assert not ws[:32768].any()
+        for g in (got, api.attn_prompt(*args, causal=causal, workspace=ws[:16])):
+            for s, (a, b) in enumerate(lens):
+                limits = np.arange(a) + b - a + 1 if causal else np.full(a, b)
+                want, spread = A.attention(q[sq[s]:sq[s + 1]], k[sk[s]:sk[s + 1]], v[sk[s]:sk[s + 1]], D ** -0.5, limits)
+                _close(_np(g)[sq[s]:sq[s + 1]], want, spread, dtype, A.UNIT[dtype], f"sequence {s}")
+    clean = _np(api.attn_prompt(*args))
+    args[2][3980, 0, 5] = float("nan")  # (queries 50 .. of the first sequence see it)
+    got = _np(api.attn_prompt(*args))
+    assert np.isnan(got[50:70, :, 5]).all()
+    got[50:70, :, 5] = clean[50:70, :, 5]
+    assert np.array_equal(got, clean)
+
+
 def test_prompts_scores_far_apart():
     rng = np.random.default_rng(12)
     n, D = 400, 128
