@@ -417,6 +417,96 @@ def test_prompt_starts_outside_the_tensors_are_cut_off():
     assert (out[:40] == 7).all() and (out[60:] == 7).all() and not (out[40:60] == 7).all()
 
 
+def test_a_cache_of_more_than_4_gib():
+    """Pages whose places pass 32 bits: written, read back and attended to."""
+    import torch
+
+    rng = np.random.default_rng(20)
+    D, page, Hkv, Hq, pages, c = 128, 256, 8, 16, 16000, 900
+    cache = torch.empty((pages, Hkv, page * (D + 8)), dtype=torch.uint8, device="cuda")
+    assert cache.numel() > 1 << 32
+    table = np.array([[15999, 3, 15500, 15421]], dtype=np.int32)  # (15421 * 278528 just above 2^32)
+    j = np.arange(c)
+    slots = (table[0, j // page] * page + j % page).astype(np.int32)
+    k, v, q = _draw(rng, (c, Hkv, D), A.F16, True), _draw(rng, (c, Hkv, D), A.F16), _draw(rng, (1, Hq, D), A.F16)
+    api.kv4_write(_gpu(k, A.F16), _gpu(v, A.F16), _gpu(slots), cache)
+    k, v = (A.dequantise(*A.quantise(x)) for x in (k, v))
+    for got, x in zip(api.kv4_read(cache, _gpu(slots)), (k, v)):
+        assert np.array_equal(_np(got), A.round_to(x, A.F16))
+    got = api.kv4_attention(_gpu(q, A.F16), cache, _gpu(table), _gpu(np.array([c], dtype=np.int32)))
+    want, spread = A.attention(q, k, v, D ** -0.5, [c])
+    _close(_np(got), want, spread, A.F16, 2.0 ** -11)
+
+
+def test_keys_and_values_that_heads_or_tokens_share():
+    """Strides of zero: heads that are one head expanded, tokens that are one token."""
+    rng = np.random.default_rng(21)
+    n, Hq, Hkv, D = 150, 4, 2, 64
+    q, k, v = _draw(rng, (n, Hq, D), A.BF16), _draw(rng, (n, 1, D), A.BF16), _draw(rng, (1, Hkv, D), A.BF16)
+    starts = _gpu(np.array([0, n], dtype=np.int32))
+    dk, dv = _gpu(k, A.BF16).expand(n, Hkv, D), _gpu(v, A.BF16).expand(n, Hkv, D)
+    got = _np(api.attn_prompt(_gpu(q, A.BF16), dk, dv, starts))
+    assert np.array_equal(got, _np(api.attn_prompt(_gpu(q, A.BF16), dk.contiguous(), dv.contiguous(), starts)))
+    want, spread = A.attention(q, np.repeat(k, Hkv, 1), np.repeat(v, n, 0), D ** -0.5, np.arange(n) + 1)
+    _close(got, want, spread, A.BF16, A.UNIT[A.BF16])
+    one, two = api.kv4_cache(10, 16, Hkv, D), api.kv4_cache(10, 16, Hkv, D)
+    slots = _gpu(np.arange(n, dtype=np.int32))
+    assert np.array_equal(api.kv4_write(dk, dv, slots, one).cpu().numpy(), api.kv4_write(dk.contiguous(), dv.contiguous(), slots, two).cpu().numpy())
+
+
+def test_attention_of_many_sequences():
+    """More sequences than a wave has lanes, of all lengths, empty ones among them; the same without a workspace, bit for bit where
+    an item is not split."""
+    import torch
+
+    rng = np.random.default_rng(22)
+    contexts = [int(x) for x in rng.integers(0, 300, 150)]
+    contexts[70], contexts[149] = 5000, 2500
+    D, page, Hq, Hkv = 64, 16, 4, 2
+    cache, table, keys, values = _filled(rng, contexts, page, Hkv, D, A.F16)
+    q = _draw(rng, (len(contexts), Hq, D), A.F16)
+    args = (_gpu(q, A.F16), cache, _gpu(table), _gpu(np.array(contexts, dtype=np.int32)))
+    ws = torch.zeros(int(api.lib().kv4_attention_workspace_size(len(contexts), 1, Hq, Hkv, D)), dtype=torch.uint8, device="cuda")
+    ws[32768:] = 255
+    got = [_np(api.kv4_attention(*args, workspace=w)) for w in (ws, ws, ws[:16])]
+    assert np.array_equal(got[0], got[1]) and not ws[:32768].any()
+    for g in got[1:]:
+        for b, c in enumerate(contexts):
+            want, spread = A.attention(q[b:b + 1], keys[b], values[b], D ** -0.5, [c])
+            _close(g[b:b + 1], want, spread, A.F16, 2.0 ** -11, f"sequence {b} of {c}")
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.11, 1e-30])
+def test_scales_of_any_sign(scale):
+    rng = np.random.default_rng(23)
+    c, Hq, Hkv, D = 70, 4, 2, 128
+    q, k, v = _draw(rng, (c, Hq, D), A.F16), _draw(rng, (c, Hkv, D), A.F16), _draw(rng, (c, Hkv, D), A.F16)
+    got = api.attn_prompt(_gpu(q, A.F16), _gpu(k, A.F16), _gpu(v, A.F16), _gpu(np.array([0, c], dtype=np.int32)), scale=scale)
+    want, spread = A.attention(q, k, v, scale, np.arange(c) + 1)
+    _close(_np(got), want, spread, A.F16, 2.0 ** -11)
+    cache = api.kv4_cache(5, 16, Hkv, D)
+    api.kv4_write(_gpu(k, A.F16), _gpu(v, A.F16), _gpu(np.arange(c, dtype=np.int32)), cache)
+    k, v = (A.dequantise(*A.quantise(x)) for x in (k, v))
+    got = api.kv4_attention(_gpu(q[None, -3:], A.F16), cache, _gpu(np.arange(5, dtype=np.int32)[None]), _gpu(np.array([c], dtype=np.int32)), scale=scale)
+    want, spread = A.attention(q[-3:], k, v, scale, c - 2 + np.arange(3))
+    _close(_np(got)[0], want, spread, A.F16, 2.0 ** -11)
+
+
+def test_example_layer():
+    """Prompts, then steps from a graph.  4 bits hold a vector to a step of a fifteenth of its range, 0.35 of its standard deviation or
+    so for 128 elements: errors of 0.1 of it in keys and values, each of which moves the result by about 0.1 of itself."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "attention_layer.py")
+    spec = importlib.util.spec_from_file_location("attention_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    got, want = (x.float().cpu().numpy() for x in example.run(8, 2, (150, 33, 64), steps=5))
+    assert got.shape == want.shape == (3, 5, 1024)
+    assert 0.01 < np.linalg.norm(got - want) / np.linalg.norm(want) < 0.25
+
+
 # --------------------------------------------------------------------------- streams, graphs, refusals
 def test_another_stream_and_a_graph():
     """A decode step (append, attention) captured and replayed with other inputs between the replays, the allocator in use beside it;
