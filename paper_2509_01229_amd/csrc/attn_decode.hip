@@ -54,6 +54,14 @@ __device__ __forceinline__ void halves8(uint32_t w, uint32_t zz, uint32_t (&o)[4
     for (int r = 0; r < 4; ++r)
         o[r] = __builtin_bit_cast(uint32_t, (f16x2v)(__builtin_bit_cast(f16x2v, o[r]) - __builtin_bit_cast(f16x2v, r & 1 ? zz << 4 : zz)));
 }
+// what the two halves of x, which are a and b rounded, leave of them (one instruction each: the halves are taken as they are)
+__device__ __forceinline__ uint32_t rest_of(uint32_t x, float a, float b)
+{
+    float c, d;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(c) : "v"(x), "v"(a));
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(d) : "v"(x), "v"(b));
+    return __builtin_bit_cast(uint32_t, f16x2v{(f16)c, (f16)d});
+}
 __device__ __forceinline__ v4f mfma16(const uint32_t (&a)[4], vec<f16, 8> b, v4f c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec<f16, 8>, u32x4{a[0], a[1], a[2], a[3]}), b, c, 0, 0, 0);
@@ -340,13 +348,6 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
             next = pages_of(key + 2 * kUnit);
             __builtin_amdgcn_sched_barrier(0);
             asm("" : "+v"(xv.w[0]), "+v"(xv.w[1]));  // (nothing of the values is looked at before)
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t word = xv.w[t][i];  // (a bit cast of a vector's element takes its first)
-                    sv[t][i] = __builtin_bit_cast(float, word);
-                }
             if (tail) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -355,9 +356,16 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
                         const int j = key + 16 * t + 4 * g + i;
 #pragma unroll
                         for (int r = 0; r < RT; ++r) sc[r][t][i] = j < limit[r] ? sc[r][t][i] : -__builtin_inff();
-                        sv[t][i] = j < ctx ? sv[t][i] : 0.0f;
+                        xv.w[t][i] = j < ctx ? xv.w[t][i] : 0u;
                     }
             }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t word = xv.w[t][i];  // (a bit cast of a vector's element takes its first)
+                    sv[t][i] = __builtin_bit_cast(float, word);
+                }
 #pragma unroll
             for (int i = 0; i < 8; i += 2) vt = max3_numbers(vt, sv[i >> 2][i & 3], sv[i >> 2][(i & 3) + 1]);
             float top[RT];
@@ -424,11 +432,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
                     }
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const f16x2v x = {(f16)p[2 * i], (f16)p[2 * i + 1]};
-                        w[2 * t + i] = __builtin_bit_cast(uint32_t, x);
-                        if constexpr (TWO)
-                            w2[2 * t + i] = __builtin_bit_cast(uint32_t, f16x2v{(f16)__builtin_fmaf((float)x[0], -1.0f, p[2 * i]),
-                                                                                (f16)__builtin_fmaf((float)x[1], -1.0f, p[2 * i + 1])});
+                        w[2 * t + i] = __builtin_bit_cast(uint32_t, f16x2v{(f16)p[2 * i], (f16)p[2 * i + 1]});
+                        if constexpr (TWO) w2[2 * t + i] = rest_of(w[2 * t + i], p[2 * i], p[2 * i + 1]);
                     }
                 }
                 weights[r] = __builtin_bit_cast(vec<f16, 8>, u32x4{w[0], w[1], w[2], w[3]});
@@ -445,14 +450,13 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
 #pragma unroll
                 for (int p2 = 0; p2 < 4; ++p2) halves8(xv.v[p2 >> 1][(p2 & 1) * (W / 4) + h], zz[p2], v8[p2]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t x[4] = {v8[0][e], v8[1][e], v8[2][e], v8[3][e]};
+                for (int two = TWO ? 0 : 1; two < 2; ++two)
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        if constexpr (TWO) o[r][4 * h + e] = mfma16(x, rest[r], o[r][4 * h + e]);
-                        o[r][4 * h + e] = mfma16(x, weights[r], o[r][4 * h + e]);
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t x[4] = {v8[0][e], v8[1][e], v8[2][e], v8[3][e]};
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) o[r][4 * h + e] = mfma16(x, two ? weights[r] : rest[r], o[r][4 * h + e]);
                     }
-                }
             }
             load(xv, key + kUnit);
             __builtin_amdgcn_sched_barrier(0);
