@@ -341,7 +341,7 @@ int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, int head_di
  * a query that sees no key gets zeros, rows that belong to no sequence are left alone.  Masked keys and values have no
  * part in the result whatever they hold.  total_q <= 2^28.  workspace as for w4a8_gemm (attn_prompt_workspace_size() bytes, 0
  * where there are many queries; the first 32 KiB zeroed once; may be NULL: slower where few queries read many keys). */
-size_t attn_prompt_workspace_size(int n_seqs, int total_q, int total_k, int Hq, int head_dim);
+size_t attn_prompt_workspace_size(int n_seqs, int total_q, int total_k, int Hq, int Hkv, int head_dim);
 int attn_prompt(int dtype, int n_seqs, int total_q, int total_k, int Hq, int Hkv, int head_dim, const void *q, long long q_token,
                 long long q_head, const void *k, long long k_token, long long k_head, const void *v, long long v_token, long long v_head,
                 const int *starts_q, const int *starts_k, float scale, int causal, void *out, void *workspace, size_t workspace_bytes,

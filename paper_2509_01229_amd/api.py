@@ -118,7 +118,7 @@ def lib() -> ctypes.CDLL:
     L.attn_prompt.restype = i
     L.attn_prompt.argtypes = [i] * 7 + [vp, ll, ll] * 3 + [vp, vp, f, i, vp, vp, sz, vp]
     L.attn_prompt_workspace_size.restype = sz
-    L.attn_prompt_workspace_size.argtypes = [i] * 5
+    L.attn_prompt_workspace_size.argtypes = [i] * 6
     L.w4a8_calib_stream_read.restype = i
     L.w4a8_calib_stream_read.argtypes = [vp, sz, vp]
     L.w4a8_calib_mfma_i8.restype = i
@@ -781,7 +781,7 @@ def attn_prompt(q, k, v, starts_q, starts_k=None, scale=None, causal=True, out=N
         raise ValueError(f"starts_q must be [sequences + 1], got {tuple(starts_q.shape)}")
     S = starts_q.shape[0] - 1
     out = torch.empty((Tq, Hq, D), dtype=q.dtype, device=q.device) if out is None else out
-    need = int(lib().attn_prompt_workspace_size(S, Tq, Tk, Hq, D))
+    need = int(lib().attn_prompt_workspace_size(S, Tq, Tk, Hq, Hkv, D))
     wsp, wsb = _ws(workspace, device=q.device, stream=stream, need=need)
     _check(lib().attn_prompt(_dtype_code(q), S, Tq, Tk, Hq, Hkv, D, *dq, *dk, *dv, _dev(starts_q, torch.int32, (S + 1,), "starts_q"),
                              _dev(starts_k, torch.int32, (S + 1,), "starts_k"), D ** -0.5 if scale is None else scale, int(bool(causal)),

@@ -2,8 +2,9 @@
 //
 //     o_i = sum_j softmax_j(scale * q_i . k_j) v_j,   j < len_k,   causal: j <= i + len_k - len_q
 //
-// One pass over the keys with a running maximum and sum (FP32).  A block takes 128 queries of one head (a wave 32 of them, held as
-// MFMA operands) through the keys, 64 at a time, which go straight into LDS while the 64 before them are worked on; both products on 32x32x16 MFMAs with the keys' side as the first operand
+// One pass over the keys with a running maximum and sum (FP32).  A block takes 128 rows, queries times the heads that share a kv head (few
+// queries fill it, and the causal mask cuts fewer of its tiles than for 128 queries of one head); a wave takes 32 of them, held as
+// MFMA operands, through the keys, 64 at a time, which go straight into LDS while the 64 before them are worked on; both products on 32x32x16 MFMAs with the keys' side as the first operand
 // (S^T = K Q^T, O^T = V^T P^T): a lane's scores are 32 keys of one query, and they are in the order in which the weights enter the
 // second product.  The values are read from LDS transposed (ds_read_b64_tr_b16).  Weights are rounded to the type of the values.
 //
@@ -24,11 +25,11 @@ struct PromptArgs {
     void *out;
     unsigned *tickets;
     float *parts;
-    int n_seqs, total_q, total_k, Hq, group, causal, tiles, splits;
+    int n_seqs, total_q, total_k, Hq, Hkv, group, causal, tiles, splits;
     float scale_log2;
 };
 
-constexpr int kQueries = 128, kKeys = 64, kPromptWaves = 4;
+constexpr int kRows = 128, kKeys = 64, kPromptWaves = 4;
 constexpr float kWeightBits = 6.0f;  // a row's largest weight is 2^6 when its maximum is up to date (2^14 at most)
 
 template <class T>
@@ -73,12 +74,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 
-    // Blocks with ids 8 apart run on one XCD: each XCD gets consecutive heads, and goes through a head's tiles from the last
+    // Blocks with ids 8 apart run on one XCD: each XCD gets consecutive kv heads, and goes through a head's tiles from the last
     // (the longest rows of keys) to the first, so that what runs at a time shares keys and values in the XCD's L2.
-    const int blocks = a.tiles * a.Hq * a.splits, per = (blocks + 7) >> 3, id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+    const int blocks = a.tiles * a.Hkv * a.splits, per = (blocks + 7) >> 3, id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
     if ((int)blockIdx.x >> 3 >= per || id >= blocks) return;
-    const int whole = id / a.splits, part = id % a.splits;  // a tile of a head, which part of its keys
-    const int head = whole / a.tiles, hk = head / a.group;
+    const int whole = id / a.splits, part = id % a.splits;  // a tile of a kv head, which part of its keys
+    const int hk = whole / a.tiles;
     int tile = a.tiles - 1 - whole % a.tiles;
 
     // the tile's sequence (tiles past the last: none)
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
             from = min(max(a.starts_q[s], 0), a.total_q);
             len = max(min(a.starts_q[s + 1], a.total_q) - from, 0);
         }
-        const int tiles = (len + kQueries - 1) / kQueries, upto = sums_up_to(tiles);
+        const int tiles = (len * a.group + kRows - 1) / kRows, upto = sums_up_to(tiles);
         const uint64_t past = __ballot(upto > tile);
         if (past) {
             const int at = __builtin_ctzll(past);
@@ -104,14 +105,13 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
     }
     if (seq < 0) return;
     const int k0 = min(max(a.starts_k[seq], 0), a.total_k), len_k = max(min(a.starts_k[seq + 1], a.total_k) - k0, 0);
-    const int first = tile * kQueries, before = len_k - len_q;  // of the block's rows; keys that every row sees, and one more each
-    const int row = first + 32 * wave + n;
-    const int limit = a.causal ? min(len_k, row + before + 1) : len_k;  // keys that this lane's row sees
-    const int until = a.causal ? min(len_k, min(first + kQueries, len_q) + before) : len_k;  // that some row of the block sees
-    // keys that all rows of the wave (some row of it, all rows of the block) see
-    const int wave_all = a.causal ? min(len_k, first + 32 * wave + before + 1) : len_k;
-    const int wave_any = a.causal ? min(len_k, first + 32 * wave + 32 + before) : len_k;
-    const int block_all = a.causal ? min(len_k, first + before + 1) : len_k;
+    // Rows: the queries' heads of this kv head, row = query * group + head.  The first rows of the block and of the wave, how many there are
+    const int first = tile * kRows, first_w = first + 32 * wave, rows = len_q * a.group, before = len_k - len_q;
+    const int row = first_w + n, query = min(row, rows - 1) / a.group, head = hk * a.group + min(row, rows - 1) % a.group;
+    const auto sees = [&](int r) { return a.causal ? min(len_k, min(r, rows - 1) / a.group + before + 1) : len_k; };  // keys
+    const int limit = sees(row), until = sees(first + kRows - 1), block_all = sees(first);
+    const int wave_all = __builtin_amdgcn_readfirstlane(sees(first_w)), wave_any = __builtin_amdgcn_readfirstlane(sees(first_w + 31));
+    const bool any_row = first_w < rows;
 
     // A wave loads 16 rows of a tile of keys and of values.  A row's pieces lie at their number XOR the row (keys; the lanes that read together
     // have 16 rows) or XOR twice the row (values: 4 rows, two pieces), so that none of them meet in a bank.
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
 
     vec<T, 8> q[D / 16];
     {
-        const T *src = static_cast<const T *>(a.q) + (long long)(q0 + min(row, len_q - 1)) * a.q_token + head * a.q_head + 8 * h;
+        const T *src = static_cast<const T *>(a.q) + (long long)(q0 + query) * a.q_token + head * a.q_head + 8 * h;
         const uint32_t sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u;  // (the scale's)
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
@@ -260,12 +260,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
         if (odd) s_odd = t + 1;
         wait_and_meet();
         if (t > t_last) issue(t - 1, buf ^ 1);
-        if (t * kKeys < wave_any) step(std::true_type{}, t * kKeys, s_odd == t + 1);  // (else: no row of the wave sees any of them)
+        if (any_row && t * kKeys < wave_any) step(std::true_type{}, t * kKeys, s_odd == t + 1);  // (else: no row of the wave sees any of them)
     }
     for (; t >= t_last; --t, buf ^= 1) {
         wait_and_meet();
         if (t > t_last) issue(t - 1, buf ^ 1);
-        step(std::false_type{}, t * kKeys, false);
+        if (any_row) step(std::false_type{}, t * kKeys, false);
     }
     const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, l), __builtin_bit_cast(unsigned, l), false, false);
     l = __builtin_bit_cast(float, (unsigned)both[0]) + __builtin_bit_cast(float, (unsigned)both[1]);
@@ -312,9 +312,9 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
                 for (int i = 0; i < 16; ++i) o[e][i] = o[e][i] * old + x[4 * e + (i >> 2)][i & 3] * by;
         }
     }
-    if (row >= len_q) return;
+    if (row >= rows) return;
     const float by = l == 0.0f ? 0.0f : 1.0f / l;
-    T *dst = static_cast<T *>(a.out) + ((size_t)(q0 + row) * a.Hq + head) * D;
+    T *dst = static_cast<T *>(a.out) + ((size_t)(q0 + query) * a.Hq + head) * D;
 #pragma unroll
     for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -339,14 +339,14 @@ int splits_of(long long blocks, int total_k, int n_seqs)
     if (blocks < 1 || blocks > 256) return 1;
     return (int)std::max<long long>(1, std::min<long long>({512 / blocks, total_k / std::max(n_seqs, 1) / 1024, 8}));
 }
-long long tiles_of(int total_q, int n_seqs) { return total_q / kQueries + n_seqs; }  // at most
+long long tiles_of(int total_q, int n_seqs, int group) { return (long long)total_q * group / kRows + n_seqs; }  // of a kv head, at most
 size_t part_bytes(int head_dim) { return sizeof(float) * 64 * kPromptWaves * (head_dim / 2 + 4); }
 }  // namespace
 
-extern "C" size_t attn_prompt_workspace_size(int n_seqs, int total_q, int total_k, int Hq, int head_dim)
+extern "C" size_t attn_prompt_workspace_size(int n_seqs, int total_q, int total_k, int Hq, int Hkv, int head_dim)
 {
-    if (n_seqs < 1 || total_q < 1 || total_k < 1 || Hq < 1 || !head_dim_ok(head_dim)) return 0;
-    const long long blocks = tiles_of(total_q, n_seqs) * Hq;
+    if (n_seqs < 1 || total_q < 1 || total_k < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv || !head_dim_ok(head_dim)) return 0;
+    const long long blocks = tiles_of(total_q, n_seqs, Hq / Hkv) * Hkv;
     const int splits = splits_of(blocks, total_k, n_seqs);
     return splits == 1 ? 0 : kTickets + (size_t)blocks * splits * part_bytes(head_dim);
 }
@@ -372,14 +372,14 @@ extern "C" int attn_prompt(int dtype, int n_seqs, int total_q, int total_k, int 
     if (total_k > 1 && (k_token < 0 || v_token < 0 || k_token > (1 << 24) || v_token > (1 << 24)))
         return fail(LQ_ERR_INVALID, "k and v: strides from token to token must be from 0 to 2^24 elements, got %lld and %lld", k_token, v_token);
     if (total_k <= 1) k_token = v_token = 0;
-    const long long tiles = tiles_of(total_q, n_seqs);
-    if (tiles * Hq > (1 << 24)) return fail(LQ_ERR_INVALID, "too many rows: %d queries of %d sequences, %d heads", total_q, n_seqs, Hq);
-    const size_t need = attn_prompt_workspace_size(n_seqs, total_q, total_k, Hq, head_dim);
-    const int splits = need && workspace && workspace_bytes >= need ? splits_of(tiles * Hq, total_k, n_seqs) : 1;
+    const long long tiles = tiles_of(total_q, n_seqs, Hq / Hkv);
+    if (tiles * Hkv > (1 << 23) || (long long)total_q * (Hq / Hkv) > (1 << 30)) return fail(LQ_ERR_INVALID, "too many rows: %d queries of %d sequences, %d heads", total_q, n_seqs, Hq);
+    const size_t need = attn_prompt_workspace_size(n_seqs, total_q, total_k, Hq, Hkv, head_dim);
+    const int splits = need && workspace && workspace_bytes >= need ? splits_of(tiles * Hkv, total_k, n_seqs) : 1;
     const PromptArgs a{q, k, v, q_token, q_head, k_token, k_head, v_token, v_head, starts_q, starts_k, out,
                        static_cast<unsigned *>(workspace), splits > 1 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + kTickets) : nullptr,
-                       n_seqs, total_q, total_k, Hq, Hq / Hkv, causal != 0, (int)tiles, splits, scale * 1.44269504f};
-    const dim3 grid((unsigned)((tiles * Hq * splits + 7) / 8 * 8));
+                       n_seqs, total_q, total_k, Hq, Hkv, Hq / Hkv, causal != 0, (int)tiles, splits, scale * 1.44269504f};
+    const dim3 grid((unsigned)((tiles * Hkv * splits + 7) / 8 * 8));
     (void)hipGetLastError();
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kPromptWaves), 0, static_cast<hipStream_t>(hip_stream), a); };
     if (dtype == LQ_F16)

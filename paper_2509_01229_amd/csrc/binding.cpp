@@ -445,7 +445,7 @@ PyObject *prompt(PyObject *, PyObject *const *a, Py_ssize_t n)
         Py_RETURN_NONE;
     const int S = (int)tensor(a[3]).size(0) - 1;
     at::Tensor workspace;
-    if (!workspace_of(a[8], a[10], q, stream, attn.prompt_workspace_size(S, (int)T, (int)Tk, (int)Hq, (int)D), workspace)) {
+    if (!workspace_of(a[8], a[10], q, stream, attn.prompt_workspace_size(S, (int)T, (int)Tk, (int)Hq, (int)Hkv, (int)D), workspace)) {
         if (PyErr_Occurred()) return nullptr;
         Py_RETURN_NONE;
     }

@@ -366,7 +366,7 @@ def test_prompts_few_queries_over_many_keys(dtype, D):
     sq, sk = (np.concatenate(([0], np.cumsum([x[i] for x in lens]))).astype(np.int32) for i in (0, 1))
     q, k, v = _draw(rng, (sq[-1], Hq, D), dtype) * np.float32(2.0), _draw(rng, (sk[-1], Hkv, D), dtype, True), _draw(rng, (sk[-1], Hkv, D), dtype)
     args = [_gpu(x, dtype) for x in (q, k, v)] + [_gpu(sq), _gpu(sk)]
-    need = int(api.lib().attn_prompt_workspace_size(len(lens), int(sq[-1]), int(sk[-1]), Hq, D))
+    need = int(api.lib().attn_prompt_workspace_size(len(lens), int(sq[-1]), int(sk[-1]), Hq, Hkv, D))
     assert need > 32768
     for causal in (True, False):
         ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
