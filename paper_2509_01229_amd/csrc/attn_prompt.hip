@@ -181,11 +181,19 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
     // One tile.  CUT: some row of the block does not see all of its keys.
     const auto step = [&](auto cut, int key, bool careful) {
         constexpr bool CUT = decltype(cut)::value;
+        // (the next fragments are read before the products of these: 2% on long prompts)
         v16f s[2] = {};
+        vec<T, 8> frag[2][2] = {{keys(0, 0), keys(1, 0)}};
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i)
+        for (int i = 0; i < D / 16; ++i) {
+            if (i + 1 < D / 16)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) s[u] = mfma32<T>(keys(u, i), q[i], s[u]);
+                for (int u = 0; u < 2; ++u) frag[(i + 1) & 1][u] = keys(u, i + 1);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) s[u] = mfma32<T>(frag[i & 1][u], q[i], s[u]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         if (CUT && key + kKeys > wave_all) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -233,16 +241,18 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
                     o[e] = mfma32<T>(__builtin_bit_cast(vec<T, 8>, x), p[u], o[e]);
                 }
             for (int j = 0; j < kKeys; ++j) {
-                const bool sees = key + j < limit;
+                const char *const at = reinterpret_cast<const char *>(s_v) + (buf * kKeys + j) * (D * 2) + 8 * h;
+                const int turn = (j & (CHUNKS / 2 - 1)) << 5;
+                const bool seen = key + j < limit;
 #pragma unroll
-                for (int e = 0; e < D / 32; ++e)
+                for (int c = 0; c < CHUNKS; ++c) {
+                    const auto x = *reinterpret_cast<const vec<T, 4> *>(at + ((16 * c) ^ turn));
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int d = 32 * e + 8 * (i >> 2) + 4 * h + (i & 3);
-                        const T x = reinterpret_cast<const T *>(&s_v[buf][j][(d >> 3) ^ ((j & (CHUNKS / 2 - 1)) << 1)])[d & 7];
-                        const float f = (float)x;
-                        if (sees && !(fabsf(f) < __builtin_inff())) o[e][i] += f;
+                    for (int r = 0; r < 4; ++r) {
+                        const float f = (float)x[r];
+                        o[c >> 2][4 * (c & 3) + r] += seen && !(fabsf(f) < __builtin_inff()) ? f : 0.0f;
                     }
+                }
             }
         }
     };
