@@ -74,31 +74,42 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 
-    // Blocks with ids 8 apart run on one XCD: each XCD gets consecutive kv heads, and goes through a head's tiles from the last
-    // (the longest rows of keys) to the first, so that what runs at a time shares keys and values in the XCD's L2.
-    const int blocks = a.tiles * a.Hkv * a.splits, per = (blocks + 7) >> 3, id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
-    if ((int)blockIdx.x >> 3 >= per || id >= blocks) return;
-    const int whole = id / a.splits, part = id % a.splits;  // a tile of a kv head, which part of its keys
-    const int hk = whole / a.tiles;
-    int tile = a.tiles - 1 - whole % a.tiles;
-
-    // the tile's sequence (tiles past the last: none)
-    int seq = -1, q0 = 0, len_q = 0;
-    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+    // The tiles of rows of all sequences; a lane looks at a sequence of every 64.
+    const auto rows_of = [&](int s0, int &from, int &len) {
         const int s = s0 + lane;
-        int from = 0, len = 0;
+        from = len = 0;
         if (s < a.n_seqs) {
             from = min(max(a.starts_q[s], 0), a.total_q);
             len = max(min(a.starts_q[s + 1], a.total_q) - from, 0);
         }
-        const int tiles = (len * a.group + kRows - 1) / kRows, upto = sums_up_to(tiles);
+        return sums_up_to((len * a.group + kRows - 1) / kRows);  // tiles of the sequences s0 .. s
+    };
+    int from, len, upto = rows_of(0, from, len), tiles = __builtin_amdgcn_readlane(upto, 63);
+    for (int s0 = 64; s0 < a.n_seqs; s0 += 64) {
+        int x, y;
+        tiles += __builtin_amdgcn_readlane(rows_of(s0, x, y), 63);
+    }
+    tiles = min(tiles, a.tiles);  // (more than there can be where sequences overlap)
+    // Blocks with ids 8 apart run on one XCD: each XCD gets consecutive kv heads, and goes through a head's tiles from the last
+    // (the longest rows of keys) to the first, so that what runs at a time shares keys and values in the XCD's L2.  Blocks that the grid
+    // has too many come last.
+    const int blocks = tiles * a.Hkv * a.splits, per = (blocks + 7) >> 3, id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+    if ((int)blockIdx.x >> 3 >= per || id >= blocks) return;
+    const int whole = id / a.splits, part = id % a.splits;  // a tile of a kv head, which part of its keys
+    const int hk = whole / tiles;
+    int tile = tiles - 1 - whole % tiles;
+
+    // the tile's sequence
+    int seq = -1, q0 = 0, len_q = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+        if (s0) upto = rows_of(s0, from, len);
         const uint64_t past = __ballot(upto > tile);
         if (past) {
             const int at = __builtin_ctzll(past);
             seq = s0 + at;
             q0 = __builtin_amdgcn_readlane(from, at);
             len_q = __builtin_amdgcn_readlane(len, at);
-            tile -= __builtin_amdgcn_readlane(upto - tiles, at);
+            tile -= at ? __builtin_amdgcn_readlane(upto, at - 1) : 0;
             break;
         }
         tile -= __builtin_amdgcn_readlane(upto, 63);
