@@ -32,6 +32,7 @@ struct DecodeArgs {
     void *out;
     unsigned *tickets;
     float *parts;
+    u32x4 *plan;
     int n_seqs, n_new, Hq, Hkv, group, rows, row_tiles, width, pages, lg_page, split, target;
     float scale_log2;  // softmax scale / ln 2
 };
@@ -124,13 +125,75 @@ constexpr float kWeightBits = 6.0f;       // a row's largest weight is 2^6 when 
 // units for all sequences, so many that about `target` blocks have work, and a block takes a chunk.  The chunks of an item are joined by the
 // last of its blocks to arrive at its ticket: each leaves its maxima, sums and unscaled results in the workspace (written and read past
 // the L2s, which the XCDs do not share), in the order of the split chunks of all items; the ticket is that of the item's first.
-// A sequence without keys has one unit all the same (its zeros are written there).  With split = 0 a block is an item.
+// A sequence without keys has one unit all the same (its zeros are written there).  With split = 0 a block is an item.  Each block finds its
+// chunk from all context lengths (1.2 us for up to 64 sequences), or reads it from what one block found before.
 constexpr int kMaxParts = 32, kLongChunk = 8;
 __host__ __device__ constexpr int blocks_per_cu(int row_tiles) { return row_tiles == 1 ? 4 : 2; }
 constexpr size_t kTickets = 32768;  // bytes at the head of the workspace, those of the GEMM's
 __host__ __device__ constexpr int part_floats(int rows, int D) { return rows * (D + 4); }
 
 __device__ __forceinline__ int units_of(int ctx) { return max(1, (ctx + kUnit - 1) / kUnit); }
+// Units of a chunk, for `total` units in all (of all items), `most` of one sequence: as many as make `target` chunks, half as many chunks
+// while they have at most kLongChunk units (a block's start and end cost as much as some units); and joining a part costs the last block
+// about a quarter of a unit where there are few, more than kMaxParts of them are never ahead.  (16 contexts of 4096, 64/8 heads: 8 units
+// 21.3 us, 4 units 24.2; two of 131072: 32 units 56.8, 16 units 71.5.)
+__device__ __forceinline__ int units_of_chunk(int total, int most, int target)
+{
+    return max(max(max((total + target - 1) / target, min((2 * total + target - 1) / target, kLongChunk)), (int)__builtin_sqrtf(0.25f * (float)most)),
+               (most + kMaxParts - 1) / kMaxParts);
+}
+// Where there are many items, a kernel of one block finds the chunks before the others start and puts long ones first; entry i has those of
+// blocks items * i on: the sequence, the place of its first chunk among the split ones (over items), chunk | chunks << 16, the
+// sequence's units.  A sequence of -1: no chunk.
+__host__ __device__ constexpr long long plan_entries(long long n_seqs, long long items, int target) { return target / items + n_seqs; }
+constexpr int kPlanThreads = 1024, kPlanClasses = 256;
+__global__ __launch_bounds__(kPlanThreads) void kv4_attention_plan_kernel(const DecodeArgs a)
+{
+    __shared__ int s_total[kPlanThreads / 64], s_most[kPlanThreads / 64], s_place[2][kPlanClasses];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, items = a.Hkv * a.row_tiles;
+    const int longest = a.width << a.lg_page;
+    const auto units = [&](int s) { return units_of(min(max(a.context[s], 0), longest)); };
+    int total = 0, most = 0;
+    for (int s = threadIdx.x; s < a.n_seqs; s += kPlanThreads) {
+        const int u = units(s);
+        total += u;
+        most = max(most, u);
+    }
+    total = sums_up_to(total);
+    most = lanes_up_to(most, [](int x, int y) { return max(x, y); });
+    if (lane == 63) s_total[wave] = total, s_most[wave] = most;
+    for (int i = threadIdx.x; i < 2 * kPlanClasses; i += kPlanThreads) s_place[0][i] = 0;
+    __syncthreads();
+    total = most = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) total += s_total[w], most = max(most, s_most[w]);
+    const int size = units_of_chunk(total * items, most, a.target);
+    // classes by the length of a sequence's chunks, long ones first
+    const float by_size = (float)kPlanClasses / (float)size;
+    const auto class_of = [&](int u, int c) { return min(max(kPlanClasses - (int)((float)u * by_size / (float)c), 0), kPlanClasses - 1); };
+    for (int s = threadIdx.x; s < a.n_seqs; s += kPlanThreads) {
+        const int u = units(s), c = (u + size - 1) / size, k = class_of(u, c);
+        atomicAdd(&s_place[0][k], c);
+        if (c > 1) atomicAdd(&s_place[1][k], c);
+    }
+    __syncthreads();
+    // first places: chunks (wave 0), split chunks (wave 1)
+    if (wave < 2) {
+        constexpr int EACH = kPlanClasses / 64;
+        int c[EACH], sum = 0;
+        for (int i = 0; i < EACH; ++i) c[i] = s_place[wave][EACH * lane + i], sum += c[i];
+        int place = sums_up_to(sum) - sum;
+        for (int i = 0; i < EACH; ++i) s_place[wave][EACH * lane + i] = place, place += c[i];
+        if (lane == 63) s_total[wave] = place;
+    }
+    __syncthreads();
+    const int entries = (int)plan_entries(a.n_seqs, items, a.target);
+    for (int s = threadIdx.x; s < a.n_seqs; s += kPlanThreads) {
+        const int u = units(s), c = (u + size - 1) / size, k = class_of(u, c);
+        const int at = atomicAdd(&s_place[0][k], c), part = c > 1 ? atomicAdd(&s_place[1][k], c) : 0;
+        for (int i = 0; i < c; ++i) a.plan[at + i] = u32x4{(unsigned)s, (unsigned)part, (unsigned)(i | c << 16), (unsigned)u};
+    }
+    for (int i = s_total[0] + (int)threadIdx.x; i < entries; i += kPlanThreads) a.plan[i] = u32x4{~0u, 0, 0, 0};
+}
 // 16 bytes past the L2 (device scope)
 constexpr int kShared = 16;  // sc1
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t shared_buffer(float *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(p, 0, bytes, 0x00027000); }
@@ -148,7 +211,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int P = 1 << a.lg_page, items = a.Hkv * a.row_tiles;
-    const size_t page_bytes = (size_t)a.Hkv * kv4_head_bytes(P, D);
+    const unsigned page_bytes = (unsigned)a.Hkv * (unsigned)kv4_head_bytes(P, D);
     const int longest = a.width << a.lg_page;
     // (integers that no kernel writes meanwhile: scalar loads)
     typedef const __attribute__((address_space(4))) int *ints;
@@ -157,7 +220,19 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
 
     // this block's sequence, item and units; the item's chunks, and where they are among the split ones
     int seq, item, unit = 0, units = 1, count, chunks = 1, chunk = 0, first_part = 0;
-    if (a.split) {
+    if (a.plan) {
+        const u32x4 *const plan = a.plan + blockIdx.x / (unsigned)items;
+        const u32x4 x = *(const __attribute__((address_space(4))) u32x4 *)(uintptr_t)plan;
+        seq = (int)x[0];
+        if (seq < 0) return;
+        item = (int)(blockIdx.x % (unsigned)items);
+        chunk = (int)(x[2] & 0xffffu);
+        chunks = (int)(x[2] >> 16);
+        units = (int)x[3];
+        first_part = (int)x[1] * items + item * chunks;
+        unit = (int)((unsigned)chunk * (unsigned)units / (unsigned)chunks);
+        count = (int)((unsigned)(chunk + 1) * (unsigned)units / (unsigned)chunks) - unit;
+    } else if (a.split) {
         int total = 0, most = 0;
         const int first64 = lane < a.n_seqs ? units_of(context(lane)) : 0;
         const auto units64 = [&](int s0) { return s0 == 0 ? first64 : s0 + lane < a.n_seqs ? units_of(context(s0 + lane)) : 0; };
@@ -167,12 +242,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
             most = max(most, __builtin_amdgcn_readlane(lanes_up_to(u, [](int x, int y) { return max(x, y); }), 63));
         }
         total *= items;
-        // Units of a chunk: as many as make a.target chunks, half as many chunks while they have at most kLongChunk units (a block's start
-        // and end cost as much as some units); and joining a part costs the last block about a quarter of a unit where there are few,
-        // more than kMaxParts of them are never ahead.  (16 contexts of 4096, 64/8 heads: 8 units 21.3 us, 4 units 24.2; two of 131072: 32 units
-        // 56.8, 16 units 71.5.)
-        const int size = max(max(max((total + a.target - 1) / a.target, min((2 * total + a.target - 1) / a.target, kLongChunk)),
-                                 (int)__builtin_sqrtf(0.25f * (float)most)), (most + kMaxParts - 1) / kMaxParts);
+        const int size = units_of_chunk(total, most, a.target);
         int before = 0, parts = 0;  // chunks, split chunks of the sequences that come before
         seq = -1;
         for (int s0 = 0; seq < 0 && s0 < a.n_seqs; s0 += 64) {
@@ -209,25 +279,27 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
         const int ctx = context(seq), end = min(ctx, (unit + count) * kUnit);
         int limit[RT];                        // keys that this lane's rows see
 
-        const int last_page = max((ctx - 1) >> a.lg_page, 0);
+        const unsigned last_page = max((ctx - 1) >> a.lg_page, 0);
 
         // the pages of 32 keys: numbers first, then addresses
         struct Place {
-            int page[2];
+            unsigned page[2];
         };
+        typedef const __attribute__((address_space(4))) char *bytes;
+        const bytes pages = (bytes)(table + (size_t)seq * a.width);
         const auto pages_of = [&](int key) {
             Place p;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) p.page[t] = table[(size_t)seq * a.width + min((key + 16 * t) >> a.lg_page, last_page)];
+            for (int t = 0; t < 2; ++t) p.page[t] = *(ints)(pages + 4 * min((unsigned)(key + 16 * t) >> a.lg_page, last_page));
             return p;
         };
         buf_t head[2];
         const auto go_to = [&](Place p, bool any) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const bool out_of_range = p.page[t] < 0 || p.page[t] >= a.pages;
+                const bool out_of_range = p.page[t] >= (unsigned)a.pages;
                 bad |= out_of_range;
-                head[t] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(cache + (size_t)(out_of_range ? 0 : p.page[t]) * page_bytes), 0,
+                head[t] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(cache + (uint64_t)(out_of_range ? 0u : p.page[t]) * page_bytes), 0,
                                                             any ? kv4_head_bytes(P, D) : 0, 0x00027000);
             }
         };
@@ -627,12 +699,20 @@ static int row_tiles_of(int rows) { return rows <= 16 ? 1 : 2; }
 // Blocks that have work where the keys can be split: as many as the CUs hold at a time
 static int target_of(int row_tiles) { return 256 * blocks_per_cu(row_tiles); }
 
+static size_t parts_bytes(int row_tiles, int head_dim) { return sizeof(float) * 2 * target_of(row_tiles) * part_floats(16 * row_tiles, head_dim); }
+// Whether the chunks are found by a kernel of their own: where there are as many items as blocks at a time.  Measured with and without, 8 kv
+// heads: 128 contexts of 400 to 8192 tokens 112 and 125 us, of 8192 each 193 and 190; 256 of 512 to 1024 48.5 and 55; 1000 of 100 to 1000
+// 146 and 221; with a quarter of the items, where most blocks run at once, it costs what it saves (32 contexts of 400 to 4096: 28.0 and
+// 26.1; 64 of 200 to 2048: 25.8 and 27.5).
+static bool planned(long long n_seqs, long long items, int row_tiles) { return n_seqs * items >= target_of(row_tiles); }
+
 extern "C" size_t kv4_attention_workspace_size(int n_seqs, int n_new, int Hq, int Hkv, int head_dim)
 {
     if (n_seqs < 1 || n_new < 1 || Hkv < 1 || Hq < 1 || Hq % Hkv || !head_dim_ok(head_dim)) return 0;
     const long long rows = (long long)n_new * (Hq / Hkv);
     const int RT = row_tiles_of((int)std::min(rows, 1LL << 20));
-    return kTickets + sizeof(float) * 2 * target_of(RT) * part_floats(16 * RT, head_dim);
+    const long long items = (rows + 16 * RT - 1) / (16 * RT) * Hkv;
+    return kTickets + parts_bytes(RT, head_dim) + (planned(n_seqs, items, RT) ? 16 * plan_entries(n_seqs, items, target_of(RT)) : 0);
 }
 
 extern "C" int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, int head_dim, const void *q, long long q_seq,
@@ -646,9 +726,9 @@ extern "C" int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, 
         return fail(LQ_ERR_INVALID, "bad shape: %d sequences, %d new tokens, %d heads, %d kv heads (heads a multiple of kv heads, up to 4096)",
                     n_seqs, n_new, Hq, Hkv);
     if (!page_ok(page_size)) return fail(LQ_ERR_INVALID, "page_size must be a power of two from 16 to 256, got %d", page_size);
-    if (num_pages < 1 || num_pages > INT32_MAX / page_size || table_width < 1 || table_width > INT32_MAX / page_size - 1)
-        return fail(LQ_ERR_INVALID, "num_pages and table_width times page_size must be from 1 to below 2^31, got %d and %d times %d", num_pages,
-                    table_width, page_size);
+    if (num_pages < 1 || num_pages > INT32_MAX / page_size || table_width < 1 || table_width > (1 << 30) / page_size)
+        return fail(LQ_ERR_INVALID, "num_pages times page_size must be from 1 to below 2^31, table_width times it to 2^30, got %d and %d times %d",
+                    num_pages, table_width, page_size);
     if (!(scale > -1e30f && scale < 1e30f)) return fail(LQ_ERR_INVALID, "scale must be finite");
     const long long rows = (long long)n_new * (Hq / Hkv);
     if (rows > (1 << 20)) return fail(LQ_ERR_INVALID, "too many rows: %d new tokens, %d heads a kv head", n_new, Hq / Hkv);
@@ -664,13 +744,17 @@ extern "C" int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, 
         return fail(LQ_ERR_ALIGN, "q: strides must be multiples of 8 elements, got %lld, %lld and %lld", q_seq, q_token, q_head);
     // units are counted in 32 bits; no more of them than this
     const long long most = items * n_seqs * (((long long)table_width * page_size + kUnit - 1) / kUnit);
-    const bool split = workspace && workspace_bytes >= kv4_attention_workspace_size(n_seqs, n_new, Hq, Hkv, head_dim) && most < (1LL << 31);
+    const bool split = workspace && workspace_bytes >= kv4_attention_workspace_size(n_seqs, n_new, Hq, Hkv, head_dim) && most < (1LL << 30);
     const DecodeArgs a{q, q_seq, q_token, q_head, static_cast<const uint8_t *>(cache), block_table, context, out,
                        static_cast<unsigned *>(workspace), split ? reinterpret_cast<float *>(static_cast<char *>(workspace) + kTickets) : nullptr,
+                       split && planned(n_seqs, items, RT) ? reinterpret_cast<u32x4 *>(static_cast<char *>(workspace) + kTickets + parts_bytes(RT, head_dim)) : nullptr,
                        n_seqs, n_new, Hq, Hkv, Hq / Hkv, (int)rows, (int)tiles, table_width, num_pages, log2_of(page_size), split,
                        target_of(RT), scale * 1.44269504f};
-    const dim3 grid((unsigned)(split ? std::min<long long>(target_of(RT) + items * n_seqs, most) : items * n_seqs));
+    const dim3 grid((unsigned)(a.plan  ? plan_entries(n_seqs, items, target_of(RT)) * items
+                               : split ? std::min<long long>(target_of(RT) + items * n_seqs, most)
+                                       : items * n_seqs));
     (void)hipGetLastError();
+    if (a.plan) hipLaunchKernelGGL(kv4_attention_plan_kernel, dim3(1), dim3(kPlanThreads), 0, static_cast<hipStream_t>(hip_stream), a);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kDecodeWaves), 0, static_cast<hipStream_t>(hip_stream), a); };
     auto by_dim = [&](auto x) {
         using T = decltype(x);

@@ -476,6 +476,34 @@ def test_attention_of_many_sequences():
             _close(g[b:b + 1], want, spread, A.F16, 2.0 ** -11, f"sequence {b} of {c}")
 
 
+@pytest.mark.parametrize("n,longest,Hq,Hkv,new,long", [
+    (140, 300, 8, 8, 1, {70: 5000, 139: 2500}),        # split ones among many
+    (70, 90, 32, 8, 5, {3: 3000, 4: 0}),               # 20 rows
+    (1100, 40, 2, 2, 1, {0: 0, 1099: 1500, 500: 129}),  # more sequences than a block has threads
+    (520, 0, 2, 2, 1, {}),                             # nothing but empty ones
+])
+def test_attention_of_more_items_than_run_at_once(n, longest, Hq, Hkv, new, long):
+    """The chunks are found before the blocks start, long ones first; all the same twice, and the tickets are back at zero."""
+    import torch
+
+    rng = np.random.default_rng(n)
+    contexts = [int(x) for x in rng.integers(0, longest + 1, n)]
+    for s, c in long.items():
+        contexts[s] = c
+    D, page, dtype = 64, 16, A.BF16
+    cache, table, keys, values = _filled(rng, contexts, page, Hkv, D, dtype)
+    q = _draw(rng, (n * new, Hq, D), dtype)
+    args = (_gpu(q, dtype).unflatten(0, (n, new)), cache, _gpu(table), _gpu(np.array(contexts, dtype=np.int32)))
+    ws = torch.zeros(int(api.lib().kv4_attention_workspace_size(n, new, Hq, Hkv, D)), dtype=torch.uint8, device="cuda")
+    ws[32768:] = 255
+    got = [_np(api.kv4_attention(*args, workspace=w)) for w in (ws, ws, ws[:16])]
+    assert np.array_equal(got[0], got[1]) and not ws[:32768].any()
+    for g in got[1:]:
+        for b, c in enumerate(contexts):
+            want, spread = A.attention(q[b * new:(b + 1) * new], keys[b], values[b], D ** -0.5, c - new + 1 + np.arange(new))
+            _close(g[b], want, spread, dtype, 2.0 ** -11, f"sequence {b} of {c}")
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.11, 1e-30])
 def test_scales_of_any_sign(scale):
     rng = np.random.default_rng(23)
