@@ -74,22 +74,21 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 
-    // The tiles of rows of all sequences; a lane looks at a sequence of every 64.
-    const auto rows_of = [&](int s0, int &from, int &len) {
-        const int s = s0 + lane;
-        from = len = 0;
-        if (s < a.n_seqs) {
-            from = min(max(a.starts_q[s], 0), a.total_q);
-            len = max(min(a.starts_q[s + 1], a.total_q) - from, 0);
+    // Up to 64 sequences: a lane looks at each, and `tiles` is the number of tiles that they have.  More of them: sequence s has the tiles from
+    // floor(rows before it / kRows) + s on (enough for its rows, one more at times, which has none), and is searched for 64 ways at a time.
+    // (1000 sequences of 100 tokens, 32/8 heads: looked at 64 at a time 1000 us, searched for 648; four of 256, 32/32 heads: the tiles that there are
+    // 13.2 us, those from floor(...) 17.1.)
+    const auto start_of = [&](int s) { return min(max(a.starts_q[s], 0), a.total_q); };
+    const bool few = a.n_seqs <= 64;
+    int from = 0, len = 0, upto = 0, tiles = a.tiles;
+    if (few) {
+        if (lane < a.n_seqs) {
+            from = start_of(lane);
+            len = max(min(a.starts_q[lane + 1], a.total_q) - from, 0);
         }
-        return sums_up_to((len * a.group + kRows - 1) / kRows);  // tiles of the sequences s0 .. s
-    };
-    int from, len, upto = rows_of(0, from, len), tiles = __builtin_amdgcn_readlane(upto, 63);
-    for (int s0 = 64; s0 < a.n_seqs; s0 += 64) {
-        int x, y;
-        tiles += __builtin_amdgcn_readlane(rows_of(s0, x, y), 63);
+        upto = sums_up_to((len * a.group + kRows - 1) / kRows);  // tiles of the sequences 0 .. lane
+        tiles = min(__builtin_amdgcn_readlane(upto, 63), a.tiles);  // (more than there can be where sequences overlap)
     }
-    tiles = min(tiles, a.tiles);  // (more than there can be where sequences overlap)
     // Blocks with ids 8 apart run on one XCD: each XCD gets consecutive kv heads, and goes through a head's tiles from the last
     // (the longest rows of keys) to the first, so that what runs at a time shares keys and values in the XCD's L2.  Blocks that the grid
     // has too many come last.
@@ -100,21 +99,28 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
     int tile = tiles - 1 - whole % tiles;
 
     // the tile's sequence
-    int seq = -1, q0 = 0, len_q = 0;
-    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-        if (s0) upto = rows_of(s0, from, len);
-        const uint64_t past = __ballot(upto > tile);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            seq = s0 + at;
-            q0 = __builtin_amdgcn_readlane(from, at);
-            len_q = __builtin_amdgcn_readlane(len, at);
-            tile -= at ? __builtin_amdgcn_readlane(upto, at - 1) : 0;
-            break;
+    int seq, q0, len_q;
+    if (few) {
+        seq = __builtin_ctzll(__ballot(upto > tile) | 1ull << 63);
+        q0 = __builtin_amdgcn_readlane(from, seq);
+        len_q = __builtin_amdgcn_readlane(len, seq);
+        tile -= seq ? __builtin_amdgcn_readlane(upto, seq - 1) : 0;
+    } else {
+        const auto first_tile = [&](int s) { return (int)((unsigned)(start_of(s) * a.group) / (unsigned)kRows) + s; };
+        int end = a.n_seqs;
+        seq = 0;
+        while (end - seq > 1) {
+            const int step = (end - seq + 63) >> 6, s = seq + step * lane;
+            const uint64_t past = __ballot(s >= end || first_tile(min(s, end - 1)) > tile);
+            const int at = past ? max(__builtin_ctzll(past) - 1, 0) : 63;
+            seq += step * at;
+            end = min(end, seq + step);
         }
-        tile -= __builtin_amdgcn_readlane(upto, 63);
+        q0 = __builtin_amdgcn_readfirstlane(start_of(seq));
+        len_q = __builtin_amdgcn_readfirstlane(max(min(a.starts_q[seq + 1], a.total_q) - q0, 0));
+        tile -= __builtin_amdgcn_readfirstlane(first_tile(seq));
     }
-    if (seq < 0) return;
+    if (tile < 0 || tile * kRows >= len_q * a.group) return;
     const int k0 = min(max(a.starts_k[seq], 0), a.total_k), len_k = max(min(a.starts_k[seq + 1], a.total_k) - k0, 0);
     // Rows: the queries' heads of this kv head, row = query * group + head.  The first rows of the block and of the wave, how many there are
     const int first = tile * kRows, first_w = first + 32 * wave, rows = len_q * a.group, before = len_k - len_q;

@@ -387,6 +387,32 @@ def test_prompts_few_queries_over_many_keys(dtype, D):
     assert np.array_equal(got, clean)
 
 
+@pytest.mark.parametrize("n,longest", [(65, 40), (150, 90), (4500, 3)])
+def test_prompts_many_sequences(n, longest):
+    """More sequences than a wave has lanes, empty ones among them, a long one, and rows before the first and behind the last that
+    are nobody's."""
+    rng = np.random.default_rng(n)
+    D, Hq, Hkv, dtype = 64, 6, 2, A.F16
+    lens_q, lens_k = rng.integers(0, longest + 1, n), rng.integers(0, longest + 1, n)
+    lens_q[n // 2], lens_k[n // 2], lens_k[n - 1] = 300, 333, 200
+    sq, sk = (np.concatenate(([at], at + np.cumsum(x))).astype(np.int32) for at, x in ((5, lens_q), (3, lens_k)))
+    q, k, v = _draw(rng, (sq[-1] + 9, Hq, D), dtype), _draw(rng, (sk[-1] + 2, Hkv, D), dtype, True), _draw(rng, (sk[-1] + 2, Hkv, D), dtype)
+    import torch
+
+    args = [_gpu(x, dtype) for x in (q, k, v)] + [_gpu(sq), _gpu(sk)]
+    for causal in (True, False):
+        out = torch.full_like(args[0], 7.0)
+        got = _np(api.attn_prompt(*args, causal=causal, out=out))
+        assert (got[:5] == 7.0).all() and (got[sq[-1]:] == 7.0).all()
+        for s in range(n):
+            a, b = int(lens_q[s]), int(lens_k[s])
+            if not a:
+                continue
+            limits = np.arange(a) + b - a + 1 if causal else np.full(a, b)
+            want, spread = A.attention(q[sq[s]:sq[s + 1]], k[sk[s]:sk[s + 1]], v[sk[s]:sk[s + 1]], D ** -0.5, limits)
+            _close(got[sq[s]:sq[s + 1]], want, spread, dtype, A.UNIT[dtype], f"sequence {s}")
+
+
 def test_prompts_scores_far_apart():
     rng = np.random.default_rng(12)
     n, D = 400, 128
