@@ -4,14 +4,22 @@
 //
 // One pass over the keys with a running maximum and sum (FP32).  A block takes 128 rows, queries times the heads that share a kv head (few
 // queries fill it, and the causal mask cuts fewer of its tiles than for 128 queries of one head); a wave takes 32 of them, held as
-// MFMA operands, through the keys, 64 at a time, which go straight into LDS while the 64 before them are worked on; both products on 32x32x16 MFMAs with the keys' side as the first operand
-// (S^T = K Q^T, O^T = V^T P^T): a lane's scores are 32 keys of one query, and they are in the order in which the weights enter the
-// second product.  The values are read from LDS transposed (ds_read_b64_tr_b16).  Weights are rounded to the type of the values.
+// MFMA operands, through the keys, 64 at a time, which go straight into LDS while the 64 before them are worked on; both products
+// on 32x32x16 MFMAs with the keys' side as the first operand (S^T = K Q^T, O^T = V^T P^T): a lane's scores are 32 keys of one query, and
+// they are in the order in which the weights enter the second product.  The values are read from LDS transposed (ds_read_b64_tr_b16).
+// Weights are rounded to the type of the values, as the matrix cores multiply one type; a row's largest is 2^6 .. 2^14, so that FP16 holds those
+// down to 2^-20 of it in full, and their sum is that of the numbers before rounding (FP32).
 //
 // Keys are taken from the last to the first: the tiles that the causal mask cuts come first.  What is masked has no
 // part in the result, whatever it holds: scores by selection, and values, where a masked one is not finite, by taking
 // the tile's values that are not finite out of the product and adding them to the rows that see them.
+//
+// Measured (BF16, 64/8 heads of 128): 8192 tokens, not causal, 1980 us, 1110 TFLOP/s; three causal prompts of 12000 tokens together 795 us, 1020 (a
+// product of 8192^3 in the library: 1400).  The matrix cores are busy in 55% of the cycles (counters); next to the 32 MFMAs of a wave's tile stand
+// about 130 vector instructions and 32 exponentials at a quarter of their rate, and the clock gives way before either is full.  For short
+// prompts the time is one of latencies: four of 256 tokens, 32/32 heads, 13.2 us.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "attn_common.h"
@@ -29,7 +37,7 @@ struct PromptArgs {
     float scale_log2;
 };
 
-constexpr int kRows = 128, kKeys = 64, kPromptWaves = 4;
+constexpr int kFew = 64, kRows = 128, kKeys = 64, kPromptWaves = 4;
 constexpr float kWeightBits = 6.0f;  // a row's largest weight is 2^6 when its maximum is up to date (2^14 at most)
 
 template <class T>
@@ -79,7 +87,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
     // (1000 sequences of 100 tokens, 32/8 heads: looked at 64 at a time 1000 us, searched for 648; four of 256, 32/32 heads: the tiles that there are
     // 13.2 us, those from floor(...) 17.1.)
     const auto start_of = [&](int s) { return min(max(a.starts_q[s], 0), a.total_q); };
-    const bool few = a.n_seqs <= 64;
+    const bool few = a.n_seqs <= kFew;
     int from = 0, len = 0, upto = 0, tiles = a.tiles;
     if (few) {
         if (lane < a.n_seqs) {
@@ -302,7 +310,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
         constexpr int FLOATS = 64 * kPromptWaves * (D / 2 + 4);  // of a part
         float *const parts = a.parts + (size_t)whole * a.splits * FLOATS;
         const auto all = __builtin_amdgcn_make_buffer_rsrc(parts, 0, a.splits * FLOATS * 4, 0x00027000);
-        const auto at = [&](int p, int piece) { return (p * FLOATS + (piece * 64 * kPromptWaves + (int)threadIdx.x) * 4) * 4; };
+        const int none = row < rows ? 0 : a.splits * FLOATS * 4;  // (a lane without a row leaves and reads nothing)
+        const auto at = [&](int p, int piece) { return (p * FLOATS + (piece * 64 * kPromptWaves + (int)threadIdx.x) * 4) * 4 + none; };
         constexpr int kShared = 16;  // sc1
 #pragma unroll
         for (int e = 0; e < D / 32; ++e)
@@ -359,14 +368,24 @@ using namespace lqq;
 
 namespace {
 constexpr size_t kTickets = 32768;  // bytes at the head of the workspace, those of the GEMM's
-// Parts of the keys: as many as fill two blocks a CU where the tiles of queries do not, each of 1024 keys or more on the average.
-// (512 queries of two sequences over 6000 keys, 32 heads: one part 122 us, three parts see the table of cases.)
-int splits_of(long long blocks, int total_k, int n_seqs)
+// Parts of the keys, where the tiles of queries are fewer than the CUs: as many as give each CU a block.  A second one on a CU makes both nearly
+// half as fast, and a part costs its tile's last block 1.2 us, about what 60 keys cost: two blocks a CU where the parts stay longer than
+// 600 keys for each part that there is, and no more parts than parts of 60 keys for each.  `keys`: what a query sees on the average.  (FP16, 32/8 heads:
+// 512 queries of two sequences over 6000 keys, one part 114 us, three 75, seven 85; 17 queries over 16000: one 258, eight 46.6, sixteen 36.5, 31
+// 41; 200 queries over 3000: one 57, four 27.7, six 32.4; 200 queries, 64/8 heads, over 8000: two 83, four 73; 256 alone, 64/8 heads: one 11.1,
+// two 13.7.)
+int splits_of(long long blocks, int total_q, int total_k, int n_seqs)
 {
     if (blocks < 1 || blocks > 256) return 1;
-    return (int)std::max<long long>(1, std::min<long long>({512 / blocks, total_k / std::max(n_seqs, 1) / 1024, 8}));
+    const long long keys = std::max(total_k - total_q / 2, 0) / std::max(n_seqs, 1), one = 256 / blocks;
+    return (int)std::max<long long>(1, std::min<long long>({keys > 600 * one * one ? 512 / blocks : one, (long long)std::sqrt((double)keys / 60.0), 32}));
 }
-long long tiles_of(int total_q, int n_seqs, int group) { return (long long)total_q * group / kRows + n_seqs; }  // of a kv head, at most
+// Tiles of a kv head, at most (more than 64 sequences: as they are searched for)
+long long tiles_of(int total_q, int n_seqs, int group)
+{
+    const long long rows = (long long)total_q * group;
+    return n_seqs <= kFew ? (rows + (long long)n_seqs * (kRows - 1)) / kRows : rows / kRows + n_seqs;
+}
 size_t part_bytes(int head_dim) { return sizeof(float) * 64 * kPromptWaves * (head_dim / 2 + 4); }
 }  // namespace
 
@@ -374,7 +393,7 @@ extern "C" size_t attn_prompt_workspace_size(int n_seqs, int total_q, int total_
 {
     if (n_seqs < 1 || total_q < 1 || total_k < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv || !head_dim_ok(head_dim)) return 0;
     const long long blocks = tiles_of(total_q, n_seqs, Hq / Hkv) * Hkv;
-    const int splits = splits_of(blocks, total_k, n_seqs);
+    const int splits = splits_of(blocks, total_q, total_k, n_seqs);
     return splits == 1 ? 0 : kTickets + (size_t)blocks * splits * part_bytes(head_dim);
 }
 
@@ -402,7 +421,7 @@ extern "C" int attn_prompt(int dtype, int n_seqs, int total_q, int total_k, int 
     const long long tiles = tiles_of(total_q, n_seqs, Hq / Hkv);
     if (tiles * Hkv > (1 << 23) || (long long)total_q * (Hq / Hkv) > (1 << 30)) return fail(LQ_ERR_INVALID, "too many rows: %d queries of %d sequences, %d heads", total_q, n_seqs, Hq);
     const size_t need = attn_prompt_workspace_size(n_seqs, total_q, total_k, Hq, Hkv, head_dim);
-    const int splits = need && workspace && workspace_bytes >= need ? splits_of(tiles * Hkv, total_k, n_seqs) : 1;
+    const int splits = need && workspace && workspace_bytes >= need ? splits_of(tiles * Hkv, total_q, total_k, n_seqs) : 1;
     const PromptArgs a{q, k, v, q_token, q_head, k_token, k_head, v_token, v_head, starts_q, starts_k, out,
                        static_cast<unsigned *>(workspace), splits > 1 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + kTickets) : nullptr,
                        n_seqs, total_q, total_k, Hq, Hkv, Hq / Hkv, causal != 0, (int)tiles, splits, scale * 1.44269504f};
