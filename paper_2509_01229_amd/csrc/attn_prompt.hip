@@ -138,8 +138,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
     const int wave_all = __builtin_amdgcn_readfirstlane(sees(first_w)), wave_any = __builtin_amdgcn_readfirstlane(sees(first_w + 31));
     const bool any_row = first_w < rows;
 
-    // A wave loads 16 rows of a tile of keys and of values.  A row's pieces lie at their number XOR the row (keys; the lanes that read together
-    // have 16 rows) or XOR twice the row (values: 4 rows, two pieces), so that none of them meet in a bank.
+    // A wave loads 16 rows of a tile of keys and of values.  A row's pieces lie at their number XOR what these give, so that lanes that read together
+    // do not meet in a bank: 16 rows and the same piece of each (keys), four rows and four pieces of each (values).  256 bytes are one round of the
+    // banks, a row or two of them.
+    const auto turn_k = [](int j) { return D == 128 ? j & 15 : j >> 1 & 7; };
+    const auto turn_v = [](int j) { return D == 128 ? (j & 3) << 2 : (j >> 1 & 1) << 2; };
     const char *const k_head = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + k0 * a.k_token + hk * a.k_head);
     const char *const v_head = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + k0 * a.v_token + hk * a.v_head);
     const uint32_t lds_k = (uint32_t)(size_t)(__attribute__((address_space(3))) void *)s_k, lds_v = (uint32_t)(size_t)(__attribute__((address_space(3))) void *)s_v;
@@ -150,8 +153,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int r = 16 * wave + ROWS * i + lane / CHUNKS, p = lane % CHUNKS, from = min(r, last);
-            k_at[i] = (uint32_t)from * k_row + 16 * (p ^ (r & (CHUNKS - 1)));
-            v_at[i] = (uint32_t)from * v_row + 16 * (p ^ ((r & (CHUNKS / 2 - 1)) << 1));
+            k_at[i] = (uint32_t)from * k_row + 16 * (p ^ turn_k(r));
+            v_at[i] = (uint32_t)from * v_row + 16 * (p ^ turn_v(r));
         }
     };
     const auto issue = [&](int t, int buf) {
@@ -192,14 +195,14 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
     // K fragment of 32 keys (u) for elements 16 i ..; V fragment of 16 keys (u) and elements 32 e ..
     const auto keys = [&](int u, int i) {
         const int j = 32 * u + n, c = 2 * i + h;
-        return __builtin_bit_cast(vec<T, 8>, s_k[buf][j][c ^ (j & (CHUNKS - 1))]);
+        return __builtin_bit_cast(vec<T, 8>, s_k[buf][j][c ^ turn_k(j)]);
     };
     const auto values = [&](int u, int e) {
         uint2 half[2];
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
             const int i = lane & 15, j = 16 * u + 8 * w + 4 * h + (i >> 2), c = 4 * e + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-            half[w] = read_transposed(reinterpret_cast<const char *>(&s_v[buf][j][c ^ ((j & (CHUNKS / 2 - 1)) << 1)]) + 8 * (i & 1));
+            half[w] = read_transposed(reinterpret_cast<const char *>(&s_v[buf][j][c ^ turn_v(j)]) + 8 * (i & 1));
         }
         return __builtin_bit_cast(vec<T, 8>, u32x4{half[0].x, half[0].y, half[1].x, half[1].y});
     };
@@ -267,7 +270,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
                 }
             for (int j = 0; j < kKeys; ++j) {
                 const char *const at = reinterpret_cast<const char *>(s_v) + (buf * kKeys + j) * (D * 2) + 8 * h;
-                const int turn = (j & (CHUNKS / 2 - 1)) << 5;
+                const int turn = turn_v(j) << 4;
                 const bool seen = key + j < limit;
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) {
