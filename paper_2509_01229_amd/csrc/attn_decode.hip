@@ -20,9 +20,10 @@
 // Measured (FP16, heads of 128): 128 contexts of 8192 tokens, 32/8 heads, 185 to 193 us, 6.0 to 6.2 TB/s of the 7.0 that a pure read reaches; two of
 // 131072, 64/8 heads, 60 us (4.7 TB/s, their 32 parts an item joined in 10 of them); 16 of 4096 21.7 us; one of 517, 32/32 heads, 8.7 us,
 // which are latencies: contexts, page numbers, first keys, and the join of the parts one after the other.  With 32 rows a pass (four
-// new tokens of 64/8 heads, BF16) two of 131072 77 us (3.7 TB/s): about 300 vector instructions and 36 MFMAs for 32 keys are what bounds it;
-// three blocks a CU instead of two (83 us) or the unpacking between the MFMAs (76) do not change that.
+// new tokens of 64/8 heads, BF16) two of 131072 70.5 us (4.0 TB/s): about 300 vector instructions and 36 MFMAs for 32 keys are what bounds it;
+// with blocks of four waves 77, and three of these a CU instead of two (83) or the unpacking between the MFMAs (76) did not change that.
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_common.h"
 
@@ -123,9 +124,9 @@ struct Values {
     }
 };
 
-constexpr int kDecodeWaves = 4;
-constexpr int kUnit = 32 * kDecodeWaves;  // keys that a block goes through at once
-constexpr float kWeightBits = 6.0f;       // a row's largest weight is 2^6 when its maximum is up to date
+constexpr int blocks_per_cu(int row_tiles, int waves) { return (row_tiles == 1 ? 16 : 8) / waves; }
+constexpr int unit_keys(int waves) { return 32 * waves; }  // keys that a block goes through at once
+constexpr float kWeightBits = 6.0f;                        // a row's largest weight is 2^6 when its maximum is up to date
 
 // The work is units of kUnit keys.  With split = 1 an item (sequence, kv head, tile of rows) is cut into chunks of the same number of
 // units for all sequences, so many that about `target` blocks have work, and a block takes a chunk.  The chunks of an item are joined by the
@@ -133,32 +134,38 @@ constexpr float kWeightBits = 6.0f;       // a row's largest weight is 2^6 when 
 // the L2s, which the XCDs do not share), in the order of the split chunks of all items; the ticket is that of the item's first.
 // A sequence without keys has one unit all the same (its zeros are written there).  With split = 0 a block is an item.  Each block finds its
 // chunk from all context lengths (1.2 us for up to 64 sequences), or reads it from what one block found before.
-constexpr int kMaxParts = 32, kLongChunk = 8;
-__host__ __device__ constexpr int blocks_per_cu(int row_tiles) { return row_tiles == 1 ? 4 : 2; }
+constexpr int kMaxParts = 32, kLongChunk = 1024;
 constexpr size_t kTickets = 32768;  // bytes at the head of the workspace, those of the GEMM's
 __host__ __device__ constexpr int part_floats(int rows, int D) { return rows * (D + 4); }
 
-__device__ __forceinline__ int units_of(int ctx) { return max(1, (ctx + kUnit - 1) / kUnit); }
+template <int WAVES>
+__device__ __forceinline__ int units_of(int ctx)
+{
+    return max(1, (ctx + unit_keys(WAVES) - 1) / unit_keys(WAVES));
+}
 // Units of a chunk, for `total` units in all (of all items), `most` of one sequence: as many as make `target` chunks, half as many chunks
-// while they have at most kLongChunk units (a block's start and end cost as much as some units); and joining a part costs the last block
-// about a quarter of a unit where there are few, more than kMaxParts of them are never ahead.  (16 contexts of 4096, 64/8 heads: 8 units
-// 21.3 us, 4 units 24.2; two of 131072: 32 units 56.8, 16 units 71.5.)
+// while they have at most kLongChunk keys (a block's start and end cost as much as some units); and joining a part costs the last block
+// about as much as 32 keys of a block of four waves where there are few, more than kMaxParts of them are never ahead.  (16 contexts of 4096,
+// 64/8 heads: 8 units 21.3 us, 4 units 24.2; two of 131072: 32 units 56.8, 16 units 71.5.)
+template <int WAVES>
 __device__ __forceinline__ int units_of_chunk(int total, int most, int target)
 {
-    return max(max(max((total + target - 1) / target, min((2 * total + target - 1) / target, kLongChunk)), (int)__builtin_sqrtf(0.25f * (float)most)),
+    return max(max(max((total + target - 1) / target, min((2 * total + target - 1) / target, kLongChunk / unit_keys(WAVES))),
+                   (int)__builtin_sqrtf((float)most / (float)WAVES)),
                (most + kMaxParts - 1) / kMaxParts);
 }
 // Where there are many items, a kernel of one block finds the chunks before the others start and puts long ones first; entry i has those of
 // blocks items * i on: the sequence, the place of its first chunk among the split ones (over items), chunk | chunks << 16, the
-// sequence's units.  A sequence of -1: no chunk.
+// sequence's context.  A sequence of -1: no chunk.
 __host__ __device__ constexpr long long plan_entries(long long n_seqs, long long items, int target) { return target / items + n_seqs; }
 constexpr int kPlanThreads = 1024, kPlanClasses = 256;
+template <int WAVES>
 __global__ __launch_bounds__(kPlanThreads) void kv4_attention_plan_kernel(const DecodeArgs a)
 {
     __shared__ int s_total[kPlanThreads / 64], s_most[kPlanThreads / 64], s_place[2][kPlanClasses];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, items = a.Hkv * a.row_tiles;
     const int longest = a.width << a.lg_page;
-    const auto units = [&](int s) { return units_of(min(max(a.context[s], 0), longest)); };
+    const auto units = [&](int s) { return units_of<WAVES>(min(max(a.context[s], 0), longest)); };
     int total = 0, most = 0;
     for (int s = threadIdx.x; s < a.n_seqs; s += kPlanThreads) {
         const int u = units(s);
@@ -172,7 +179,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv4_attention_plan_kernel(const 
     __syncthreads();
     total = most = 0;
     for (int w = 0; w < kPlanThreads / 64; ++w) total += s_total[w], most = max(most, s_most[w]);
-    const int size = units_of_chunk(total * items, most, a.target);
+    const int size = units_of_chunk<WAVES>(total * items, most, a.target);
     // classes by the length of a sequence's chunks, long ones first
     const float by_size = (float)kPlanClasses / (float)size;
     const auto class_of = [&](int u, int c) { return min(max(kPlanClasses - (int)((float)u * by_size / (float)c), 0), kPlanClasses - 1); };
@@ -196,7 +203,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv4_attention_plan_kernel(const 
     for (int s = threadIdx.x; s < a.n_seqs; s += kPlanThreads) {
         const int u = units(s), c = (u + size - 1) / size, k = class_of(u, c);
         const int at = atomicAdd(&s_place[0][k], c), part = c > 1 ? atomicAdd(&s_place[1][k], c) : 0;
-        for (int i = 0; i < c; ++i) a.plan[at + i] = u32x4{(unsigned)s, (unsigned)part, (unsigned)(i | c << 16), (unsigned)u};
+        for (int i = 0; i < c; ++i) a.plan[at + i] = u32x4{(unsigned)s, (unsigned)part, (unsigned)(i | c << 16), (unsigned)a.context[s]};
     }
     for (int i = s_total[0] + (int)threadIdx.x; i < entries; i += kPlanThreads) a.plan[i] = u32x4{~0u, 0, 0, 0};
 }
@@ -204,15 +211,17 @@ __global__ __launch_bounds__(kPlanThreads) void kv4_attention_plan_kernel(const 
 constexpr int kShared = 16;  // sc1
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t shared_buffer(float *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(p, 0, bytes, 0x00027000); }
 
-// (RT: tiles of 16 rows that share a pass over the keys)
-template <int D, class T, int RT>
-__global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_attention_kernel(const DecodeArgs a)
+// (RT: tiles of 16 rows that share a pass over the keys; WAVES: of a block, the keys of a unit shared between them)
+template <int D, class T, int RT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (RT == 1 ? 4 : 2)) void kv4_attention_kernel(const DecodeArgs a)
 {
     constexpr int W = D / 16, STEPS = D / 32;  // elements of a column group; MFMAs of a key tile
     constexpr int ROWS = 16 * RT;
     constexpr bool TWO = __is_same(T, f16);
-    __shared__ float s_o[kDecodeWaves][16][D + 4], s_m[kDecodeWaves][ROWS], s_l[kDecodeWaves][ROWS];
+    constexpr int kUnit = unit_keys(WAVES);
+    __shared__ float s_o[WAVES][16][D + 4], s_m[WAVES][ROWS], s_l[WAVES][ROWS];
     __shared__ int s_last;
+    __shared__ float s_scale[RT][16];
     __shared__ vec<f16, 8> s_q[RT][STEPS + 1][64];  // (the waves have the same queries)
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -222,10 +231,10 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
     // (integers that no kernel writes meanwhile: scalar loads)
     typedef const __attribute__((address_space(4))) int *ints;
     const ints table = (ints)(uintptr_t)a.table, contexts = (ints)(uintptr_t)a.context;
-    const auto context = [&](int s) { return min(max(contexts[s], 0), longest); };
+    const auto within = [&](int context) { return min(max(context, 0), longest); };
 
     // this block's sequence, item and units; the item's chunks, and where they are among the split ones
-    int seq, item, unit = 0, units = 1, count, chunks = 1, chunk = 0, first_part = 0;
+    int seq, context, item, unit = 0, units = 1, count, chunks = 1, chunk = 0, first_part = 0;
     if (a.plan) {
         const u32x4 *const plan = a.plan + blockIdx.x / (unsigned)items;
         const u32x4 x = *(const __attribute__((address_space(4))) u32x4 *)(uintptr_t)plan;
@@ -234,31 +243,34 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
         item = (int)(blockIdx.x % (unsigned)items);
         chunk = (int)(x[2] & 0xffffu);
         chunks = (int)(x[2] >> 16);
-        units = (int)x[3];
+        context = (int)x[3];
+        units = units_of<WAVES>(within(context));
         first_part = (int)x[1] * items + item * chunks;
         unit = (int)((unsigned)chunk * (unsigned)units / (unsigned)chunks);
         count = (int)((unsigned)(chunk + 1) * (unsigned)units / (unsigned)chunks) - unit;
     } else if (a.split) {
         int total = 0, most = 0;
-        const int first64 = lane < a.n_seqs ? units_of(context(lane)) : 0;
-        const auto units64 = [&](int s0) { return s0 == 0 ? first64 : s0 + lane < a.n_seqs ? units_of(context(s0 + lane)) : 0; };
+        const auto context64 = [&](int s0) { return s0 + lane < a.n_seqs ? contexts[s0 + lane] : 0; };
+        const int first64 = context64(0);
+        const auto units64 = [&](int s0, int c) { return s0 + lane < a.n_seqs ? units_of<WAVES>(within(c)) : 0; };
         for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-            const int u = units64(s0);
+            const int u = units64(s0, s0 ? context64(s0) : first64);
             total += __builtin_amdgcn_readlane(sums_up_to(u), 63);
             most = max(most, __builtin_amdgcn_readlane(lanes_up_to(u, [](int x, int y) { return max(x, y); }), 63));
         }
         total *= items;
-        const int size = units_of_chunk(total, most, a.target);
+        const int size = units_of_chunk<WAVES>(total, most, a.target);
         int before = 0, parts = 0;  // chunks, split chunks of the sequences that come before
         seq = -1;
         for (int s0 = 0; seq < 0 && s0 < a.n_seqs; s0 += 64) {
-            const int u = units64(s0), c = (u + size - 1) / size, sum = sums_up_to(c), split = sums_up_to(c > 1 ? c : 0);
+            const int keys = s0 ? context64(s0) : first64, u = units64(s0, keys), c = (u + size - 1) / size, sum = sums_up_to(c), split = sums_up_to(c > 1 ? c : 0);
             const uint64_t past = __ballot((before + sum) * items > (int)blockIdx.x);
             const int at = past ? __builtin_ctzll(past) : 63;
             before += __builtin_amdgcn_readlane(sum, at);
             parts += __builtin_amdgcn_readlane(split, at);
             if (past) {
                 seq = s0 + at;
+                context = __builtin_amdgcn_readlane(keys, at);
                 units = __builtin_amdgcn_readlane(u, at);
                 chunks = __builtin_amdgcn_readlane(c, at);
                 before -= chunks;
@@ -275,14 +287,15 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
     } else {
         seq = (int)blockIdx.x / items;
         item = (int)blockIdx.x % items;
-        count = units_of(context(seq));
+        context = contexts[seq];
+        count = units_of<WAVES>(within(context));
     }
 
     {
         const int rt = item % a.row_tiles, hk = item / a.row_tiles;
         const uint8_t *const cache = a.cache + (size_t)hk * kv4_head_bytes(P, D);
-        bool bad = contexts[seq] > longest;  // more than the table has pages for
-        const int ctx = context(seq), end = min(ctx, (unit + count) * kUnit);
+        bool bad = context > longest;  // more than the table has pages for
+        const int ctx = within(context), end = min(ctx, (unit + count) * kUnit);
         int limit[RT];                        // keys that this lane's rows see
 
         const unsigned last_page = max((ctx - 1) >> a.lg_page, 0);
@@ -339,11 +352,13 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
         }
         // Queries in the keys' operand order, times a power of two that brings the row's largest element to 4 .. 8 (exact down to 2^-16 of
         // it), those that meet even pairs (halves8) times 16.  A last operand holds what the zero points are multiplied with, minus 16 times
-        // the sum of the row's elements, as three numbers (33 bits of it).
+        // the sum of the row's elements, as three numbers (33 bits of it).  Of two tiles each is one wave's (one context of 2000, 32 rows: 16.1 us instead
+        // of 17.5); of one tile every wave writes the same, and no wave waits (one of 517: 8.8 instead of 9.0).
         constexpr int Q = STEPS + 1;
         float q_scale[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
+            if (RT == 2 && wave != (int)((blockIdx.x + r) % WAVES)) continue;
             const bool real = rt * ROWS + r * 16 + n < a.rows;
             float f[STEPS][8];
             const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;  // (the scale's)
@@ -371,7 +386,13 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
             q[STEPS] = vec<f16, 8>{};
             if (g == 0) q[STEPS][0] = s0, q[STEPS][1] = s1, q[STEPS][2] = s2;
 #pragma unroll
-            for (int i = 0; i < Q; ++i) s_q[r][i][lane] = q[i];  // (each wave writes all of them, the same)
+            for (int i = 0; i < Q; ++i) s_q[r][i][lane] = q[i];
+            if (RT == 2 && g == 0) s_scale[r][n] = q_scale[r];
+        }
+        if (RT == 2) {
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (not __syncthreads(): the keys stay in flight)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) q_scale[r] = s_scale[r][n];
         }
         const auto query = [&](int r, int i) { return s_q[r][i][lane]; };
 
@@ -550,7 +571,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
         }
         // thread: 8 elements of a row of each tile; the waves' results one tile at a time
         float most[RT], sum[RT], f[RT][8];
-        constexpr int STEP = 64 * kDecodeWaves;
+        constexpr int STEP = 64 * WAVES;
         static_assert(16 * D / 8 <= STEP, "");
         const int c = (int)threadIdx.x % (D / 8) * 8;
         int r16 = (int)threadIdx.x / (D / 8);
@@ -566,12 +587,12 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
             if (!mine) continue;
             most[r] = s_m[0][16 * r + r16];
 #pragma unroll
-            for (int w = 1; w < kDecodeWaves; ++w) most[r] = fmaxf(most[r], s_m[w][16 * r + r16]);
+            for (int w = 1; w < WAVES; ++w) most[r] = fmaxf(most[r], s_m[w][16 * r + r16]);
             sum[r] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[r][e] = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kDecodeWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 const float mw = s_m[w][16 * r + r16], by = mw == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mw - most[r]);
                 sum[r] += s_l[w][16 * r + r16] * by;
 #pragma unroll
@@ -609,7 +630,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
             };
             // threads: piece (8 elements) of a real row, and as many groups of threads as there are for the parts
             const int left = a.rows - rt * ROWS, rows16 = left >= 9 ? 16 : left >= 5 ? 8 : left >= 3 ? 4 : left;  // (a power of two)
-            const int pieces = rows16 * (D / 8), groups = 64 * kDecodeWaves / pieces, group = (int)threadIdx.x / pieces;
+            const int pieces = rows16 * (D / 8), groups = 64 * WAVES / pieces, group = (int)threadIdx.x / pieces;
             float *const s_f = &s_o[0][0][0];
             // the results of `count` chunks, from `from` on in steps of `by`, joined in their order
             const auto join = [&](int from, int by, int count) {
@@ -672,7 +693,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, blocks_per_cu(RT)) void kv4_atte
             };
             // kJoin chunks at a time, then their results, so that what is left to do when the last chunk is done is short (32 chunks, 32 rows:
             // 94.5 us instead of 101.3; 16 chunks of 8 rows, whose loads are all in flight together, in one go 10.9 us, in two 12.6)
-            constexpr int kJoin = RT == 1 ? 16 : 8;
+                        constexpr int kJoin = RT == 1 || WAVES == 8 ? 16 : 8;
             const int g0 = chunk / kJoin * kJoin, n = min(kJoin, chunks - g0), sets = (chunks + kJoin - 1) / kJoin;
             store(chunk);
             if (!last_at(g0, n)) return;
@@ -702,15 +723,20 @@ using namespace lqq;
 
 // Rows that share a pass: one tile of 16, or two
 static int row_tiles_of(int rows) { return rows <= 16 ? 1 : 2; }
+// Waves of a block: four, two or four of which a CU holds; with two tiles of rows and few items eight, which leave half as many parts to join.  (64/8
+// heads, 4 new tokens: two contexts of 131072 76.7 us with four waves, 70.5 with eight; 32 of 8192 69.6 and 67; 64 of 400 to 4000 62.6 and 51.5; but 128 of
+// these 88 and 97, and 300 of 50 to 500 62.6 and 103, as nothing else runs on a CU while a block starts and ends; one
+// of 2000 15.6 and 16.6.  Blocks of 16 waves with one tile:
+// 59 and 54.6 for two contexts of 131072, but 8.9 and 13.4 for one of 517.)
+static int waves_of(long long n_seqs, long long items, int row_tiles) { return row_tiles == 2 && n_seqs * items <= 512 ? 8 : 4; }
 // Blocks that have work where the keys can be split: as many as the CUs hold at a time
-static int target_of(int row_tiles) { return 256 * blocks_per_cu(row_tiles); }
-
-static size_t parts_bytes(int row_tiles, int head_dim) { return sizeof(float) * 2 * target_of(row_tiles) * part_floats(16 * row_tiles, head_dim); }
+static int target_of(int row_tiles, int waves) { return 256 * blocks_per_cu(row_tiles, waves); }
+static size_t parts_bytes(int row_tiles, int head_dim, int target) { return sizeof(float) * 2 * target * part_floats(16 * row_tiles, head_dim); }
 // Whether the chunks are found by a kernel of their own: where there are as many items as blocks at a time.  Measured with and without, 8 kv
 // heads: 128 contexts of 400 to 8192 tokens 112 and 125 us, of 8192 each 193 and 190; 256 of 512 to 1024 48.5 and 55; 1000 of 100 to 1000
 // 146 and 221; with a quarter of the items, where most blocks run at once, it costs what it saves (32 contexts of 400 to 4096: 28.0 and
 // 26.1; 64 of 200 to 2048: 25.8 and 27.5).
-static bool planned(long long n_seqs, long long items, int row_tiles) { return n_seqs * items >= target_of(row_tiles); }
+static bool planned(long long n_seqs, long long items, int target) { return n_seqs * items >= target; }
 
 extern "C" size_t kv4_attention_workspace_size(int n_seqs, int n_new, int Hq, int Hkv, int head_dim)
 {
@@ -718,7 +744,8 @@ extern "C" size_t kv4_attention_workspace_size(int n_seqs, int n_new, int Hq, in
     const long long rows = (long long)n_new * (Hq / Hkv);
     const int RT = row_tiles_of((int)std::min(rows, 1LL << 20));
     const long long items = (rows + 16 * RT - 1) / (16 * RT) * Hkv;
-    return kTickets + parts_bytes(RT, head_dim) + (planned(n_seqs, items, RT) ? 16 * plan_entries(n_seqs, items, target_of(RT)) : 0);
+    const int target = target_of(RT, waves_of(n_seqs, items, RT));
+    return kTickets + parts_bytes(RT, head_dim, target) + (planned(n_seqs, items, target) ? 16 * plan_entries(n_seqs, items, target) : 0);
 }
 
 extern "C" int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, int head_dim, const void *q, long long q_seq,
@@ -749,25 +776,29 @@ extern "C" int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, 
     if ((n_seqs > 1 && q_seq % 8) || (n_new > 1 && q_token % 8) || (Hq > 1 && q_head % 8))
         return fail(LQ_ERR_ALIGN, "q: strides must be multiples of 8 elements, got %lld, %lld and %lld", q_seq, q_token, q_head);
     // units are counted in 32 bits; no more of them than this
-    const long long most = items * n_seqs * (((long long)table_width * page_size + kUnit - 1) / kUnit);
+    const int waves = waves_of(n_seqs, items, RT), target = target_of(RT, waves);
+    const long long most = items * n_seqs * (((long long)table_width * page_size + unit_keys(waves) - 1) / unit_keys(waves));
     const bool split = workspace && workspace_bytes >= kv4_attention_workspace_size(n_seqs, n_new, Hq, Hkv, head_dim) && most < (1LL << 30);
     const DecodeArgs a{q, q_seq, q_token, q_head, static_cast<const uint8_t *>(cache), block_table, context, out,
                        static_cast<unsigned *>(workspace), split ? reinterpret_cast<float *>(static_cast<char *>(workspace) + kTickets) : nullptr,
-                       split && planned(n_seqs, items, RT) ? reinterpret_cast<u32x4 *>(static_cast<char *>(workspace) + kTickets + parts_bytes(RT, head_dim)) : nullptr,
+                       split && planned(n_seqs, items, target) ? reinterpret_cast<u32x4 *>(static_cast<char *>(workspace) + kTickets + parts_bytes(RT, head_dim, target)) : nullptr,
                        n_seqs, n_new, Hq, Hkv, Hq / Hkv, (int)rows, (int)tiles, table_width, num_pages, log2_of(page_size), split,
-                       target_of(RT), scale * 1.44269504f};
-    const dim3 grid((unsigned)(a.plan  ? plan_entries(n_seqs, items, target_of(RT)) * items
-                               : split ? std::min<long long>(target_of(RT) + items * n_seqs, most)
+                       target, scale * 1.44269504f};
+    const dim3 grid((unsigned)(a.plan  ? plan_entries(n_seqs, items, target) * items
+                               : split ? std::min<long long>(target + items * n_seqs, most)
                                        : items * n_seqs));
     (void)hipGetLastError();
-    if (a.plan) hipLaunchKernelGGL(kv4_attention_plan_kernel, dim3(1), dim3(kPlanThreads), 0, static_cast<hipStream_t>(hip_stream), a);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kDecodeWaves), 0, static_cast<hipStream_t>(hip_stream), a); };
+    if (a.plan)
+        hipLaunchKernelGGL(waves == 4 ? kv4_attention_plan_kernel<4> : kv4_attention_plan_kernel<8>, dim3(1), dim3(kPlanThreads), 0,
+                           static_cast<hipStream_t>(hip_stream), a);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, static_cast<hipStream_t>(hip_stream), a); };
     auto by_dim = [&](auto x) {
         using T = decltype(x);
-        if (head_dim == 128)
-            RT == 1 ? go(kv4_attention_kernel<128, T, 1>) : go(kv4_attention_kernel<128, T, 2>);
-        else
-            RT == 1 ? go(kv4_attention_kernel<64, T, 1>) : go(kv4_attention_kernel<64, T, 2>);
+        const auto of = [&](auto D) {
+            constexpr int d = decltype(D)::value;
+            RT == 1 ? go(kv4_attention_kernel<d, T, 1, 4>) : waves == 4 ? go(kv4_attention_kernel<d, T, 2, 4>) : go(kv4_attention_kernel<d, T, 2, 8>);
+        };
+        head_dim == 128 ? of(std::integral_constant<int, 128>{}) : of(std::integral_constant<int, 64>{});
     };
     dtype == LQ_F16 ? by_dim(f16{}) : by_dim(bf16{});
     const hipError_t e = hipGetLastError();
