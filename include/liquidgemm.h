@@ -329,7 +329,8 @@ int kv4_read(int dtype, int tokens, int Hkv, int head_dim, const void *cache, in
  * at place j % page_size of page block_table[seq][j / page_size] (int32 [n_seqs, table_width]; entries behind the context are not read).
  * scale multiplies the scores.  A token that sees no key gets zeros; a page number outside the cache, or a context longer than
  * the table, gives the sequence's kv heads that met it NaN.  workspace as for w4a8_gemm (kv4_attention_workspace_size() bytes, the
- * first 32 KiB zeroed once, may be NULL: slower where there are few sequences; shared with w4a8_gemm calls on the same stream). */
+ * first 32 KiB zeroed once, may be NULL: slower where there are few sequences, or many of unlike length; shared with w4a8_gemm calls on the
+ * same stream).  num_pages * page_size < 2^31, table_width * page_size <= 2^30. */
 size_t kv4_attention_workspace_size(int n_seqs, int n_new, int Hq, int Hkv, int head_dim);
 int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, int head_dim, const void *q, long long q_seq, long long q_token,
                   long long q_head, const void *cache, int num_pages, int page_size, const int *block_table, int table_width,

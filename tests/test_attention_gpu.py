@@ -625,6 +625,34 @@ def test_another_stream_and_a_graph():
     assert torch.equal(here, there)
 
 
+@pytest.mark.parametrize("n,Hq,Hkv,new", [(140, 8, 8, 1), (40, 32, 8, 5), (6, 16, 2, 4)])
+def test_a_graph_follows_the_contexts(n, Hq, Hkv, new):
+    """Attention captured with short contexts and replayed with others: what each block does is found anew in every replay."""
+    import torch
+
+    D, page, width = 64, 16, 20
+    rng = np.random.default_rng(31)
+    full = [page * width] * n
+    cache, table, _, _ = _filled(rng, full, page, Hkv, D, A.F16, garbage=False, spare=0)
+    table, ctx = _gpu(table), torch.ones(n, dtype=torch.int32, device="cuda")
+    q = _gpu(_draw(rng, (n * new, Hq, D), A.F16), A.F16).unflatten(0, (n, new))
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        api.kv4_attention(q, cache, table, ctx)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        captured = api.kv4_attention(q, cache, table, ctx)
+    for i in range(5):
+        lens = rng.integers(0, page * width + 1, n) if i % 2 else np.where(rng.random(n) < 0.1, page * width, i)
+        ctx.copy_(_gpu(lens.astype(np.int32)))
+        torch.randn(1 << 20, device="cuda").sum().item()
+        captured.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = captured.clone()
+        assert torch.equal(got, api.kv4_attention(q, cache, table, ctx)) and torch.isfinite(got).all()
+
+
 def test_refusals():
     import torch
 
