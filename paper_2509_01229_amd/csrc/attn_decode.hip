@@ -20,7 +20,7 @@
 // Measured (FP16, heads of 128): 128 contexts of 8192 tokens, 32/8 heads, 185 to 193 us, 6.0 to 6.2 TB/s of the 7.0 that a pure read reaches; two of
 // 131072, 64/8 heads, 60 us (4.7 TB/s, their 32 parts an item joined in 10 of them); 16 of 4096 21.7 us; one of 517, 32/32 heads, 8.7 us,
 // which are latencies: contexts, page numbers, first keys, and the join of the parts one after the other.  With 32 rows a pass (four
-// new tokens of 64/8 heads, BF16) two of 131072 70.5 us (4.0 TB/s): about 300 vector instructions and 36 MFMAs for 32 keys are what bounds it;
+// new tokens of 64/8 heads, BF16) two of 131072 70.5 us (4.0 TB/s): about 290 vector instructions and 36 MFMAs for 32 keys are what bounds it;
 // with blocks of four waves 77, and three of these a CU instead of two (83) or the unpacking between the MFMAs (76) did not change that.
 #include <algorithm>
 #include <type_traits>
