@@ -112,7 +112,8 @@ int liquidquant_unpack_weights(const void *W_packed, const uint8_t *gparams, int
  *     kernels leave the tickets zero again, so one initialisation serves any number of calls,
  *     shapes and HIP graph replays.  The rest needs no initialisation.
  *   - One workspace serves one call at a time: calls that may overlap in time on one GPU
- *     (different streams) need different workspaces; calls on one stream can share one.
+ *     (different streams) need different workspaces; calls on one stream can share one, whichever
+ *     host threads they come from (a call's launches stay together on its stream).
  *   - With a smaller (or NULL) workspace the dispatcher runs the same kernels without the
  *     split (or with as many slices as the workspace holds), which is slower for small N but
  *     gives the same result; a variant that names its split (w4a8_gemm_variant) fails with

@@ -26,6 +26,7 @@
 #include <type_traits>
 
 #include "attn_common.h"
+#include "workspace_turn.h"
 
 namespace lqq {
 
@@ -239,7 +240,7 @@ __global__ __launch_bounds__(64 * WAVES, (RT == 1 ? 4 : 2)) void kv4_attention_k
         const u32x4 *const plan = a.plan + blockIdx.x / (unsigned)items;
         const u32x4 x = *(const __attribute__((address_space(4))) u32x4 *)(uintptr_t)plan;
         seq = (int)x[0];
-        if (seq < 0) return;
+        if ((unsigned)seq >= (unsigned)a.n_seqs) return;
         item = (int)(blockIdx.x % (unsigned)items);
         chunk = (int)(x[2] & 0xffffu);
         chunks = (int)(x[2] >> 16);
@@ -788,6 +789,7 @@ extern "C" int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, 
                                : split ? std::min<long long>(target + items * n_seqs, most)
                                        : items * n_seqs));
     (void)hipGetLastError();
+    const WorkspaceTurn turn(split ? workspace : nullptr, hip_stream);  // (the list of chunks is the next kernel's, and no other call's)
     if (a.plan)
         hipLaunchKernelGGL(waves == 4 ? kv4_attention_plan_kernel<4> : kv4_attention_plan_kernel<8>, dim3(1), dim3(kPlanThreads), 0,
                            static_cast<hipStream_t>(hip_stream), a);

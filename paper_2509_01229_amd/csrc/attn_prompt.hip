@@ -23,6 +23,7 @@
 #include <type_traits>
 
 #include "attn_common.h"
+#include "workspace_turn.h"
 
 namespace lqq {
 
@@ -430,6 +431,7 @@ extern "C" int attn_prompt(int dtype, int n_seqs, int total_q, int total_k, int 
                        n_seqs, total_q, total_k, Hq, Hkv, Hq / Hkv, causal != 0, (int)tiles, splits, scale * 1.44269504f};
     const dim3 grid((unsigned)((tiles * Hkv * splits + 7) / 8 * 8));
     (void)hipGetLastError();
+    const WorkspaceTurn turn(splits > 1 ? workspace : nullptr, hip_stream);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kPromptWaves), 0, static_cast<hipStream_t>(hip_stream), a); };
     if (dtype == LQ_F16)
         head_dim == 128 ? go(attn_prompt_kernel<128, f16>) : go(attn_prompt_kernel<64, f16>);

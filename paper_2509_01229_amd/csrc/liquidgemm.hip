@@ -43,6 +43,7 @@
 
 #include "lqq_common.h"
 #include "lqq_device.h"
+#include "workspace_turn.h"
 
 namespace lqq {
 
@@ -1187,6 +1188,7 @@ static int run(int variant, const Args &a)
 {
     if (int rc = check_device_args(a)) return rc;
     if (a.M == 0) return LQ_OK;
+    const WorkspaceTurn turn(a.ws, a.stream);
     const int first = variant < 0 ? rows_of_first_launch(a.M, a.N, a.K) : a.M;
     if (first == a.M) return run_rows(variant, a);
     // two launches on the same stream (rows are independent); a workspace serves both in turn
