@@ -241,7 +241,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attn_prompt_kernel(const
             top = top > m_up ? top : m;  // (a row's results go by its own scores alone)
             const float by = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m - top) * scale);
             m = top;
-            m_up = top + (14.0f - kWeightBits) / scale;
+            m_up = top == -__builtin_inff() ? top : top + (14.0f - kWeightBits) / scale;  // (a quotient of infinity: one maximum is enough)
             base = top == -__builtin_inff() ? 0.0f : kWeightBits - top * scale;
             l *= by;
 #pragma unroll
