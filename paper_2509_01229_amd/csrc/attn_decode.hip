@@ -371,7 +371,8 @@ __global__ __launch_bounds__(64 * WAVES, (RT == 1 ? 4 : 2)) void kv4_attention_k
             }
             most = across_groups(most, [](float x, float y) { return fmaxf(x, y); });
             const int e = min(max((int)(__builtin_bit_cast(uint32_t, most) >> 23), 29), 227) - 129;
-            q_scale[r] = fmaxf(fabsf(a.scale_log2), 0x1p-126f) * 0x1p20f * power_of_two(e);
+            // (not zero, whatever the scale and the row: minus infinity times it has to stay that)
+            q_scale[r] = fmaxf(fabsf(a.scale_log2) * 0x1p20f * power_of_two(e), 0x1p-126f);
             vec<f16, 8> q[Q];
             float sum = 0.0f;
 #pragma unroll
@@ -484,7 +485,7 @@ __global__ __launch_bounds__(64 * WAVES, (RT == 1 ? 4 : 2)) void kv4_attention_k
                     const float now = top[r] > m_up[r] ? top[r] : m[r];  // (a row's results go by its own scores alone)
                     const float by = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m[r] - now) * q_scale[r]);
                     m[r] = now;
-                    m_up[r] = now + (14.0f - kWeightBits) / q_scale[r];
+                    m_up[r] = now == -__builtin_inff() ? now : now + (14.0f - kWeightBits) / q_scale[r];  // (a quotient of infinity: one maximum is enough)
                     base[r] = base_of(r);
                     l[r] *= by;
 #pragma unroll

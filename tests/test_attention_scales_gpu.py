@@ -51,3 +51,36 @@ def test_prompts_keys_in_parts(dtype, D, scale):
                 limits = np.arange(a) + b - a + 1 if causal else np.full(a, b)
                 want, spread = A.attention(q[sq[s]:sq[s + 1]], k[sk[s]:sk[s + 1]], v[sk[s]:sk[s + 1]], scale, limits)
                 _close(got[sq[s]:sq[s + 1]], want, spread, dtype, A.UNIT[dtype], f"sequence {s}, causal {causal}")
+
+
+def _decode(q, k, v, scale, dtype, page=16):
+    """q [new, heads, D] over the keys and values of one sequence; the definition's result, and what its weights' errors multiply."""
+    new, c, Hkv, D = len(q), len(k), k.shape[1], k.shape[2]
+    pages = -(-c // page)
+    cache = api.kv4_cache(pages, page, Hkv, D)
+    api.kv4_write(_gpu(k, dtype), _gpu(v, dtype), _gpu(np.arange(c, dtype=np.int32)), cache)
+    got = api.kv4_attention(_gpu(q[None], dtype), cache, _gpu(np.arange(pages, dtype=np.int32)[None]), _gpu(np.array([c], dtype=np.int32)), scale=scale)[0]
+    k, v = (A.dequantise(*A.quantise(x)) for x in (k, v))
+    return got, *A.attention(q, k, v, scale, c - new + 1 + np.arange(new))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,Hq,Hkv,new,c", [(128, 4, 2, 1, 70), (64, 8, 1, 5, 900), (128, 16, 2, 1, 3000), (128, 16, 2, 3, 3000)])
+@pytest.mark.parametrize("scale", [0.0, 1e-30, -1e-30, 1e-42, 0.1])
+def test_queries_of_zeros_over_the_cache(dtype, D, Hq, Hkv, new, c, scale):
+    """They see the mean of the values whatever the scale; next to rows that are not zero."""
+    rng = np.random.default_rng(41)
+    q, k, v = _draw(rng, (new, Hq, D), dtype), _draw(rng, (c, Hkv, D), dtype), _draw(rng, (c, Hkv, D), dtype)
+    q[:, 1] = 0
+    q[-1, -1] = 0
+    got, want, spread = _decode(q, k, v, scale, dtype)
+    _close(got, want, spread, dtype, 2.0 ** -11)
+
+
+@pytest.mark.parametrize("new", [1, 6])
+def test_queries_of_zeros_alone(new):
+    rng = np.random.default_rng(42)
+    k, v = _draw(rng, (200, 1, 64), A.F16), _draw(rng, (200, 1, 64), A.F16)
+    for scale in (0.0, 0.125):
+        got, want, spread = _decode(np.zeros((new, 4, 64), np.float32), k, v, scale, A.F16)
+        _close(got, want, spread, A.F16, 2.0 ** -11)
