@@ -370,9 +370,9 @@ __global__ __launch_bounds__(64 * WAVES, (RT == 1 ? 4 : 2)) void kv4_attention_k
                 for (int e = 0; e < 8; ++e) f[i][e] = real ? (float)raw[r][i][e] * sign : 0.0f, most = fmaxf(most, fabsf(f[i][e]));
             }
             most = across_groups(most, [](float x, float y) { return fmaxf(x, y); });
-            const int e = min(max((int)(__builtin_bit_cast(uint32_t, most) >> 23), 29), 227) - 129;
-            // (not zero, whatever the scale and the row: minus infinity times it has to stay that)
-            q_scale[r] = fmaxf(fabsf(a.scale_log2) * 0x1p20f * power_of_two(e), 0x1p-126f);
+            const int e = min(max((int)(__builtin_bit_cast(uint32_t, most) >> 23), 29), 254) - 129;
+            // (neither zero nor infinite, whatever the scale and the row: minus infinity times it stays that, and zero stays zero)
+            q_scale[r] = fminf(fmaxf(fabsf(a.scale_log2) * 0x1p20f * power_of_two(e), 0x1p-126f), 0x1p127f);
             vec<f16, 8> q[Q];
             float sum = 0.0f;
 #pragma unroll

@@ -84,3 +84,18 @@ def test_queries_of_zeros_alone(new):
     for scale in (0.0, 0.125):
         got, want, spread = _decode(np.zeros((new, 4, 64), np.float32), k, v, scale, A.F16)
         _close(got, want, spread, A.F16, 2.0 ** -11)
+
+
+@pytest.mark.parametrize("size", [2.0 ** 113, 2.0 ** 118, 2.0 ** 124])
+def test_queries_near_the_end_of_bf16(size):
+    """With a scale that brings the scores back to ordinary numbers, and with one that leaves all weight to the key that fits best."""
+    rng = np.random.default_rng(43)
+    k, v = _draw(rng, (90, 1, 64), A.BF16), _draw(rng, (90, 1, 64), A.BF16)
+    q = A.round_to(_draw(rng, (1, 2, 64), A.BF16) * np.float32(size), A.BF16)
+    assert np.isfinite(q).all()
+    got, want, spread = _decode(q, k, v, 0.125 / size, A.BF16)
+    _close(got, want, spread, A.BF16, 2.0 ** -11)
+    k[40, 0] = A.round_to(np.sign(q[0, 0]) * 3, A.BF16)
+    k[17, 0] = A.round_to(np.sign(q[0, 1]) * 3, A.BF16)
+    got, want, spread = _decode(q, k, v, 0.125, A.BF16)
+    _close(got, want, spread, A.BF16, 2.0 ** -11)
