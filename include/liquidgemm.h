@@ -286,7 +286,8 @@ int w4a8_quantize_activations(int M, int K, const uint16_t *X_f16, const float *
  *   LQ_ROPE_LINEAR   f_i / factor
  *   LQ_ROPE_NTK      base * factor^(rot_dim / (rot_dim - 2)) in place of base
  *   LQ_ROPE_YARN     f_i where a pair turns 32 times or more within original_positions, f_i / factor where once or less, in between
- *                    a mixture, linear in i; cosines and sines times 0.1 ln(factor) + 1
+ *                    a mixture, linear in i from the last pair of the first kind to the first of the second, which i < rot_dim / 2 may
+ *                    not reach (counted up to rot_dim - 1); cosines and sines times 0.1 ln(factor) + 1
  * factor >= 1; rot_dim a multiple of 16 up to 1024 (NTK: at least 16); base > 1. */
 #define LQ_ROPE_PLAIN 0
 #define LQ_ROPE_LINEAR 1

@@ -34,7 +34,7 @@ def rope_table(positions, rot, base=10000.0, scaling=None, factor=1.0, original=
         freq = freq / factor
     if scaling == "yarn":
         turns_at = lambda turns: rot * math.log(original / (2 * math.pi * turns)) / (2 * math.log(base))
-        low, high = max(math.floor(turns_at(32)), 0), min(math.ceil(turns_at(1)), half - 1)
+        low, high = max(math.floor(turns_at(32)), 0), min(math.ceil(turns_at(1)), rot - 1)
         if high <= low:
             high = low + 0.001
         mix = np.clip((np.arange(half) - low) / (high - low), 0, 1)

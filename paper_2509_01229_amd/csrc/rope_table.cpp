@@ -16,12 +16,13 @@ extern "C" int attn_rope_table(int max_positions, int rot_dim, double base, int 
     if (!table) return fail(LQ_ERR_INVALID, "null pointer");
     const int half = rot_dim / 2;
     if (scaling == LQ_ROPE_NTK) base *= std::pow(factor, rot_dim / (rot_dim - 2.0));
-    // the pairs that turn 32 times and once within the original positions: base^(-2i / rot_dim) original / 2 pi = turns, for i
+    // the pairs that turn 32 times and once within the original positions: base^(-2i / rot_dim) original / 2 pi = turns, for i (which may
+    // be past the last pair: then none is stretched in full)
     const auto pair_of = [&](double turns) { return rot_dim * std::log(original_positions / (turns * 2.0 * M_PI)) / (2.0 * std::log(base)); };
     double low = 0, high = 0, magnitude = 1.0;
     if (scaling == LQ_ROPE_YARN) {
         low = std::fmax(std::floor(pair_of(32.0)), 0.0);
-        high = std::fmin(std::ceil(pair_of(1.0)), half - 1.0);
+        high = std::fmin(std::ceil(pair_of(1.0)), rot_dim - 1.0);
         if (high <= low) high = low + 0.001;
         magnitude = 0.1 * std::log(factor) + 1.0;
     }
