@@ -16,6 +16,7 @@ from __future__ import annotations
 import ctypes
 import os
 import sys
+import threading
 import warnings
 
 import numpy as np
@@ -287,6 +288,7 @@ def w4a8_gemm_workspace_size(M: int, N: int, K: int, group: int) -> int:
 
 _ws_cache = {}
 _ws_retired = []
+_ws_lock = threading.Lock()  # (of two threads that find no buffer, one makes it: neither's may be lost)
 
 
 def w4a8_workspace_init(workspace, stream=None) -> None:
@@ -312,16 +314,17 @@ def _ws(workspace, M=0, N=0, K=0, group=64, device=None, stream=None, need=None)
             return None, 0
         # (the native module looks buffers up by the same key)
         key = (torch.device(device).index, int(stream) if stream is not None else int(torch.cuda.current_stream().cuda_stream))
-        buf = _ws_cache.get(key)
-        if buf is None or buf.numel() < need:
-            # A raw stream is unknown to torch's allocator, so a superseded buffer is kept
-            # alive (earlier launches on that stream may still use it) and the new one is
-            # zeroed under a device-wide synchronisation before any stream can see it.
-            if buf is not None:
-                _ws_retired.append(buf)
-            buf = torch.zeros(need, dtype=torch.uint8, device=device)
-            torch.cuda.synchronize(device)
-            _ws_cache[key] = buf
+        with _ws_lock:
+            buf = _ws_cache.get(key)
+            if buf is None or buf.numel() < need:
+                # A raw stream is unknown to torch's allocator, so a superseded buffer is kept
+                # alive (earlier launches on that stream may still use it) and the new one is
+                # zeroed under a device-wide synchronisation before any stream can see it.
+                if buf is not None:
+                    _ws_retired.append(buf)
+                buf = torch.zeros(need, dtype=torch.uint8, device=device)
+                torch.cuda.synchronize(device)
+                _ws_cache[key] = buf
         workspace = buf
     return _dev(workspace, torch.uint8, name="workspace"), workspace.numel()
 
