@@ -300,7 +300,7 @@ def w4a8_workspace_init(workspace, stream=None) -> None:
 
 
 def _ws(workspace, M=0, N=0, K=0, group=64, device=None, stream=None, need=None):
-    """Workspace pointer and size.  With workspace=None a zero-initialised buffer of the size
+    """Workspace pointer and size.  With workspace=None a zero-initialised buffer of at least the size
     the library asks for (`need`: of another call than a GEMM) is allocated once per (device, stream) and reused: calls on different
     streams may overlap and must not share one (device memory plumbing, nothing else)."""
     import torch
@@ -322,7 +322,9 @@ def _ws(workspace, M=0, N=0, K=0, group=64, device=None, stream=None, need=None)
                 # zeroed under a device-wide synchronisation before any stream can see it.
                 if buf is not None:
                     _ws_retired.append(buf)
-                buf = torch.zeros(need, dtype=torch.uint8, device=device)
+                # A power of two: needs that grow call by call (with a batch, a prompt) meet a wait and
+                # leave a buffer behind a few times in all, and less than the one in use.
+                buf = torch.zeros(1 << (need - 1).bit_length(), dtype=torch.uint8, device=device)
                 torch.cuda.synchronize(device)
                 _ws_cache[key] = buf
         workspace = buf
