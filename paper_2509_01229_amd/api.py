@@ -571,6 +571,7 @@ def w4a8_describe_grouped(row_offsets, N: int, K: int, group: int) -> str:
 
 
 # ------------------------------------------------------------------------------ attention
+# (For inference: tensors that require a gradient are refused where torch would record one.)
 LQ_F16, LQ_BF16 = 0, 1
 _ROPE_SCALING = {None: 0, "linear": 1, "ntk": 2, "yarn": 3}
 
@@ -601,6 +602,16 @@ def _heads(t, name, dtype=None, shape=None):
     if t.stride(-1) != 1 and t.shape[-1] != 1:
         raise ValueError(f"{name}: the elements of a head must be consecutive")
     return (ctypes.c_void_p(t.data_ptr()), *t.stride()[:-1])
+
+
+def _no_gradients(**tensors):
+    """The attention calls are for inference: a gradient that is asked for is refused, not left out without a word."""
+    import torch
+
+    if torch.is_grad_enabled():
+        for name, t in tensors.items():
+            if isinstance(t, torch.Tensor) and t.requires_grad:
+                raise ValueError(f"{name} requires a gradient, and this call computes none: call it under torch.no_grad(), or with {name}.detach()")
 
 
 def _dtype_code(t):
@@ -658,6 +669,7 @@ def attn_qk_norm_rope(q, k, positions, table, interleaved=False, q_norm=None, k_
         return _result(done)
     import torch
 
+    _no_gradients(q=q, k=k, table=table, q_norm=q_norm, k_norm=k_norm, out_q=out_q, out_k=out_k)
     dq, dk = _heads(q, "q"), _heads(k, "k", q.dtype)
     (T, Hq, D), Hkv = q.shape, k.shape[1]
     if tuple(k.shape) != (T, Hkv, D):
@@ -680,6 +692,7 @@ def kv4_write(k, v, slots, cache, stream=None):
         return _result(done)
     import torch
 
+    _no_gradients(k=k, v=v)
     dk, (T, Hkv, D) = _heads(k, "k"), k.shape
     dv = _heads(v, "v", k.dtype, (T, Hkv, D))
     pages, heads, page, dim = _kv4_shape(cache)
@@ -699,6 +712,7 @@ def kv4_append(q, k, v, positions, table, slots, cache, interleaved=False, q_nor
         return _result(done)
     import torch
 
+    _no_gradients(q=q, k=k, v=v, table=table, q_norm=q_norm, k_norm=k_norm, out_q=out_q)
     dq, dk = _heads(q, "q"), _heads(k, "k", q.dtype)
     (T, Hq, D), Hkv = q.shape, k.shape[1]
     if tuple(k.shape) != (T, Hkv, D):
@@ -745,6 +759,7 @@ def kv4_attention(q, cache, block_table, context, scale=None, out=None, workspac
         return _result(done)
     import torch
 
+    _no_gradients(q=q, out=out)
     pages, Hkv, page, D = _kv4_shape(cache)
     one = q.dim() == 3
     if q.dim() not in (3, 4) or q.shape[-1] != D:
@@ -776,6 +791,7 @@ def attn_prompt(q, k, v, starts_q, starts_k=None, scale=None, causal=True, out=N
         return _result(done)
     import torch
 
+    _no_gradients(q=q, k=k, v=v, out=out)
     dq, dk = _heads(q, "q"), _heads(k, "k", q.dtype)
     (Tq, Hq, D), (Tk, Hkv, _) = q.shape, k.shape
     if k.shape[2] != D:

@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -207,6 +208,8 @@ PyObject *grouped(PyObject *, PyObject *const *a, Py_ssize_t n)
 }
 
 // ---------------------------------------------------------------------------------- attention
+// A gradient is asked for: the general path says that there is none
+bool wants_gradient(PyObject *o) { return o != Py_None && c10::GradMode::is_enabled() && tensor(o).requires_grad(); }
 // [.., heads, head_dim] with strides of its own, FP16 or BF16 (`like`: as that one)
 bool heads(PyObject *o, int64_t dims, const at::Tensor *like = nullptr)
 {
@@ -216,7 +219,7 @@ bool heads(PyObject *o, int64_t dims, const at::Tensor *like = nullptr)
         return false;
     for (const int64_t n : t.sizes())
         if (n > INT_MAX) return false;
-    return t.stride(dims - 1) == 1 && t.size(dims - 1) > 1;
+    return t.stride(dims - 1) == 1 && t.size(dims - 1) > 1 && !wants_gradient(o);
 }
 bool heads_of(PyObject *o, const at::Tensor &like, std::initializer_list<int64_t> shape)
 {
@@ -261,7 +264,8 @@ struct Rotation {
 bool rotation(PyObject *positions, PyObject *table, PyObject *interleaved, PyObject *q_norm, PyObject *k_norm, PyObject *eps, int64_t T, int64_t D, Rotation &r)
 {
     if (!plain(positions, at::kInt, {T}) || !plain_dims(table, at::kFloat, 2) || !PyBool_Check(interleaved) || !PyFloat_CheckExact(eps) ||
-        (q_norm != Py_None && !plain(q_norm, at::kFloat, {D})) || (k_norm != Py_None && !plain(k_norm, at::kFloat, {D})))
+        (q_norm != Py_None && !plain(q_norm, at::kFloat, {D})) || (k_norm != Py_None && !plain(k_norm, at::kFloat, {D})) ||
+        wants_gradient(table) || wants_gradient(q_norm) || wants_gradient(k_norm))
         return false;
     r = Rotation{interleaved == Py_True, PyFloat_AS_DOUBLE(eps)};
     return true;
@@ -441,7 +445,7 @@ PyObject *prompt(PyObject *, PyObject *const *a, Py_ssize_t n)
     const int64_t T = q.size(0), Hq = q.size(1), D = q.size(2), Tk = k.size(0), Hkv = k.size(1);
     if (k.size(2) != D || !heads_of(a[2], q, {Tk, Hkv, D}) || !plain_dims(a[3], at::kInt, 1) || tensor(a[3]).size(0) < 1 ||
         !plain(a[4], at::kInt, {tensor(a[3]).size(0)}) || !scale_of(a[5], D, scale) || !PyBool_Check(a[6]) ||
-        (a[7] != Py_None && !plain(a[7], q.scalar_type(), {T, Hq, D})) || !stream_of(a[9], stream))
+        (a[7] != Py_None && !plain(a[7], q.scalar_type(), {T, Hq, D})) || wants_gradient(a[7]) || !stream_of(a[9], stream))
         Py_RETURN_NONE;
     const int S = (int)tensor(a[3]).size(0) - 1;
     at::Tensor workspace;
