@@ -25,7 +25,8 @@ using vec = T __attribute__((ext_vector_type(N)));
 // A key row is what one lane of each k block of a 16x16x32 MFMA loads at once, a group of four tokens of a column group is
 // what a lane needs of the values: both operands come out of 16-byte loads (D = 128) without a lane taking another's.
 __host__ __device__ constexpr int kv4_head_bytes(int P, int D) { return P * (D + 8); }
-constexpr int kv4_key_byte(int P, int D, int j) { return j * (D / 2); }
+template <int D>
+__device__ __forceinline__ int kv4_key_byte(int j) { return j * (D / 2); }
 template <int D>
 __device__ __forceinline__ int kv4_value_byte(int P, int j)  // of column group 0; the next one is D/8 bytes on
 {

@@ -695,7 +695,7 @@ __global__ __launch_bounds__(64 * WAVES, (RT == 1 ? 4 : 2)) void kv4_attention_k
             };
             // kJoin chunks at a time, then their results, so that what is left to do when the last chunk is done is short (32 chunks, 32 rows:
             // 94.5 us instead of 101.3; 16 chunks of 8 rows, whose loads are all in flight together, in one go 10.9 us, in two 12.6)
-                        constexpr int kJoin = RT == 1 || WAVES == 8 ? 16 : 8;
+            constexpr int kJoin = RT == 1 || WAVES == 8 ? 16 : 8;
             const int g0 = chunk / kJoin * kJoin, n = min(kJoin, chunks - g0), sets = (chunks + kJoin - 1) / kJoin;
             store(chunk);
             if (!last_at(g0, n)) return;

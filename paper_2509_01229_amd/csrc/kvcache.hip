@@ -94,7 +94,7 @@ __device__ __forceinline__ void store_codes(uint8_t *head, int P, int j, int l, 
         *reinterpret_cast<uint16_t *>(at) = (uint16_t)codes;
         *reinterpret_cast<uint16_t *>(at + (D == 128 ? 4 : 8)) = (uint16_t)(codes >> 16);
     } else {
-        *reinterpret_cast<uint32_t *>(head + j * (D / 2) + l * 4) = codes;
+        *reinterpret_cast<uint32_t *>(head + kv4_key_byte<D>(j) + l * 4) = codes;
     }
     if (l == 0) *reinterpret_cast<uint32_t *>(head + kv4_word_byte<D>(P, j, value)) = word;
 }
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(int tokens, int Hkv, cons
         const uint8_t *const at = page + (size_t)head * kv4_head_bytes(P, D);
         uint32_t kc = 0, vc = 0, kw = 0, vw = 0;
         if (held) {
-            kc = *reinterpret_cast<const uint32_t *>(at + j * (D / 2) + l * 4);
+            kc = *reinterpret_cast<const uint32_t *>(at + kv4_key_byte<D>(j) + l * 4);
             const uint8_t *const vb = at + kv4_value_byte<D>(P, j) + l * 16;
             vc = *reinterpret_cast<const uint16_t *>(vb) | (uint32_t)*reinterpret_cast<const uint16_t *>(vb + (D == 128 ? 4 : 8)) << 16;
             kw = *reinterpret_cast<const uint32_t *>(at + kv4_word_byte<D>(P, j, false));
