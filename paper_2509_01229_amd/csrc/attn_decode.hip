@@ -20,8 +20,9 @@
 // Measured (FP16, heads of 128): 128 contexts of 8192 tokens, 32/8 heads, 185 to 193 us, 6.0 to 6.2 TB/s of the 7.0 that a pure read reaches; two of
 // 131072, 64/8 heads, 60 us (4.7 TB/s, their 32 parts an item joined in 10 of them); 16 of 4096 21.7 us; one of 517, 32/32 heads, 8.7 us,
 // which are latencies: contexts, page numbers, first keys, and the join of the parts one after the other.  With 32 rows a pass (four
-// new tokens of 64/8 heads, BF16) two of 131072 70.5 us (4.0 TB/s): about 290 vector instructions and 36 MFMAs for 32 keys are what bounds it;
-// with blocks of four waves 77, and three of these a CU instead of two (83) or the unpacking between the MFMAs (76) did not change that.
+// new tokens of 64/8 heads, BF16) two of up to 131072 67 us (3.8 TB/s).  There 32 keys take about 290 vector instructions (half of a SIMD's cycles; 58% with
+// the exponentials' rate) and 36 MFMAs (a quarter): neither is full, and two waves a SIMD do not overlap them and the loads any better; with
+// blocks of four waves 77 us instead of 70.5, three of these a CU instead of two 83, the unpacking between the MFMAs 76.
 #include <algorithm>
 #include <type_traits>
 
@@ -135,6 +136,9 @@ constexpr float kWeightBits = 6.0f;                        // a row's largest we
 // the L2s, which the XCDs do not share), in the order of the split chunks of all items; the ticket is that of the item's first.
 // A sequence without keys has one unit all the same (its zeros are written there).  With split = 0 a block is an item.  Each block finds its
 // chunk from all context lengths (1.2 us for up to 64 sequences), or reads it from what one block found before.
+// Every item rounds its own number of chunks up, so there can be more than `target`, by up to one an item.  Where all chunks are as
+// long, the last of them then start when the others end: with four new tokens, 64/8 heads, BF16, where 256 blocks run at a time, 32 contexts of 8192
+// make 256 chunks (77 us, inputs that change) and 33 make 264 (117); two of 131072 make 256 (82), three 264 (160).
 constexpr int kMaxParts = 32, kLongChunk = 1024;
 constexpr size_t kTickets = 32768;  // bytes at the head of the workspace, those of the GEMM's
 __host__ __device__ constexpr int part_floats(int rows, int D) { return rows * (D + 4); }
@@ -144,8 +148,8 @@ __device__ __forceinline__ int units_of(int ctx)
 {
     return max(1, (ctx + unit_keys(WAVES) - 1) / unit_keys(WAVES));
 }
-// Units of a chunk, for `total` units in all (of all items), `most` of one sequence: as many as make `target` chunks, half as many chunks
-// while they have at most kLongChunk keys (a block's start and end cost as much as some units); and joining a part costs the last block
+// Units of a chunk, for `total` units in all (of all items), `most` of one sequence: as many as would cut all of them, end to end, into `target` chunks,
+// half as many chunks while they have at most kLongChunk keys (a block's start and end cost as much as some units); and joining a part costs the last block
 // about as much as 32 keys of a block of four waves where there are few, more than kMaxParts of them are never ahead.  (16 contexts of 4096,
 // 64/8 heads: 8 units 21.3 us, 4 units 24.2; two of 131072: 32 units 56.8, 16 units 71.5.)
 template <int WAVES>
@@ -728,10 +732,10 @@ static int row_tiles_of(int rows) { return rows <= 16 ? 1 : 2; }
 // Waves of a block: four, two or four of which a CU holds; with two tiles of rows and few items eight, which leave half as many parts to join.  (64/8
 // heads, 4 new tokens: two contexts of 131072 76.7 us with four waves, 70.5 with eight; 32 of 8192 69.6 and 67; 64 of 400 to 4000 62.6 and 51.5; but 128 of
 // these 88 and 97, and 300 of 50 to 500 62.6 and 103, as nothing else runs on a CU while a block starts and ends; one
-// of 2000 15.6 and 16.6.  Blocks of 16 waves with one tile:
+// of 2000 15.6 and 16.6.  The two and the 32 contexts make as many chunks as run at a time.  Blocks of 16 waves with one tile:
 // 59 and 54.6 for two contexts of 131072, but 8.9 and 13.4 for one of 517.)
 static int waves_of(long long n_seqs, long long items, int row_tiles) { return row_tiles == 2 && n_seqs * items <= 512 ? 8 : 4; }
-// Blocks that have work where the keys can be split: as many as the CUs hold at a time
+// Blocks that have work where the keys can be split, about: as many as the CUs hold at a time
 static int target_of(int row_tiles, int waves) { return 256 * blocks_per_cu(row_tiles, waves); }
 static size_t parts_bytes(int row_tiles, int head_dim, int target) { return sizeof(float) * 2 * target * part_floats(16 * row_tiles, head_dim); }
 // Whether the chunks are found by a kernel of their own: where there are as many items as blocks at a time.  Measured with and without, 8 kv

@@ -16,7 +16,8 @@
 //
 // Measured (BF16, 64/8 heads of 128): 8192 tokens, not causal, 1980 us, 1110 TFLOP/s; three causal prompts of 12000 tokens together 795 us, 1020 (a
 // product of 8192^3 in the library: 1400).  The matrix cores are busy in 55% of the cycles (counters); next to the 32 MFMAs of a wave's tile stand
-// about 130 vector instructions and 32 exponentials at a quarter of their rate, and the clock gives way before either is full.  For short
+// about 130 vector instructions and 32 exponentials at a quarter of their rate, 56% of a SIMD's cycles.  Neither is full: a wave's scores, softmax and second
+// product follow one another, and the two waves of a SIMD overlap them little.  For short
 // prompts the time is one of latencies: four of 256 tokens, 32/32 heads, 13.2 us.
 #include <algorithm>
 #include <cmath>

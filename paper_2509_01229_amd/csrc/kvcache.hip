@@ -20,7 +20,8 @@
 // tokens' cosines and sines over the heads that it goes through, and the value codes of four tokens, which share 16-byte pieces of
 // a page, are stored by one wave.  Bound by memory (2 bytes in, 2 or 17/32 out an element), by the launch for few tokens.  Measured, calls one
 // after another: norms and rotation of 4096 tokens with 64/8 heads of 128 28.9 us (5.2 TB/s; a large copy 5.4), of one token 5.1; 32768 tokens
-// of 8 kv heads written 34.2 us (5.0 TB/s), read back 28.7 (5.9); 16 tokens appended 4.8, 32768 of 64/8 heads 244 us (5.1 TB/s).
+// of 8 kv heads written 34.2 us (5.0 TB/s), read back 28.7 (5.9), 6000 tokens 9.1 to 10.4 and 5.8 to 7.0 (5.8 at a copy's rate: a wave writes head
+// after head with one load a lane in flight, and 1500 blocks do not cover its latency); 16 tokens appended 4.8, 32768 of 64/8 heads 244 us (5.1 TB/s).
 #include "attn_common.h"
 
 namespace lqq {
