@@ -53,6 +53,11 @@ extern "C" {
 #define LQ_ERR_WORKSPACE (-3) /* workspace_bytes < w4a8_gemm_workspace_size(...)     */
 #define LQ_ERR_HIP (-4)       /* a HIP runtime call or kernel launch failed          */
 
+/* Types of elements, where a call takes more than one. */
+#define LQ_F16 0
+#define LQ_BF16 1
+#define LQ_I8 2
+
 /* Library / packed-layout version (changes whenever the blob layout changes). */
 int w4a8_version(void);
 
@@ -256,6 +261,58 @@ int w4a8_quantize_activations(int M, int K, const uint16_t *X_f16, const float *
                               int8_t *X_i8, float *act_scales, void *hip_stream);
 
 /* ------------------------------------------------------------------------------------
+ * The norm and the gated activation in front of the products (device): they end in the X and act_scales that w4a8_gemm and
+ * w4a8_grouped_gemm consume.  dtype: that of x, LQ_F16 or LQ_BF16.  K % 8 == 0; rows of x may have a stride of their own (x_row, in
+ * elements, a multiple of 8).  M = 0 is a successful no-op.
+ * ------------------------------------------------------------------------------------ */
+
+/* The residual's addition, the root-mean-square norm and the INT8 quantisation in one pass:
+ *   h = x + residual, rounded to the type (h = x where residual and h are NULL)   -> h, [M,K] (what the next layer adds to)
+ *   r = fp32(1 / sqrt(mean(h^2) + eps)), the mean and the root in FP64;  y = (h * weight) * r, each product rounded to FP32
+ *   act_scales[m] = max_k |y| / 127  (1 if the row is zero);  X_i8 = clamp(rint(y / act_scales[m]), -127, 127)
+ *   y rounded to the type -> y_out [M,K], where it is not NULL (for a router)
+ * weight: device FP32 [K], or NULL for ones.  h may be residual or x itself (rows without gaps); other overlaps are not allowed.
+ * eps: positive.  The results are determined bit for bit (but where the FP64 mean lies within 2^-50 of a rounding border).  Rows with a NaN or an
+ * infinity in h, or for which h * weight overflows, give unspecified codes for that row only. */
+int w4a8_norm_quantize(int dtype, int M, int K, const void *x, long long x_row, const void *residual, long long residual_row,
+                       const float *weight, float eps, void *h, void *y_out, int8_t *X_i8, float *act_scales, void *hip_stream);
+
+/* y = gate / (1 + exp(-gate)) * up for x [M, 2K], a row's K gates before its K ups, in FP32 (exp and the quotient to within 2^-19 of themselves
+ * where |gate| <= 16), quantised as above.  Rows with a NaN or an infinity in x or y give unspecified codes for that row only. */
+int w4a8_swiglu_quantize(int dtype, int M, int K, const void *x, long long x_row, int8_t *X_i8, float *act_scales, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------
+ * Around the grouped GEMM (device): tokens sorted by expert, and back with weights.  Every token has `each` experts (1 .. 64); pair
+ * token * each + j is a token and its j-th expert.  Integers and FP32 arrays are 4-byte aligned, rows 16-byte; strides of rows are in elements.
+ * ------------------------------------------------------------------------------------ */
+
+/* Copies each token's row to a row for each of its experts, sorted by expert and within an expert by pair:
+ *   type        LQ_F16, LQ_BF16 or LQ_I8: that of X and rows;  K elements a row, a multiple of 16 bytes
+ *   X           [tokens, K], rows x_row apart;  act_scales [tokens] FP32, or NULL
+ *   experts     int32 [tokens, each]; a pair whose expert is not one of 0 .. n_experts - 1 has no row (n_experts: 1 .. 256)
+ *   rows        [tokens * each, K] out; row_scales [tokens * each] out, or NULL as act_scales is
+ *   row_offsets int32 [n_experts + 1] out: expert e has the rows row_offsets[e] .. row_offsets[e+1] - 1 (w4a8_grouped_gemm reads them on the
+ *               host); rows and scales behind the last one's are left alone
+ *   places      int32 [tokens, each] out: the pair's row, or -1
+ * A token may name an expert twice (two rows).  tokens < 2^23. */
+int moe_dispatch(int type, int tokens, int each, int n_experts, int K, const void *X, long long x_row, const float *act_scales,
+                 const int *experts, void *rows, float *row_scales, int *row_offsets, int *places, void *hip_stream);
+
+/* out[t] = sum_j weights[t][j] * Y[places[t][j]]: Y [rows, N] FP16 or BF16, N % 8 == 0, weights FP32 [tokens, each] or NULL for ones, out
+ * [tokens, N] of Y's type.  Sums in FP32 in the order of j, one rounding.  A place outside 0 .. rows - 1 adds nothing, whatever its weight.
+ * With weights = NULL this is also the gradient of moe_dispatch: of X, from the gradient of its rows. */
+int moe_combine(int dtype, int tokens, int each, int rows, int N, const void *Y, long long y_row, const int *places, const float *weights,
+                void *out, void *hip_stream);
+
+/* The gradients of moe_combine from grad [tokens, N], that of out:
+ *   grad_Y[places[t][j]] = weights[t][j] * grad[t], rounded once   ([rows, N], without gaps)
+ *   grad_weights[t][j]   = grad[t] . Y[places[t][j]], FP32 (0 for a place outside the rows)
+ * rows_used: device, one integer (moe_dispatch's row_offsets + n_experts): the rows of grad_Y from there on are zeroed; NULL: rows that no place names
+ * are left alone.  No two pairs may have the same place (undefined which is kept, piece by piece). */
+int moe_combine_backward(int dtype, int tokens, int each, int rows, int N, const void *grad, long long grad_row, const void *Y, long long y_row,
+                         const int *places, const float *weights, const int *rows_used, void *grad_Y, float *grad_weights, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------
  * Attention (device): what stands between the qkv projection and the output projection of a decoder layer, with a cache of
  * keys and values in 4 bits.  Rotary positions with the norms of queries and keys, the cache written, read back and attended
  * to, attention over whole prompts.
@@ -276,9 +333,6 @@ int w4a8_quantize_activations(int M, int K, const uint16_t *X_f16, const float *
  *       z = rint(-lo / s);  code = clamp(rint(x / s) + z, 0, 15);  it stands for (code - z) * s
  *     and is determined bit for bit.  A vector with an element that is not finite (or whose range overflows) stands for NaN.
  * ------------------------------------------------------------------------------------ */
-
-#define LQ_F16 0
-#define LQ_BF16 1
 
 /* Host.  table [max_positions][rot_dim] FP32 for attn_qk_norm_rope: row p holds the cosines of p * f_i, then the sines, i < rot_dim/2,
  * f_i = base^(-2i / rot_dim), computed in FP64 and rounded once.  `scaling` stretches the positions that a model was trained on:
@@ -337,6 +391,18 @@ size_t kv4_attention_workspace_size(int n_seqs, int n_new, int Hq, int Hkv, int 
 int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, int head_dim, const void *q, long long q_seq, long long q_token,
                   long long q_head, const void *cache, int num_pages, int page_size, const int *block_table, int table_width,
                   const int *context, float scale, void *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Attention of chunks of new tokens over the cache: sequence s has the queries starts_q[s] .. starts_q[s+1] - 1 of [total_q, Hq, head_dim] (int32
+ * [n_seqs + 1] on the device; any number of them, what lies outside the tensor is cut off), whose keys and values the cache holds already; cache,
+ * pages, context and scale as in kv4_attention: query i of a sequence's n sees the keys j < context[s] - n + 1 + i.  One call takes prompts'
+ * chunks and single tokens together.  out [total_q, Hq, head_dim]; a query that sees no key gets zeros, rows that belong to no
+ * sequence are left alone.  A page number outside the cache, or a context longer than the table, gives NaN to the queries that see keys of it (and may to
+ * others of the sequence).  total_q <= 2^28.  workspace as for w4a8_gemm (kv4_attention_chunks_workspace_size() bytes, 0 where there are many
+ * queries; the first 32 KiB zeroed once; may be NULL: slower where few queries read many keys). */
+size_t kv4_attention_chunks_workspace_size(int n_seqs, int total_q, int Hq, int Hkv, int head_dim, int page_size, int table_width);
+int kv4_attention_chunks(int dtype, int n_seqs, int total_q, int Hq, int Hkv, int head_dim, const void *q, long long q_token, long long q_head,
+                         const int *starts_q, const void *cache, int num_pages, int page_size, const int *block_table, int table_width,
+                         const int *context, float scale, void *out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Attention over packed prompts: queries starts_q[s] .. starts_q[s+1] - 1 of [total_q, Hq, head_dim] read keys and values starts_k[s] ..
  * starts_k[s+1] - 1 of [total_k, Hkv, head_dim] (int32 [n_seqs + 1] each, on the device; what lies outside the tensors is cut off);

@@ -120,6 +120,20 @@ def lib() -> ctypes.CDLL:
     L.attn_prompt.argtypes = [i] * 7 + [vp, ll, ll] * 3 + [vp, vp, f, i, vp, vp, sz, vp]
     L.attn_prompt_workspace_size.restype = sz
     L.attn_prompt_workspace_size.argtypes = [i] * 6
+    L.kv4_attention_chunks_workspace_size.restype = sz
+    L.kv4_attention_chunks_workspace_size.argtypes = [i] * 7
+    L.kv4_attention_chunks.restype = i
+    L.kv4_attention_chunks.argtypes = [i] * 6 + [vp, ll, ll, vp, vp, i, i, vp, i, vp, f, vp, vp, sz, vp]
+    L.w4a8_norm_quantize.restype = i
+    L.w4a8_norm_quantize.argtypes = [i, i, i, vp, ll, vp, ll, vp, f, vp, vp, vp, vp, vp]
+    L.w4a8_swiglu_quantize.restype = i
+    L.w4a8_swiglu_quantize.argtypes = [i, i, i, vp, ll, vp, vp, vp]
+    L.moe_dispatch.restype = i
+    L.moe_dispatch.argtypes = [i] * 5 + [vp, ll] + [vp] * 7
+    L.moe_combine.restype = i
+    L.moe_combine.argtypes = [i] * 5 + [vp, ll] + [vp] * 4
+    L.moe_combine_backward.restype = i
+    L.moe_combine_backward.argtypes = [i] * 5 + [vp, ll] * 2 + [vp] * 6
     L.w4a8_calib_stream_read.restype = i
     L.w4a8_calib_stream_read.argtypes = [vp, sz, vp]
     L.w4a8_calib_mfma_i8.restype = i
@@ -142,6 +156,7 @@ class _NoNative:
                           "build it with `python -m paper_2509_01229_amd.build`", RuntimeWarning, stacklevel=3)
 
     gemm = quantize = grouped = rope = write = append = read = decode = prompt = _decline
+    chunks = norm = swiglu = dispatch = combine = combine_backward = _decline
 
 
 def native_built_for() -> str:
@@ -169,6 +184,8 @@ def _bind(L) -> None:
     _binding.bind_attention(address(L.attn_qk_norm_rope), address(L.kv4_write), address(L.kv4_append), address(L.kv4_read),
                             address(L.kv4_attention_workspace_size), address(L.kv4_attention), address(L.attn_prompt_workspace_size),
                             address(L.attn_prompt))
+    _binding.bind_layer(address(L.kv4_attention_chunks_workspace_size), address(L.kv4_attention_chunks), address(L.w4a8_norm_quantize),
+                        address(L.w4a8_swiglu_quantize), address(L.moe_dispatch), address(L.moe_combine), address(L.moe_combine_backward))
     _native = _binding
 
 
@@ -570,9 +587,186 @@ def w4a8_describe_grouped(row_offsets, N: int, K: int, group: int) -> str:
     return text.value.decode()
 
 
+# ------------------------------------------- norm and gated activation, tokens sorted by expert and back
+# (As the attention calls: tensors that require a gradient are refused where torch would record one.  moe_combine_backward computes those of
+# moe_combine, and moe_combine without weights that of moe_dispatch.)
+LQ_F16, LQ_BF16, LQ_I8 = 0, 1, 2
+
+
+def _on_this_device(**tensors):
+    """These calls enqueue on the current device's stream: tensors of another device, or of several, are refused."""
+    import torch
+
+    here = torch.cuda.current_device() if any(isinstance(t, torch.Tensor) and t.is_cuda for t in tensors.values()) else None
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != here:
+            raise ValueError(f"{name} is on {t.device}, and the current device is cuda:{here}: call it under torch.cuda.device({name}.device)")
+
+
+def _rows(t, name, dtypes=None, shape=None):
+    """A matrix on the GPU whose rows may have a stride of their own: its pointer and that stride."""
+    import torch
+
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a torch tensor on the GPU")
+    dtypes = dtypes or (torch.float16, torch.bfloat16)
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must have dtype {' or '.join(str(d)[6:] for d in dtypes)}, got {t.dtype}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must have shape {tuple(shape) if shape is not None else '[rows, elements]'}, got {tuple(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be consecutive")
+    return ctypes.c_void_p(t.data_ptr()), t.stride(0)
+
+
+def w4a8_norm_quantize(x, weight=None, residual=None, eps=1e-6, want_y=False, out_q=None, out_scales=None, out_h=None, out_y=None, stream=None):
+    """The residual's addition, the root-mean-square norm and the INT8 quantisation of rows x [M, K], float16 or bfloat16: h = x + residual
+    (rounded to the type), y = h / sqrt(mean(h^2) + eps) * weight (float32 [K], or None for ones), INT8 codes with a scale a row.  out_h may be
+    residual or x itself.  Returns (X_i8 [M, K], act_scales [M], h or None without a residual, y rounded to the type or None without want_y or
+    out_y)."""
+    want_y = want_y or out_y is not None
+    if _native is None:
+        lib()
+    done = _native.norm(x, weight, residual, eps, want_y, out_q, out_scales, out_h, out_y, stream)
+    if done is not None:
+        return _result(done)
+    import torch
+
+    _no_gradients(x=x, weight=weight, residual=residual, out_h=out_h, out_y=out_y)
+    _on_this_device(x=x, weight=weight, residual=residual, out_q=out_q, out_scales=out_scales, out_h=out_h, out_y=out_y)
+    dx = _rows(x, "x")
+    M, K = x.shape
+    dr = _rows(residual, "residual", (x.dtype,), (M, K)) if residual is not None else (None, 0)
+    if residual is None and out_h is not None:
+        raise ValueError("out_h goes with a residual: without one h is x")
+    new = lambda given, dtype, shape=(M, K): torch.empty(shape, dtype=dtype, device=x.device) if given is None else given  # noqa: E731
+    out_q, out_scales = new(out_q, torch.int8), new(out_scales, torch.float32, (M,))
+    out_h = new(out_h, x.dtype) if residual is not None else None
+    out_y = new(out_y, x.dtype) if want_y else None
+    _check(lib().w4a8_norm_quantize(_dtype_code(x), M, K, *dx, *dr, _dev(weight, torch.float32, (K,), "weight"), eps, _dev(out_h, x.dtype, (M, K), "out_h"),
+                                    _dev(out_y, x.dtype, (M, K), "out_y"), _dev(out_q, torch.int8, (M, K), "out_q"),
+                                    _dev(out_scales, torch.float32, (M,), "out_scales"), _stream(stream)))
+    return out_q, out_scales, out_h, out_y
+
+
+def w4a8_swiglu_quantize(x, out_q=None, out_scales=None, stream=None):
+    """silu(gate) * up of rows x [M, 2K] = [gate | up], float16 or bfloat16 (the product of an MLP's, or the experts', first two matrices), as INT8
+    codes with a scale a row.  Returns (X_i8 [M, K], act_scales [M])."""
+    if _native is None:
+        lib()
+    done = _native.swiglu(x, out_q, out_scales, stream)
+    if done is not None:
+        return _result(done)
+    import torch
+
+    _no_gradients(x=x)
+    _on_this_device(x=x, out_q=out_q, out_scales=out_scales)
+    dx = _rows(x, "x")
+    M, K = x.shape[0], x.shape[1] // 2
+    if x.shape[1] % 2:
+        raise ValueError(f"x must be [rows, 2 * K], got {tuple(x.shape)}")
+    out_q = torch.empty((M, K), dtype=torch.int8, device=x.device) if out_q is None else out_q
+    out_scales = torch.empty((M,), dtype=torch.float32, device=x.device) if out_scales is None else out_scales
+    _check(lib().w4a8_swiglu_quantize(_dtype_code(x), M, K, *dx, _dev(out_q, torch.int8, (M, K), "out_q"),
+                                      _dev(out_scales, torch.float32, (M,), "out_scales"), _stream(stream)))
+    return out_q, out_scales
+
+
+def moe_dispatch(X, experts, n_experts: int, act_scales=None, out=None, out_scales=None, stream=None):
+    """Each token's row of X [tokens, K] (int8, with act_scales [tokens], or float16 or bfloat16) to a row for each of its experts (int32
+    [tokens, each]), sorted by expert, within an expert in the tokens' order.  A pair whose expert is not one of 0 .. n_experts - 1 has no row.  Returns (rows
+    [tokens * each, K], row_scales or None, row_offsets int32 [n_experts + 1], places int32 [tokens, each]: the pair's row, or -1); rows
+    from row_offsets[n_experts] on are left as they were.  w4a8_grouped_gemm takes row_offsets.tolist() and the rows up to there."""
+    if _native is None:
+        lib()
+    done = _native.dispatch(X, experts, n_experts, act_scales, out, out_scales, stream)
+    if done is not None:
+        return _result(done)
+    import torch
+
+    _no_gradients(X=X, act_scales=act_scales, out=out, out_scales=out_scales)
+    _on_this_device(X=X, experts=experts, act_scales=act_scales, out=out, out_scales=out_scales)
+    dx = _rows(X, "X", (torch.int8, torch.float16, torch.bfloat16))
+    (T, K), code = X.shape, {torch.int8: LQ_I8, torch.float16: LQ_F16, torch.bfloat16: LQ_BF16}[X.dtype]
+    if not isinstance(experts, torch.Tensor) or experts.dim() != 2:
+        raise ValueError("experts must be [tokens, experts of each]")
+    each = experts.shape[1]
+    ids = _dev(experts, torch.int32, (T, each), "experts")
+    if not 1 <= n_experts <= 256:
+        raise ValueError(f"n_experts must be 1 to 256, got {n_experts}")
+    if act_scales is None and out_scales is not None:
+        raise ValueError("out_scales goes with act_scales")
+    out = torch.empty((T * each, K), dtype=X.dtype, device=X.device) if out is None else out
+    if act_scales is not None and out_scales is None:
+        out_scales = torch.empty((T * each,), dtype=torch.float32, device=X.device)
+    offsets, places = (torch.empty(shape, dtype=torch.int32, device=X.device) for shape in ((n_experts + 1,), (T, each)))
+    _check(lib().moe_dispatch(code, T, each, n_experts, K, *dx, _dev(act_scales, torch.float32, (T,), "act_scales"), ids,
+                              _dev(out, X.dtype, (T * each, K), "out"), _dev(out_scales, torch.float32, (T * each,), "out_scales"),
+                              _dev(offsets, torch.int32), _dev(places, torch.int32), _stream(stream)))
+    return out, out_scales, offsets, places
+
+
+def _places(places, weights):
+    import torch
+
+    if not isinstance(places, torch.Tensor) or places.dim() != 2:
+        raise ValueError("places must be [tokens, rows of each]")
+    return (*places.shape, _dev(places, torch.int32, name="places"), _dev(weights, torch.float32, tuple(places.shape), "weights"))
+
+
+def moe_combine(Y, places, weights=None, out=None, stream=None):
+    """The sum of each token's rows of Y [rows, N] (float16 or bfloat16): out[t] = sum_j weights[t, j] * Y[places[t, j]]; weights float32
+    [tokens, each], or None for ones; places int32 [tokens, each] (moe_dispatch's; outside the rows: adds nothing).  Returns out [tokens, N].  Without
+    weights: the gradient of moe_dispatch's X, from that of its rows."""
+    if _native is None:
+        lib()
+    done = _native.combine(Y, places, weights, out, stream)
+    if done is not None:
+        return _result(done)
+    import torch
+
+    _no_gradients(Y=Y, weights=weights, out=out)
+    _on_this_device(Y=Y, places=places, weights=weights, out=out)
+    dy = _rows(Y, "Y")
+    T, each, dp, dw = _places(places, weights)
+    R, N = Y.shape
+    out = torch.empty((T, N), dtype=Y.dtype, device=Y.device) if out is None else out
+    _check(lib().moe_combine(_dtype_code(Y), T, each, R, N, *dy, dp, dw, _dev(out, Y.dtype, (T, N), "out"), _stream(stream)))
+    return out
+
+
+def moe_combine_backward(grad, Y, places, weights, row_offsets=None, out_Y=None, out_weights=None, stream=None):
+    """The gradients of moe_combine's Y and weights from that of its result, grad [tokens, N]: (grad_Y [rows, N], of Y's type, grad_weights
+    float32 [tokens, each]).  row_offsets: moe_dispatch's; the rows of grad_Y behind the last expert's are zeroed.  Without it rows that no place names are
+    zeros in a new tensor, and left as they were in out_Y."""
+    if _native is None:
+        lib()
+    done = _native.combine_backward(grad, Y, places, weights, row_offsets, out_Y, out_weights, stream)
+    if done is not None:
+        return _result(done)
+    import torch
+
+    _no_gradients(grad=grad, Y=Y, weights=weights, out_Y=out_Y, out_weights=out_weights)
+    _on_this_device(grad=grad, Y=Y, places=places, weights=weights, row_offsets=row_offsets, out_Y=out_Y, out_weights=out_weights)
+    dy = _rows(Y, "Y")
+    if weights is None:
+        raise ValueError("weights must be given: without them the gradient of a row is its token's")
+    T, each, dp, dw = _places(places, weights)
+    R, N = Y.shape
+    dg = _rows(grad, "grad", (Y.dtype,), (T, N))
+    if row_offsets is not None and (row_offsets.dim() != 1 or not row_offsets.shape[0]):
+        raise ValueError(f"row_offsets must be [experts + 1], got {tuple(row_offsets.shape)}")
+    used = None if row_offsets is None else ctypes.c_void_p(_dev(row_offsets, torch.int32, name="row_offsets").value + 4 * (row_offsets.shape[0] - 1))
+    if out_Y is None:
+        out_Y = (torch.zeros if used is None else torch.empty)((R, N), dtype=Y.dtype, device=Y.device)
+    out_weights = torch.empty((T, each), dtype=torch.float32, device=Y.device) if out_weights is None else out_weights
+    _check(lib().moe_combine_backward(_dtype_code(Y), T, each, R, N, *dg, *dy, dp, dw, used, _dev(out_Y, Y.dtype, (R, N), "out_Y"),
+                                      _dev(out_weights, torch.float32, (T, each), "out_weights"), _stream(stream)))
+    return out_Y, out_weights
+
+
 # ------------------------------------------------------------------------------ attention
 # (For inference: tensors that require a gradient are refused where torch would record one.)
-LQ_F16, LQ_BF16 = 0, 1
 _ROPE_SCALING = {None: 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
@@ -777,6 +971,40 @@ def kv4_attention(q, cache, block_table, context, scale=None, out=None, workspac
                                _dev(block_table, torch.int32, (B, block_table.shape[1]), "block_table"), block_table.shape[1],
                                _dev(context, torch.int32, (B,), "context"), D ** -0.5 if scale is None else scale,
                                _dev(out, q.dtype, q.shape, "out"), wsp, wsb, _stream(stream)))
+    return out
+
+
+def kv4_attention_chunks(q, cache, block_table, context, starts_q, scale=None, out=None, workspace=None, stream=None):
+    """Attention of new tokens over the cache that holds them already, packed sequences with any number of them each: q [tokens, heads,
+    head_dim], sequence s has those from starts_q[s] to starts_q[s + 1] - 1 (int32 [sequences + 1] on the GPU); cache, block_table and context as in
+    kv4_attention.  New token i of a sequence's n sees the first context - n + 1 + i.  scale: 1 / sqrt(head_dim) unless given.  Returns out, shaped as q;
+    rows that belong to no sequence are left as they were."""
+    if _native is None:
+        lib()
+    done = _native.chunks(q, cache, block_table, context, starts_q, scale, out, workspace, stream, _ws_cache)
+    if done is not None:
+        return _result(done)
+    import torch
+
+    _no_gradients(q=q, out=out)
+    _on_this_device(q=q, cache=cache, block_table=block_table, context=context, starts_q=starts_q, out=out, workspace=workspace)
+    pages, Hkv, page, D = _kv4_shape(cache)
+    dq, (T, Hq, _) = _heads(q, "q"), q.shape
+    if q.shape[2] != D:
+        raise ValueError(f"q must be [tokens, heads, {D}], got {tuple(q.shape)}")
+    if starts_q.dim() != 1 or starts_q.shape[0] < 1:
+        raise ValueError(f"starts_q must be [sequences + 1], got {tuple(starts_q.shape)}")
+    S = starts_q.shape[0] - 1
+    if block_table.dim() != 2:
+        raise ValueError(f"block_table must be [sequences, width], got {tuple(block_table.shape)}")
+    width = block_table.shape[1]
+    out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device) if out is None else out
+    need = int(lib().kv4_attention_chunks_workspace_size(S, T, Hq, Hkv, D, page, width))
+    wsp, wsb = _ws(workspace, device=q.device, stream=stream, need=need)
+    _check(lib().kv4_attention_chunks(_dtype_code(q), S, T, Hq, Hkv, D, *dq, _dev(starts_q, torch.int32, (S + 1,), "starts_q"),
+                                      _dev(cache, torch.uint8, name="cache"), pages, page, _dev(block_table, torch.int32, (S, width), "block_table"), width,
+                                      _dev(context, torch.int32, (S,), "context"), D ** -0.5 if scale is None else scale,
+                                      _dev(out, q.dtype, (T, Hq, D), "out"), wsp, wsb, _stream(stream)))
     return out
 
 

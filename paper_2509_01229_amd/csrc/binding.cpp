@@ -39,6 +39,16 @@ struct Attention {
     decltype(&attn_prompt) prompt;
 } attn{};
 
+struct Layer {
+    decltype(&kv4_attention_chunks_workspace_size) chunks_workspace_size;
+    decltype(&kv4_attention_chunks) chunks;
+    decltype(&w4a8_norm_quantize) norm;
+    decltype(&w4a8_swiglu_quantize) swiglu;
+    decltype(&moe_dispatch) dispatch;
+    decltype(&moe_combine) combine;
+    decltype(&moe_combine_backward) combine_backward;
+} layer{};
+
 // The GIL is given up for the allocation and the launch (both may wait), also where they throw.
 struct WithoutGil {
     PyThreadState *const state = PyEval_SaveThread();
@@ -228,6 +238,15 @@ bool heads_of(PyObject *o, const at::Tensor &like, std::initializer_list<int64_t
 int dtype_of(const at::Tensor &t) { return t.scalar_type() == at::kHalf ? LQ_F16 : LQ_BF16; }
 const float *floats(PyObject *o) { return o == Py_None ? nullptr : static_cast<const float *>(tensor(o).data_ptr()); }
 const int *ints(PyObject *o) { return static_cast<const int *>(tensor(o).data_ptr()); }
+
+// on the current device, whose stream the call goes to (the general path says so where it is another)
+bool here(const at::Tensor &t) { return t.device().index() == c10::hip::getCurrentHIPStream().device_index(); }
+bool all_here(PyObject *const *a, int n)
+{
+    for (int i = 0; i < n; ++i)
+        if (a[i] != Py_None && !here(tensor(a[i]))) return false;
+    return true;
+}
 
 // a contiguous tensor of `dims` dimensions
 bool plain_dims(PyObject *o, at::ScalarType type, int64_t dims)
@@ -469,6 +488,220 @@ PyObject *prompt(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// chunks(q, cache, block_table, context, starts_q, scale, out, workspace, stream, workspaces) -> out
+PyObject *chunks(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *stream;
+    Cache c;
+    double scale;
+    if (n != 10 || !heads(a[0], 3) || !cache_of(a[1], c)) Py_RETURN_NONE;
+    const at::Tensor &q = tensor(a[0]);
+    const int64_t T = q.size(0), Hq = q.size(1);
+    if (q.size(2) != c.dim || !plain_dims(a[4], at::kInt, 1) || tensor(a[4]).size(0) < 1) Py_RETURN_NONE;
+    const int64_t S = tensor(a[4]).size(0) - 1;
+    if (!plain_dims(a[2], at::kInt, 2) || tensor(a[2]).size(0) != S || !plain(a[3], at::kInt, {S}) || !scale_of(a[5], c.dim, scale) ||
+        (a[6] != Py_None && !plain(a[6], q.scalar_type(), {T, Hq, c.dim})) || wants_gradient(a[6]) || !here(q) || !all_here(a + 1, 4) || !all_here(a + 6, 1) ||
+        !stream_of(a[8], stream))
+        Py_RETURN_NONE;
+    const int width = (int)tensor(a[2]).size(1);
+    at::Tensor workspace;
+    if (!workspace_of(a[7], a[9], q, stream, layer.chunks_workspace_size((int)S, (int)T, (int)Hq, c.heads, c.dim, c.page, width), workspace)) {
+        if (PyErr_Occurred()) return nullptr;
+        Py_RETURN_NONE;
+    }
+    at::Tensor out = a[6] != Py_None ? tensor(a[6]) : at::Tensor();
+    int rc;
+    {
+        const WithoutGil released;
+        if (!out.defined()) out = at::empty({T, Hq, c.dim}, q.options());
+        rc = layer.chunks(dtype_of(q), (int)S, (int)T, (int)Hq, c.heads, c.dim, q.data_ptr(), q.stride(0), q.stride(1), ints(a[4]), c.p, c.pages, c.page,
+                          ints(a[2]), width, ints(a[3]), (float)scale, out.data_ptr(), workspace.defined() ? workspace.data_ptr() : nullptr,
+                          workspace.defined() ? (size_t)workspace.numel() : 0, stream);
+    }
+    if (rc != LQ_OK) return PyLong_FromLong(rc);
+    return wrapped(a[6], std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// ---------------------------------------------------- norm and gated activation, tokens sorted by expert and back
+// a matrix whose rows may have a stride of their own
+bool matrix(PyObject *o, at::ScalarType type)
+{
+    if (rows_of(o, type) < 0) return false;
+    const at::Tensor &t = tensor(o);
+    return t.size(1) > 1 && t.stride(1) == 1 && !wants_gradient(o) && here(t);
+}
+bool matrix_of(PyObject *o, const at::Tensor &like) { return matrix(o, like.scalar_type()) && tensor(o).sizes().equals(like.sizes()); }
+bool float16(PyObject *o) { return matrix(o, at::kHalf) || matrix(o, at::kBFloat16); }
+// None, or a contiguous tensor
+bool given(PyObject *o, at::ScalarType type, std::initializer_list<int64_t> shape) { return o == Py_None || (plain(o, type, shape) && !wants_gradient(o) && here(tensor(o))); }
+template <class T = void>
+T *pointer(PyObject *o) { return o == Py_None ? nullptr : static_cast<T *>(tensor(o).data_ptr()); }
+at::Tensor given_or_none(PyObject *o) { return o == Py_None ? at::Tensor() : tensor(o); }
+PyObject *tuple_of(std::initializer_list<PyObject *> items)  // (takes the references)
+{
+    bool whole = true;
+    for (PyObject *const o : items) whole = whole && o;
+    PyObject *const t = whole ? PyTuple_New((Py_ssize_t)items.size()) : nullptr;
+    Py_ssize_t i = 0;
+    for (PyObject *const o : items) {
+        if (t)
+            PyTuple_SET_ITEM(t, i++, o);
+        else
+            Py_XDECREF(o);
+    }
+    return t;
+}
+PyObject *none() { Py_RETURN_NONE; }
+
+// norm(x, weight, residual, eps, want_y, out_q, out_scales, out_h, out_y, stream) -> (X_i8, act_scales, h or None, y or None)
+PyObject *norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *stream;
+    if (n != 10 || !float16(a[0]) || !PyFloat_CheckExact(a[3]) || !PyBool_Check(a[4])) Py_RETURN_NONE;
+    const at::Tensor &x = tensor(a[0]);
+    const int64_t M = x.size(0), K = x.size(1);
+    const bool residual = a[2] != Py_None, want_y = a[4] == Py_True;
+    if (!given(a[1], at::kFloat, {K}) || (residual && !matrix_of(a[2], x)) || (!residual && a[7] != Py_None) || !given(a[5], at::kChar, {M, K}) ||
+        !given(a[6], at::kFloat, {M}) || !given(a[7], x.scalar_type(), {M, K}) || !given(a[8], x.scalar_type(), {M, K}) || !stream_of(a[9], stream))
+        Py_RETURN_NONE;
+    at::Tensor q = given_or_none(a[5]), s = given_or_none(a[6]), h = given_or_none(a[7]), y = given_or_none(a[8]);
+    int rc;
+    {
+        const WithoutGil released;
+        if (!q.defined()) q = at::empty({M, K}, x.options().dtype(at::kChar));
+        if (!s.defined()) s = at::empty({M}, x.options().dtype(at::kFloat));
+        if (residual && !h.defined()) h = at::empty({M, K}, x.options());
+        if (want_y && !y.defined()) y = at::empty({M, K}, x.options());
+        rc = layer.norm(dtype_of(x), (int)M, (int)K, x.data_ptr(), x.stride(0), pointer(a[2]), residual ? tensor(a[2]).stride(0) : 0, floats(a[1]),
+                        (float)PyFloat_AS_DOUBLE(a[3]), residual ? h.data_ptr() : nullptr, want_y ? y.data_ptr() : nullptr,
+                        static_cast<int8_t *>(q.data_ptr()), static_cast<float *>(s.data_ptr()), stream);
+    }
+    if (rc != LQ_OK) return PyLong_FromLong(rc);
+    return tuple_of({wrapped(a[5], std::move(q)), wrapped(a[6], std::move(s)), residual ? wrapped(a[7], std::move(h)) : none(),
+                     want_y ? wrapped(a[8], std::move(y)) : none()});
+    END_HANDLE_TH_ERRORS
+}
+
+// swiglu(x, out_q, out_scales, stream) -> (X_i8, act_scales)
+PyObject *swiglu(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *stream;
+    if (n != 4 || !float16(a[0]) || tensor(a[0]).size(1) % 2) Py_RETURN_NONE;
+    const at::Tensor &x = tensor(a[0]);
+    const int64_t M = x.size(0), K = x.size(1) / 2;
+    if (!given(a[1], at::kChar, {M, K}) || !given(a[2], at::kFloat, {M}) || !stream_of(a[3], stream)) Py_RETURN_NONE;
+    at::Tensor q = given_or_none(a[1]), s = given_or_none(a[2]);
+    int rc;
+    {
+        const WithoutGil released;
+        if (!q.defined()) q = at::empty({M, K}, x.options().dtype(at::kChar));
+        if (!s.defined()) s = at::empty({M}, x.options().dtype(at::kFloat));
+        rc = layer.swiglu(dtype_of(x), (int)M, (int)K, x.data_ptr(), x.stride(0), static_cast<int8_t *>(q.data_ptr()), static_cast<float *>(s.data_ptr()), stream);
+    }
+    if (rc != LQ_OK) return PyLong_FromLong(rc);
+    return pair(wrapped(a[1], std::move(q)), wrapped(a[2], std::move(s)));
+    END_HANDLE_TH_ERRORS
+}
+
+// dispatch(X, experts, n_experts, act_scales, out, out_scales, stream) -> (rows, row_scales or None, row_offsets, places)
+PyObject *dispatch(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *stream;
+    int n_experts;
+    if (n != 7 || !(matrix(a[0], at::kChar) || float16(a[0])) || !plain_dims(a[1], at::kInt, 2) || !here(tensor(a[1])) || !small_int(a[2], n_experts) ||
+        n_experts < 1 || n_experts > 256)
+        Py_RETURN_NONE;
+    const at::Tensor &x = tensor(a[0]);
+    const int64_t T = x.size(0), K = x.size(1), each = tensor(a[1]).size(1);
+    const bool scales = a[3] != Py_None;
+    if (tensor(a[1]).size(0) != T || each < 1 || T * each > INT_MAX || !given(a[3], at::kFloat, {T}) || !given(a[4], x.scalar_type(), {T * each, K}) ||
+        (!scales && a[5] != Py_None) || !given(a[5], at::kFloat, {T * each}) || !stream_of(a[6], stream))
+        Py_RETURN_NONE;
+    at::Tensor rows = given_or_none(a[4]), row_scales = given_or_none(a[5]), offsets, places;
+    int rc;
+    {
+        const WithoutGil released;
+        if (!rows.defined()) rows = at::empty({T * each, K}, x.options());
+        if (scales && !row_scales.defined()) row_scales = at::empty({T * each}, x.options().dtype(at::kFloat));
+        offsets = at::empty({n_experts + 1}, x.options().dtype(at::kInt));
+        places = at::empty({T, each}, x.options().dtype(at::kInt));
+        rc = layer.dispatch(x.scalar_type() == at::kChar ? LQ_I8 : dtype_of(x), (int)T, (int)each, n_experts, (int)K, x.data_ptr(), x.stride(0), floats(a[3]),
+                            ints(a[1]), rows.data_ptr(), scales ? static_cast<float *>(row_scales.data_ptr()) : nullptr,
+                            static_cast<int *>(offsets.data_ptr()), static_cast<int *>(places.data_ptr()), stream);
+    }
+    if (rc != LQ_OK) return PyLong_FromLong(rc);
+    return tuple_of({wrapped(a[4], std::move(rows)), scales ? wrapped(a[5], std::move(row_scales)) : none(), THPVariable_Wrap(std::move(offsets)),
+                     THPVariable_Wrap(std::move(places))});
+    END_HANDLE_TH_ERRORS
+}
+
+// combine(Y, places, weights, out, stream) -> out
+PyObject *combine(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *stream;
+    if (n != 5 || !float16(a[0]) || !plain_dims(a[1], at::kInt, 2) || !here(tensor(a[1]))) Py_RETURN_NONE;
+    const at::Tensor &y = tensor(a[0]);
+    const int64_t T = tensor(a[1]).size(0), each = tensor(a[1]).size(1), R = y.size(0), N = y.size(1);
+    if (!given(a[2], at::kFloat, {T, each}) || !given(a[3], y.scalar_type(), {T, N}) || !stream_of(a[4], stream)) Py_RETURN_NONE;
+    at::Tensor out = given_or_none(a[3]);
+    int rc;
+    {
+        const WithoutGil released;
+        if (!out.defined()) out = at::empty({T, N}, y.options());
+        rc = layer.combine(dtype_of(y), (int)T, (int)each, (int)R, (int)N, y.data_ptr(), y.stride(0), ints(a[1]), floats(a[2]), out.data_ptr(), stream);
+    }
+    if (rc != LQ_OK) return PyLong_FromLong(rc);
+    return wrapped(a[3], std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// combine_backward(grad, Y, places, weights, row_offsets, out_Y, out_weights, stream) -> (grad_Y, grad_weights)
+PyObject *combine_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *stream;
+    if (n != 8 || !float16(a[1]) || !matrix(a[0], tensor(a[1]).scalar_type()) || !plain_dims(a[2], at::kInt, 2) || !here(tensor(a[2]))) Py_RETURN_NONE;
+    const at::Tensor &grad = tensor(a[0]), &y = tensor(a[1]);
+    const int64_t T = tensor(a[2]).size(0), each = tensor(a[2]).size(1), R = y.size(0), N = y.size(1);
+    const bool used = a[4] != Py_None;
+    if (grad.size(0) != T || grad.size(1) != N || a[3] == Py_None || !given(a[3], at::kFloat, {T, each}) ||
+        (used && (!plain_dims(a[4], at::kInt, 1) || tensor(a[4]).size(0) < 1 || !here(tensor(a[4])))) || !given(a[5], y.scalar_type(), {R, N}) ||
+        !given(a[6], at::kFloat, {T, each}) || !stream_of(a[7], stream))
+        Py_RETURN_NONE;
+    at::Tensor out = given_or_none(a[5]), weights = given_or_none(a[6]);
+    if (!out.defined() && !used) Py_RETURN_NONE;  // (cleared on the current stream: the general path does it)
+    int rc;
+    {
+        const WithoutGil released;
+        if (!out.defined()) out = at::empty({R, N}, y.options());
+        if (!weights.defined()) weights = at::empty({T, each}, y.options().dtype(at::kFloat));
+        rc = layer.combine_backward(dtype_of(y), (int)T, (int)each, (int)R, (int)N, grad.data_ptr(), grad.stride(0), y.data_ptr(), y.stride(0), ints(a[2]),
+                                    floats(a[3]), used ? ints(a[4]) + tensor(a[4]).size(0) - 1 : nullptr, out.data_ptr(),
+                                    static_cast<float *>(weights.data_ptr()), stream);
+    }
+    if (rc != LQ_OK) return PyLong_FromLong(rc);
+    return pair(wrapped(a[5], std::move(out)), wrapped(a[6], std::move(weights)));
+    END_HANDLE_TH_ERRORS
+}
+
+// bind_layer(kv4_attention_chunks_workspace_size, kv4_attention_chunks, w4a8_norm_quantize, w4a8_swiglu_quantize, moe_dispatch, moe_combine,
+// moe_combine_backward): their addresses
+PyObject *bind_layer(PyObject *, PyObject *args)
+{
+    unsigned long long z, c, n, s, d, m, b;
+    if (!PyArg_ParseTuple(args, "KKKKKKK", &z, &c, &n, &s, &d, &m, &b)) return nullptr;
+    layer = Layer{reinterpret_cast<decltype(layer.chunks_workspace_size)>(z), reinterpret_cast<decltype(layer.chunks)>(c),
+                  reinterpret_cast<decltype(layer.norm)>(n), reinterpret_cast<decltype(layer.swiglu)>(s), reinterpret_cast<decltype(layer.dispatch)>(d),
+                  reinterpret_cast<decltype(layer.combine)>(m), reinterpret_cast<decltype(layer.combine_backward)>(b)};
+    Py_RETURN_NONE;
+}
+
 // bind_attention(attn_qk_norm_rope, kv4_write, kv4_append, kv4_read, kv4_attention_workspace_size, kv4_attention,
 // attn_prompt_workspace_size, attn_prompt): their addresses
 PyObject *bind_attention(PyObject *, PyObject *args)
@@ -503,7 +736,14 @@ PyMethodDef methods[] = {
     {"read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(read)), METH_FASTCALL, nullptr},
     {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(decode)), METH_FASTCALL, nullptr},
     {"prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(prompt)), METH_FASTCALL, nullptr},
+    {"chunks", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(chunks)), METH_FASTCALL, nullptr},
+    {"norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(norm)), METH_FASTCALL, nullptr},
+    {"swiglu", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(swiglu)), METH_FASTCALL, nullptr},
+    {"dispatch", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(dispatch)), METH_FASTCALL, nullptr},
+    {"combine", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(combine)), METH_FASTCALL, nullptr},
+    {"combine_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(combine_backward)), METH_FASTCALL, nullptr},
     {"bind", bind, METH_VARARGS, nullptr},
+    {"bind_layer", bind_layer, METH_VARARGS, nullptr},
     {"bind_attention", bind_attention, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

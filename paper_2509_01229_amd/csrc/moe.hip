@@ -1,0 +1,306 @@
+// Around the grouped product of a mixture of experts: tokens sorted by expert, their results brought back with weights, and the gradients of that.
+//
+// A pair p = token * k + j is a token and its j-th expert e_p.  Its row is
+//     place(p) = #{p' : e_p' < e_p} + #{p' < p : e_p' = e_p},    offsets(e) = #{p' : e_p' < e}
+// over the pairs whose expert is one of 0 .. E - 1 (other pairs have the place -1 and no row): sorted by expert, in the pairs' order.  Then
+//     rows[place(p)] = X[token],     out[t] = sum_j w[t][j] Y[place(t, j)],     dY[place(t, j)] = w[t][j] g[t],     dw[t][j] = g[t] . Y[place(t, j)]
+// (sums in FP32, in the order of j, or of the elements' pieces; no atomics).
+//
+// The places are counted, not sorted: a block for each expert looks at all pairs (ballots), first for the pairs before its own, then to
+// number its own.  Up to kFewPairs of them each token's block counts its own pairs' places itself and copies the row in the same launch.  All is bound by
+// memory, or by the launch where there are few tokens.
+#include <algorithm>
+
+#include "attn_common.h"
+
+namespace lqq {
+
+constexpr int kMostExperts = 256, kMostEach = 64, kFewPairs = 1024;
+
+struct DispatchArgs {
+    const char *x;
+    const float *scales;
+    const int *experts;
+    char *rows;
+    float *row_scales;
+    int *offsets, *places;
+    long long x_row;  // bytes
+    int tokens, each, n_experts, pieces;
+};
+
+__device__ __forceinline__ int lanes_set_below(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u)); }
+
+// The row of a token to its places
+__device__ __forceinline__ void copy_row(const DispatchArgs &a, int token, const int *places, int thread, int threads)
+{
+    const u32x4 *const from = reinterpret_cast<const u32x4 *>(a.x + token * a.x_row);
+    for (int i = thread; i < a.pieces; i += threads) {
+        const u32x4 x = from[i];
+        for (int j = 0; j < a.each; ++j) {
+            const int place = places[j];
+            if (place >= 0) reinterpret_cast<u32x4 *>(a.rows)[(size_t)place * a.pieces + i] = x;
+        }
+    }
+    if (a.scales && thread < a.each && places[thread] >= 0) a.row_scales[places[thread]] = a.scales[token];
+}
+
+// Few pairs: block t < tokens counts the places of its pairs and copies the row, the last block counts the experts' pairs
+constexpr int kSmallThreads = 256;
+__global__ __launch_bounds__(kSmallThreads) void moe_dispatch_small_kernel(const DispatchArgs a)
+{
+    __shared__ int s_places[kMostEach], s_count[kMostExperts];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), pairs = a.tokens * a.each, token = blockIdx.x;
+    constexpr int WAVES = kSmallThreads / 64;
+    if (token == a.tokens) {
+        for (int e = threadIdx.x; e < kMostExperts; e += kSmallThreads) s_count[e] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < pairs; i += kSmallThreads) {
+            const int e = a.experts[i];
+            if ((unsigned)e < (unsigned)a.n_experts) atomicAdd(&s_count[e], 1);
+        }
+        __syncthreads();
+        if (wave == 0) {
+            int before = 0;
+            for (int e0 = 0; e0 < a.n_experts; e0 += 64) {
+                const int n = e0 + lane < a.n_experts ? s_count[e0 + lane] : 0, upto = sums_up_to(n);
+                if (e0 + lane < a.n_experts) a.offsets[e0 + lane] = before + upto - n;
+                before += __builtin_amdgcn_readlane(upto, 63);
+            }
+            if (lane == 0) a.offsets[a.n_experts] = before;
+        }
+        return;
+    }
+    int ids[kFewPairs / 64];
+#pragma unroll
+    for (int i = 0; i < kFewPairs / 64; ++i) ids[i] = 64 * i + lane < pairs ? a.experts[64 * i + lane] : -1;
+    for (int j = wave; j < a.each; j += WAVES) {
+        const int p = token * a.each + j, e = a.experts[p];
+        int before = 0;
+#pragma unroll
+        for (int i = 0; i < kFewPairs / 64; ++i) {
+            const bool counts = ids[i] >= 0 && (ids[i] < e || (ids[i] == e && 64 * i + lane < p));
+            before += __popcll(__ballot(counts));
+        }
+        if (lane == 0) {
+            const int place = (unsigned)e < (unsigned)a.n_experts ? before : -1;
+            s_places[j] = place;
+            a.places[p] = place;
+        }
+    }
+    __syncthreads();
+    copy_row(a, token, s_places, threadIdx.x, kSmallThreads);
+}
+
+// Many pairs: block e numbers the pairs of expert e
+constexpr int kSortThreads = 1024;
+__global__ __launch_bounds__(kSortThreads) void moe_places_kernel(const DispatchArgs a)
+{
+    constexpr int WAVES = kSortThreads / 64;
+    __shared__ int s_less[WAVES], s_own[WAVES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), e = blockIdx.x, pairs = a.tokens * a.each;
+    // a wave takes consecutive pairs, 64 at a time
+    const int each = ((pairs + WAVES - 1) / WAVES + 63) / 64 * 64, from = (int)std::min<long long>((long long)wave * each, pairs), to = (int)std::min<long long>((long long)from + each, pairs);
+    int less = 0, own = 0;
+    for (int i = from; i < to; i += 64) {
+        const int id = i + lane < to ? a.experts[i + lane] : -1;
+        less += __popcll(__ballot(id >= 0 && id < e));
+        own += __popcll(__ballot(id == e));
+    }
+    if (lane == 0) s_less[wave] = less, s_own[wave] = own;
+    __syncthreads();
+    less = own = 0;
+    int place = 0;
+    for (int w = 0; w < WAVES; ++w) {
+        less += s_less[w];
+        if (w < wave) place += s_own[w];
+        own += s_own[w];
+    }
+    place += less;
+    if (threadIdx.x == 0) a.offsets[e] = less;
+    if (threadIdx.x == 0 && e == a.n_experts - 1) a.offsets[e + 1] = less + own;
+    for (int i = from; i < to; i += 64) {
+        const int id = i + lane < to ? a.experts[i + lane] : a.n_experts;
+        const uint64_t mine = __ballot(id == e);
+        if (id == e) a.places[i + lane] = place + lanes_set_below(mine);
+        if (e == 0 && (unsigned)id >= (unsigned)a.n_experts && i + lane < to) a.places[i + lane] = -1;
+        place += __popcll(mine);
+    }
+}
+constexpr int kCopyThreads = 256;
+__global__ __launch_bounds__(kCopyThreads) void moe_copy_kernel(const DispatchArgs a)
+{
+    copy_row(a, blockIdx.x, a.places + (long long)blockIdx.x * a.each, threadIdx.x, kCopyThreads);
+}
+
+struct CombineArgs {
+    const void *y, *grad;
+    const int *places, *used;
+    const float *weights;
+    void *out;
+    float *grad_weights;
+    long long y_row, grad_row;  // elements
+    int tokens, each, rows, pieces;
+};
+// 8 elements of row `place`
+template <class T>
+__device__ __forceinline__ vec<T, 8> piece_of(const CombineArgs &a, int place, int piece)
+{
+    return reinterpret_cast<const vec<T, 8> *>(static_cast<const T *>(a.y) + place * a.y_row)[piece];
+}
+
+constexpr int kCombineThreads = 256;
+template <class T>
+__global__ __launch_bounds__(kCombineThreads) void moe_combine_kernel(const CombineArgs a)
+{
+    const int chunks = (a.pieces + kCombineThreads - 1) / kCombineThreads, token = (int)(blockIdx.x / (unsigned)chunks);
+    const int piece = (int)(blockIdx.x % (unsigned)chunks) * kCombineThreads + (int)threadIdx.x;
+    if (piece >= a.pieces) return;
+    const int *const places = a.places + (long long)token * a.each;
+    const float *const weights = a.weights ? a.weights + (long long)token * a.each : nullptr;
+    float sum[8] = {};
+    for (int j = 0; j < a.each; ++j) {
+        const int place = places[j];
+        if ((unsigned)place >= (unsigned)a.rows) continue;
+        const float w = weights ? weights[j] : 1.0f;
+        const auto x = piece_of<T>(a, place, piece);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = __builtin_fmaf((float)x[e], w, sum[e]);
+    }
+    vec<T, 8> out;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] = (T)sum[e];
+    reinterpret_cast<vec<T, 8> *>(a.out)[(size_t)token * a.pieces + piece] = out;
+}
+
+// The gradients: a block takes a token; the blocks behind the tokens clear the rows that no expert has
+template <class T>
+__global__ __launch_bounds__(kCombineThreads) void moe_combine_backward_kernel(const CombineArgs a)
+{
+    constexpr int WAVES = kCombineThreads / 64;
+    __shared__ float s_dot[WAVES][kMostEach];
+    const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+    vec<T, 8> *const out = static_cast<vec<T, 8> *>(a.out);
+    if ((int)blockIdx.x >= a.tokens) {
+        const int used = min(max(*a.used, 0), a.rows);
+        for (long long i = (long long)used * a.pieces + (blockIdx.x - a.tokens) * kCombineThreads + threadIdx.x; i < (long long)a.rows * a.pieces;
+             i += (long long)(gridDim.x - a.tokens) * kCombineThreads)
+            out[i] = vec<T, 8>{};
+        return;
+    }
+    const int token = blockIdx.x;
+    const int *const places = a.places + (long long)token * a.each;
+    const float *const weights = a.weights + (long long)token * a.each;
+    const vec<T, 8> *const grad = reinterpret_cast<const vec<T, 8> *>(static_cast<const T *>(a.grad) + token * a.grad_row);
+    for (int j = 0; j < a.each; ++j) {
+        const int place = places[j];
+        float dot = 0.0f;
+        if ((unsigned)place < (unsigned)a.rows) {
+            const float w = weights[j];
+            for (int piece = threadIdx.x; piece < a.pieces; piece += kCombineThreads) {
+                const auto g = grad[piece], y = piece_of<T>(a, place, piece);
+                vec<T, 8> d;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    dot = __builtin_fmaf((float)g[e], (float)y[e], dot);
+                    d[e] = (T)((float)g[e] * w);
+                }
+                out[(size_t)place * a.pieces + piece] = d;
+            }
+        }
+        for (int d = 32; d; d >>= 1) dot += __shfl_xor(dot, d);
+        if (lane == 0) s_dot[wave][j] = dot;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < a.each) {
+        float dot = s_dot[0][threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) dot += s_dot[w][threadIdx.x];
+        a.grad_weights[(long long)token * a.each + threadIdx.x] = dot;
+    }
+}
+
+}  // namespace lqq
+
+using namespace lqq;
+
+namespace {
+constexpr int kMostBlocks = 1 << 23;  // (a launch holds fewer than 2^32 threads)
+int type_bytes(int type) { return type == LQ_I8 ? 1 : type == LQ_F16 || type == LQ_BF16 ? 2 : 0; }
+bool pairs_ok(int tokens, int each) { return tokens >= 0 && each >= 1 && each <= kMostEach && (long long)tokens * each < (1LL << 31) - kSortThreads; }
+}  // namespace
+
+extern "C" int moe_dispatch(int type, int tokens, int each, int n_experts, int K, const void *X, long long x_row, const float *act_scales,
+                            const int *experts, void *rows, float *row_scales, int *row_offsets, int *places, void *hip_stream)
+{
+    const int size = type_bytes(type);
+    if (!size) return fail(LQ_ERR_INVALID, "type must be LQ_F16, LQ_BF16 or LQ_I8, got %d", type);
+    if (!pairs_ok(tokens, each) || tokens > kMostBlocks - 1) return fail(LQ_ERR_INVALID, "bad shape: %d tokens of %d experts each (1 to %d; up to 2^23 tokens)", tokens, each, kMostEach);
+    if (n_experts < 1 || n_experts > kMostExperts) return fail(LQ_ERR_INVALID, "n_experts must be 1 to %d, got %d", kMostExperts, n_experts);
+    if (K < 1 || K > (1 << 24) || K * size % 16) return fail(LQ_ERR_INVALID, "bad shape: rows of %d elements (a multiple of 16 bytes)", K);
+    if (!row_offsets || (tokens && (!X || !experts || !rows || !places))) return fail(LQ_ERR_INVALID, "null pointer");
+    if (!act_scales != !row_scales && tokens) return fail(LQ_ERR_INVALID, "act_scales and row_scales go together");
+    if (((uintptr_t)X | (uintptr_t)rows) & 15) return fail(LQ_ERR_ALIGN, "X and rows must be 16-byte aligned");
+    if (((uintptr_t)act_scales | (uintptr_t)row_scales | (uintptr_t)experts | (uintptr_t)row_offsets | (uintptr_t)places) & 3)
+        return fail(LQ_ERR_ALIGN, "scales, experts, row_offsets and places must be 4-byte aligned");
+    if (tokens > 1 && x_row * size % 16) return fail(LQ_ERR_ALIGN, "the stride of X's rows must be a multiple of 16 bytes, got %lld elements", x_row);
+    const DispatchArgs a{static_cast<const char *>(X), act_scales, experts, static_cast<char *>(rows), row_scales, row_offsets, places,
+                         tokens > 1 ? x_row * size : 0, tokens, each, n_experts, K * size / 16};
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();
+    if (tokens * (long long)each <= kFewPairs) {
+        hipLaunchKernelGGL(moe_dispatch_small_kernel, dim3((unsigned)tokens + 1), dim3(kSmallThreads), 0, st, a);
+    } else {
+        hipLaunchKernelGGL(moe_places_kernel, dim3((unsigned)n_experts), dim3(kSortThreads), 0, st, a);
+        hipLaunchKernelGGL(moe_copy_kernel, dim3((unsigned)tokens), dim3(kCopyThreads), 0, st, a);
+    }
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? LQ_OK : fail(LQ_ERR_HIP, "dispatch launch failed: %s", hipGetErrorString(e));
+}
+
+static int combine_shape(int dtype, int tokens, int each, int rows, int N)
+{
+    if (dtype != LQ_F16 && dtype != LQ_BF16) return fail(LQ_ERR_INVALID, "dtype must be LQ_F16 or LQ_BF16, got %d", dtype);
+    if (!pairs_ok(tokens, each) || rows < 0) return fail(LQ_ERR_INVALID, "bad shape: %d tokens of %d rows each (1 to %d), %d rows", tokens, each, kMostEach, rows);
+    if (N < 1 || N > (1 << 24) || N % 8) return fail(LQ_ERR_INVALID, "bad shape: rows of %d elements (a multiple of 8)", N);
+    return LQ_OK;
+}
+
+extern "C" int moe_combine(int dtype, int tokens, int each, int rows, int N, const void *Y, long long y_row, const int *places, const float *weights,
+                           void *out, void *hip_stream)
+{
+    if (const int rc = combine_shape(dtype, tokens, each, rows, N); rc != LQ_OK) return rc;
+    const int pieces = N / 8;
+    const long long blocks = (long long)tokens * ((pieces + kCombineThreads - 1) / kCombineThreads);
+    if (blocks > kMostBlocks) return fail(LQ_ERR_INVALID, "too large: %d tokens of %d elements", tokens, N);
+    if (tokens == 0) return LQ_OK;
+    if ((rows && !Y) || !places || !out) return fail(LQ_ERR_INVALID, "null pointer");
+    if (((uintptr_t)Y | (uintptr_t)out) & 15) return fail(LQ_ERR_ALIGN, "Y and out must be 16-byte aligned");
+    if (((uintptr_t)places | (uintptr_t)weights) & 3) return fail(LQ_ERR_ALIGN, "places and weights must be 4-byte aligned");
+    if (rows > 1 && y_row % 8) return fail(LQ_ERR_ALIGN, "the stride of Y's rows must be a multiple of 8 elements, got %lld", y_row);
+    const CombineArgs a{Y, nullptr, places, nullptr, weights, out, nullptr, rows > 1 ? y_row : 0, 0, tokens, each, rows, pieces};
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(dtype == LQ_F16 ? moe_combine_kernel<f16> : moe_combine_kernel<bf16>, dim3((unsigned)blocks), dim3(kCombineThreads), 0,
+                       static_cast<hipStream_t>(hip_stream), a);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? LQ_OK : fail(LQ_ERR_HIP, "combine launch failed: %s", hipGetErrorString(e));
+}
+
+extern "C" int moe_combine_backward(int dtype, int tokens, int each, int rows, int N, const void *grad, long long grad_row, const void *Y, long long y_row,
+                                    const int *places, const float *weights, const int *rows_used, void *grad_Y, float *grad_weights, void *hip_stream)
+{
+    if (const int rc = combine_shape(dtype, tokens, each, rows, N); rc != LQ_OK) return rc;
+    if (tokens > kMostBlocks - 1024) return fail(LQ_ERR_INVALID, "too large: %d tokens", tokens);
+    if ((tokens && (!grad || !places || !weights || !grad_weights)) || (rows && (!Y || !grad_Y))) return fail(LQ_ERR_INVALID, "null pointer");
+    if (((uintptr_t)grad | (uintptr_t)Y | (uintptr_t)grad_Y) & 15) return fail(LQ_ERR_ALIGN, "grad, Y and grad_Y must be 16-byte aligned");
+    if (((uintptr_t)places | (uintptr_t)weights | (uintptr_t)rows_used | (uintptr_t)grad_weights) & 3)
+        return fail(LQ_ERR_ALIGN, "places, weights, rows_used and grad_weights must be 4-byte aligned");
+    if ((rows > 1 && y_row % 8) || (tokens > 1 && grad_row % 8)) return fail(LQ_ERR_ALIGN, "strides of rows must be multiples of 8 elements");
+    const int pieces = N / 8, clearing = rows_used && rows ? 256 : 0;
+    if (tokens + clearing == 0) return LQ_OK;
+    const CombineArgs a{Y, grad, places, rows_used, weights, grad_Y, grad_weights, rows > 1 ? y_row : 0, tokens > 1 ? grad_row : 0, tokens, each, rows, pieces};
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(dtype == LQ_F16 ? moe_combine_backward_kernel<f16> : moe_combine_backward_kernel<bf16>, dim3((unsigned)(tokens + clearing)),
+                       dim3(kCombineThreads), 0, static_cast<hipStream_t>(hip_stream), a);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? LQ_OK : fail(LQ_ERR_HIP, "gradient launch failed: %s", hipGetErrorString(e));
+}

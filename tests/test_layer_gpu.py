@@ -1,0 +1,413 @@
+"""The norm and the gated activation with INT8 outputs, tokens sorted by expert and back, against their definitions (oracle/layer_oracle.py).
+
+The norm's results and the gradients of the rows are determined bit for bit (single FP32 roundings after FP64 sums), and so are places and moved
+rows.  The gated activation's FP32 values are within d = (4 + |gate|) 2^-22 of themselves: its codes q and scale s hold
+|q s - y| <= s / 2 + d |y| + 2^-22 * 127 s (q s is compared in FP64; y / s and s are rounded), and s itself is within d + 2^-23 of max |y| / 127.  Sums of k
+FP32 products are within (k + 1) 2^-24 of the sum of their absolute values, and a result in its type is rounded once (u = 2^-11 in FP16, 2^-8 in BF16)."""
+import numpy as np
+import pytest
+
+from oracle import attention_oracle as A
+from oracle import layer_oracle as R
+from paper_2509_01229_amd import api
+
+pytestmark = pytest.mark.gpu
+TYPES = (A.F16, A.BF16)
+
+
+def _draw(rng, shape, dtype, size=1.0):
+    return A.round_to(rng.standard_normal(shape, dtype=np.float32) * np.float32(size), dtype)
+
+
+def _gpu(x, dtype=None):
+    import torch
+
+    t = torch.from_numpy(np.ascontiguousarray(x)).cuda()
+    return t.to(getattr(torch, dtype)) if dtype else t
+
+
+def _np(t):
+    return t.float().cpu().numpy()
+
+
+def _rows(x, dtype, stride=0):
+    """x on the GPU, its rows `stride` elements apart with NaN between."""
+    import torch
+
+    t = torch.full((x.shape[0], x.shape[1] + stride), float("nan"), dtype=getattr(torch, dtype), device="cuda")
+    t[:, :x.shape[1]] = _gpu(x, dtype)
+    return t[:, :x.shape[1]]
+
+
+# ------------------------------------------------------------------------------------------- norm
+SHAPES = [(1, 8), (1, 4096), (3, 520), (130, 2048), (67, 2056), (5, 4104), (600, 4096), (20, 5120), (33, 8200), (2, 16392), (3, 28672), (2, 32776), (1, 70008)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("M,K", SHAPES)
+def test_norm_is_exact(dtype, residual, M, K):
+    import torch
+
+    rng = np.random.default_rng(M + K)
+    x, w = _draw(rng, (M, K), dtype), (1 + 0.3 * rng.standard_normal(K)).astype(np.float32)
+    res = _draw(rng, (M, K), dtype, 3.0) * np.exp2(rng.integers(-3, 4, K)).astype(np.float32) if residual else None
+    res = A.round_to(res, dtype) if residual else None
+    if M > 2:
+        x[0] = 0
+        if residual:
+            res[0], res[1] = 0, -x[1]                # rows of zeros
+        x[2] = A.round_to(x[2] * np.float32(2.0 ** -20), dtype)  # (in FP16 subnormal numbers)
+    for weight, want_y, stride in ((w, True, 0), (None, False, 24)):
+        got = api.w4a8_norm_quantize(_rows(x, dtype, stride), None if weight is None else _gpu(weight), eps=1e-6, want_y=want_y,
+                                     residual=_rows(res, dtype, 2 * stride) if residual else None)
+        q, s, h, y = R.norm_quantise(x, res, weight, 1e-6, dtype)
+        assert got[0].dtype == torch.int8 and np.array_equal(got[1].cpu().numpy().view(np.uint32), s.view(np.uint32))
+        assert np.array_equal(got[0].cpu().numpy(), q)
+        assert (got[2] is None) == (not residual) and (got[3] is None) == (not want_y)
+        if residual:
+            assert np.array_equal(_np(got[2]), h)
+        if want_y:
+            assert np.array_equal(_np(got[3]), A.round_to(y, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("K", [1024, 8192, 40000])
+def test_norm_in_place(dtype, K):
+    """h in the place of the residual, or of x; outputs that are given."""
+    import torch
+
+    rng = np.random.default_rng(K)
+    x, res = _draw(rng, (9, K), dtype), _draw(rng, (9, K), dtype)
+    q, s, h, y = R.norm_quantise(x, res, None, 1e-5, dtype)
+    for name in ("residual", "x"):
+        t = {"x": _gpu(x, dtype), "residual": _gpu(res, dtype)}
+        out = {"out_q": torch.empty((9, K), dtype=torch.int8, device="cuda"), "out_scales": torch.empty(9, device="cuda"), "out_y": torch.empty_like(t["x"]), "out_h": t[name]}
+        got = api.w4a8_norm_quantize(t["x"], residual=t["residual"], eps=1e-5, **out)
+        assert [a is b for a, b in zip(got, (out["out_q"], out["out_scales"], out["out_h"], out["out_y"]))] == [True] * 4
+        assert np.array_equal(got[0].cpu().numpy(), q) and np.array_equal(got[1].cpu().numpy(), s)
+        assert np.array_equal(_np(got[2]), h) and np.array_equal(_np(got[3]), A.round_to(y, dtype))
+
+
+def test_norm_of_numbers_near_the_ends():
+    """Squares that overflow FP32 and ones that vanish in it; a row that is not finite spoils no other."""
+    import torch
+
+    rng = np.random.default_rng(4)
+    K = 512
+    x = np.stack([_draw(rng, K, A.BF16, 1.0) * np.float32(f) for f in (2.0 ** 120, 2.0 ** 64, 2.0 ** -70, 2.0 ** -120, 1.0, 1.0)])
+    x = A.round_to(x, A.BF16)
+    q, s, _, y = R.norm_quantise(x, None, None, 1e-30, A.BF16)
+    got = api.w4a8_norm_quantize(_gpu(x, A.BF16), eps=1e-30, want_y=True)
+    assert np.array_equal(got[0].cpu().numpy(), q) and np.array_equal(got[1].cpu().numpy(), s) and np.array_equal(_np(got[3]), A.round_to(y, A.BF16))
+    for bad in (np.nan, np.inf):
+        x[4, 77] = bad
+        again = api.w4a8_norm_quantize(_gpu(x, A.BF16), eps=1e-30, want_y=True)
+        keep = [0, 1, 2, 3, 5]
+        for a, b in zip(again, got):
+            assert a is None or torch.equal(a[keep], b[keep])
+
+
+# ------------------------------------------------------------------------------- gated activation
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K", [(1, 8), (1, 1536), (7, 2056), (65, 4096), (3, 6912), (300, 11008), (2, 14336), (3, 28672), (2, 32776), (1, 65544)])
+def test_swiglu(dtype, M, K):
+    rng = np.random.default_rng(M + K)
+    x = _draw(rng, (M, 2 * K), dtype, 2.0)
+    x[0, :K] = A.round_to(np.linspace(-16, 16, K), dtype)
+    if M > 2:
+        x[1] = 0
+        x[2, K:] = 0
+    for stride in (0, 40):
+        q, s = (t.cpu().numpy().astype(np.float64) for t in api.w4a8_swiglu_quantize(_rows(x, dtype, stride)))
+        y = R.gated(x)
+        d = (4 + np.abs(x[:, :K].astype(np.float64))) * 2.0 ** -22
+        most = np.abs(y).max(-1)
+        assert (s[most == 0] == 1).all()
+        assert (np.abs(s * 127 - most) <= (d * np.abs(y)).max(-1) + 2.0 ** -23 * most)[most > 0].all()
+        assert (np.abs(q * s[:, None] - y) <= s[:, None] * (0.5 + 127 * 2.0 ** -22) + d * np.abs(y)).all()
+        assert (np.abs(q).max(-1)[most > 0] == 127).all()
+
+
+def test_swiglu_of_large_gates():
+    """Gates whose exponential is infinite or vanishes: zero, and the gate itself."""
+    x = np.zeros((2, 32), dtype=np.float32)
+    x[0, :16], x[0, 16:] = [-60000, -200, -100, -89, 100, 200, 500, 1000] * 2, 1
+    x[1, :16], x[1, 16:] = [-88.5, -50, 30, 88, 89, -30, 0, 40] * 2, 2
+    q, s = (t.cpu().numpy().astype(np.float64) for t in api.w4a8_swiglu_quantize(_gpu(x, A.F16)))
+    x = A.round_to(x, A.F16)
+    y = R.gated(x)
+    assert np.isfinite(s).all() and (np.abs(q * s[:, None] - y) <= s[:, None] * 0.50001 + (4 + np.abs(x[:, :16])) * 2.0 ** -22 * np.abs(y)).all()
+
+
+# ------------------------------------------------------------------------- tokens sorted by expert
+ROUTES = [
+    # tokens, experts a token, experts
+    (1, 1, 1), (1, 2, 8), (16, 2, 8), (37, 8, 64), (512, 2, 8), (513, 2, 8), (128, 8, 256), (1000, 3, 5), (4099, 1, 17), (700, 64, 200), (2500, 8, 128),
+]
+
+
+def _route(rng, T, each, E, style):
+    if style == "same":
+        return np.full((T, each), E // 2, dtype=np.int32)
+    ids = rng.integers(0, E, (T, each)).astype(np.int32)
+    if style == "skewed":
+        ids = np.minimum(ids, rng.integers(0, E, (T, each))).astype(np.int32)
+    if style == "absent":
+        ids = np.where(rng.random((T, each)) < 0.4, rng.choice([-1, -2 ** 31, E, 2 ** 31 - 1], (T, each)), ids).astype(np.int32)
+    if style == "nobody":
+        ids[:] = -1
+    return ids
+
+
+@pytest.mark.parametrize("style", ["skewed", "same", "absent", "nobody"])
+@pytest.mark.parametrize("T,each,E", ROUTES)
+def test_dispatch(T, each, E, style):
+    import torch
+
+    rng = np.random.default_rng(T + E)
+    ids = _route(rng, T, each, E, style)
+    offsets, places, tokens = R.dispatch(ids, E)
+    for dtype, K, stride in ((torch.int8, 48, 16), (torch.float16, 2056, 0), (torch.bfloat16, 8, 8)):
+        if T * each > 8192 and K > 1000:
+            K = 264
+        x = _gpu(rng.integers(-127, 128, (T, K + stride)).astype(np.int8)).to(dtype)[:, :K]
+        scales = _gpu(rng.random(T).astype(np.float32)) if dtype == torch.int8 else None
+        out = torch.full((T * each, K), 99, dtype=dtype, device="cuda")
+        out_scales = torch.full((T * each,), -1.0, device="cuda") if scales is not None else None
+        got = api.moe_dispatch(x, _gpu(ids), E, act_scales=scales, out=out, out_scales=out_scales)
+        assert got[0] is out and got[1] is out_scales
+        assert got[2].dtype == got[3].dtype == torch.int32 and np.array_equal(got[2].cpu().numpy(), offsets) and np.array_equal(got[3].cpu().numpy(), places)
+        n, source = len(tokens), _gpu(tokens)
+        assert torch.equal(out[:n], x[source]) and (out[n:] == 99).all()
+        if scales is not None:
+            assert torch.equal(out_scales[:n], scales[source]) and (out_scales[n:] == -1).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,each,E,N", [(1, 1, 4, 8), (16, 2, 8, 4096), (37, 8, 64, 2056), (300, 3, 7, 1032), (2, 64, 200, 24), (513, 6, 60, 264)])
+@pytest.mark.parametrize("style", ["skewed", "absent"])
+def test_combine_and_its_gradients(dtype, T, each, E, N, style):
+    import torch
+
+    rng = np.random.default_rng(T + N)
+    offsets, places, tokens = R.dispatch(_route(rng, T, each, E, style), E)
+    rows, u = T * each, A.UNIT[dtype]
+    Y, grad, w = _draw(rng, (rows, N), dtype), _draw(rng, (T, N), dtype), rng.random((T, each)).astype(np.float32)
+    Y[len(tokens):] = np.nan                             # (rows that no pair has are not looked at)
+    w[places < 0] = np.nan
+    dY, dg, dp = _rows(Y, dtype, 16), _rows(grad, dtype, 8), _gpu(places)
+    for weights in (w, None):
+        got = _np(api.moe_combine(dY, dp, None if weights is None else _gpu(weights)))
+        want, size = R.combine(Y, places, weights)
+        assert (np.abs(got - want) <= u * np.abs(want) * 1.001 + (each + 1) * 2.0 ** -24 * size + 2.0 ** -25).all()
+    of_rows, of_weights, size = R.combine_backward(grad, Y, places, w, dtype)
+    for row_offsets in (_gpu(offsets), None):
+        out = torch.full((rows, N), 7.0, dtype=dY.dtype, device="cuda")
+        for given in ({}, {"out_Y": out, "out_weights": torch.empty((T, each), device="cuda")}):
+            gY, gw = api.moe_combine_backward(dg, dY, dp, _gpu(w), row_offsets=row_offsets, **given)
+            assert not given or (gY is out and gw is given["out_weights"])
+            assert np.array_equal(_np(gY)[:len(tokens)], of_rows[:len(tokens)])
+            assert (gY[len(tokens):] == (7.0 if given and row_offsets is None else 0.0)).all()
+            assert gw.dtype == torch.float32 and (np.abs(gw.double().cpu().numpy() - of_weights) <= (N / 256 + 16) * 2.0 ** -24 * size).all()
+
+
+def test_gradients_against_differences():
+    """moe_combine_backward, and moe_combine as the gradient of moe_dispatch, against differences of what they are the gradients of.  The functions are
+    linear in each of their arguments, and the differences are taken of results that are exact: small whole numbers."""
+    import torch
+
+    rng = np.random.default_rng(8)
+    T, each, E, N = 6, 3, 5, 16
+    ids = _route(rng, T, each, E, "absent")
+    offsets, places, tokens = R.dispatch(ids, E)
+    whole = lambda *shape: rng.integers(-4, 5, shape).astype(np.float32)  # noqa: E731
+    Y, w, grad, X = whole(T * each, N), whole(T, each), whole(T, N), whole(T, N)
+    dp = _gpu(places)
+    forward = lambda Y, w: (_np(api.moe_combine(_gpu(Y, A.F16), dp, _gpu(w))).astype(np.float64) * grad).sum()  # noqa: E731
+    gY, gw = (_np(t) for t in api.moe_combine_backward(_gpu(grad, A.F16), _gpu(Y, A.F16), dp, _gpu(w), row_offsets=_gpu(offsets)))
+    base = forward(Y, w)
+    for _ in range(25):
+        r, n, t, j = rng.integers(T * each), rng.integers(N), rng.integers(T), rng.integers(each)
+        Y2, w2 = Y.copy(), w.copy()
+        Y2[r, n] += 1
+        w2[t, j] += 1
+        assert forward(Y2, w) - base == gY[r, n] and forward(Y, w2) - base == gw[t, j]
+    rows_grad = whole(T * each, N)
+    out = lambda X: api.moe_dispatch(_gpu(X, A.F16), _gpu(ids), E, out=torch.zeros((T * each, N), dtype=torch.float16, device="cuda"))[0]  # noqa: E731
+    of = lambda X: (_np(out(X)).astype(np.float64) * rows_grad).sum()  # noqa: E731
+    gX, base = _np(api.moe_combine(_gpu(rows_grad, A.F16), dp)), of(X)
+    for _ in range(25):
+        t, n = rng.integers(T), rng.integers(N)
+        X2 = X.copy()
+        X2[t, n] += 1
+        assert of(X2) - base == gX[t, n]
+
+
+def test_places_outside_the_rows_and_the_same_row_twice():
+    """Places that moe_dispatch does not give: outside the rows they add nothing, a row may count twice."""
+    rng = np.random.default_rng(9)
+    Y, w = _draw(rng, (5, 64), A.F16), rng.random((4, 3)).astype(np.float32)
+    places = np.array([[0, 0, 4], [5, 2 ** 31 - 1, -2 ** 31], [-1, 3, 3], [1, 2, -7]], dtype=np.int32)
+    got = _np(api.moe_combine(_gpu(Y, A.F16), _gpu(places), _gpu(w)))
+    want, size = R.combine(Y, places, w)
+    assert (np.abs(got - want) <= 1.001 * 2.0 ** -11 * np.abs(want) + 4 * 2.0 ** -24 * size + 2.0 ** -25).all() and (got[1] == 0).all()
+    assert (api.moe_combine(_gpu(Y[:0], A.F16), _gpu(places), _gpu(w)) == 0).all()
+
+
+# -------------------------------------------------------------------------- streams, graphs, refusals
+def test_a_graph_follows_its_inputs():
+    """All of them captured together, small and large, and replayed with other inputs between the replays; and on a stream given as a number."""
+    import torch
+
+    rng = np.random.default_rng(10)
+    for T in (20, 900):
+        K, E, each = 512, 8, 2
+        x, res, grad = (torch.empty((T, K), dtype=torch.float16, device="cuda") for _ in range(3))
+        ids, w = torch.zeros((T, each), dtype=torch.int32, device="cuda"), torch.empty((T, each), device="cuda")
+        rows = torch.zeros((T * each, K), dtype=torch.int8, device="cuda")
+        row_scales = torch.zeros(T * each, device="cuda")
+
+        def feed(i):
+            for t in (x, res, grad):
+                t.copy_(_gpu(_draw(rng, (T, K), A.F16)))
+            ids.copy_(_gpu(_route(rng, T, each, E, ("skewed", "absent", "same")[i % 3])))
+            w.copy_(_gpu(rng.random((T, each)).astype(np.float32)))
+
+        def step():
+            q, s, h, y = api.w4a8_norm_quantize(x, residual=res, want_y=True)
+            _, _, offsets, places = api.moe_dispatch(q, ids, E, act_scales=s, out=rows, out_scales=row_scales)
+            q2, s2 = api.w4a8_swiglu_quantize(y)
+            Y = y[:, None].expand(T, each, K).reshape(T * each, K)
+            out = api.moe_combine(Y, places, w)
+            return [q, s, h, y, offsets, places, q2, s2, out, *api.moe_combine_backward(grad, Y, places, w, row_offsets=offsets)]
+
+        feed(0)
+        step()
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            captured = step()
+        for i in range(4):
+            feed(i)
+            torch.randn(1 << 20, device="cuda").sum().item()
+            for t in captured:
+                t.fill_(3)
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [t.clone() for t in captured]
+            kept = rows.clone(), row_scales.clone()
+            want = step()
+            n = int(want[4][-1])
+            for a, b in zip(got, want):
+                assert torch.equal(a, b)
+            assert torch.equal(kept[0][:n], rows[:n]) and torch.equal(kept[1][:n], row_scales[:n])
+        other = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        q, s, h, y = api.w4a8_norm_quantize(x, residual=res, want_y=True, stream=other.cuda_stream)
+        torch.cuda.synchronize()
+        assert torch.equal(q, want[0]) and torch.equal(s, want[1]) and torch.equal(h, want[2]) and torch.equal(y, want[3])
+
+
+def test_refusals():
+    import torch
+
+    x, ids, w = torch.zeros((4, 64), dtype=torch.float16, device="cuda"), torch.zeros((4, 2), dtype=torch.int32, device="cuda"), torch.zeros((4, 2), device="cuda")
+    q8, s8, odd = x.to(torch.int8), torch.ones(4, device="cuda"), torch.zeros(4 * 64 + 1, dtype=torch.float16, device="cuda")[1:].view(4, 64)
+    Y = torch.zeros((8, 64), dtype=torch.float16, device="cuda")
+    offsets = torch.zeros(3, dtype=torch.int32, device="cuda")
+    weight = torch.ones(64, device="cuda")
+    norm, back = api.w4a8_norm_quantize, lambda **a: api.moe_combine_backward(*(a.get(n, d) for n, d in zip(("grad", "Y", "places", "weights"), (x, Y, ids, w))),
+                                                                              **{n: v for n, v in a.items() if n not in ("grad", "Y", "places", "weights")})
+    norm(x, weight), api.w4a8_swiglu_quantize(x), api.moe_dispatch(q8, ids, 2, act_scales=s8), api.moe_combine(Y, ids, w), back(row_offsets=offsets)
+    E = api.LiquidGemmError
+    for bad, error in [
+            (lambda: norm(x.float()), TypeError), (lambda: norm(x[0]), ValueError), (lambda: norm(x.t()), ValueError), (lambda: norm(x, weight.half()), TypeError),
+            (lambda: norm(x, weight[:32]), ValueError), (lambda: norm(x, residual=x.bfloat16()), TypeError), (lambda: norm(x, residual=x[:3]), ValueError),
+            (lambda: norm(x, eps=0.0), E), (lambda: norm(x, eps=float("nan")), E), (lambda: norm(x, out_h=x), ValueError), (lambda: norm(x, out_y=Y), ValueError),
+            (lambda: norm(x, residual=x, out_h=Y[::2]), ValueError), (lambda: norm(x[:, :60]), E), (lambda: norm(odd), E), (lambda: norm(x, out_q=q8[:3]), ValueError),
+            (lambda: norm(torch.zeros((4, 68), dtype=torch.float16, device="cuda")[:, :64]), E), (lambda: norm(x, out_scales=s8.double()), TypeError),
+            (lambda: api.w4a8_swiglu_quantize(x.float()), TypeError), (lambda: api.w4a8_swiglu_quantize(x[:, :24]), E), (lambda: api.w4a8_swiglu_quantize(x[:, :33]), ValueError),
+            (lambda: api.w4a8_swiglu_quantize(odd), E), (lambda: api.w4a8_swiglu_quantize(x, out_q=q8), ValueError),
+            (lambda: api.moe_dispatch(x.float(), ids, 2), TypeError), (lambda: api.moe_dispatch(x, ids.long(), 2), TypeError), (lambda: api.moe_dispatch(x, ids[:3], 2), ValueError),
+            (lambda: api.moe_dispatch(x, ids[:, 0], 2), ValueError), (lambda: api.moe_dispatch(x, ids, 0), ValueError), (lambda: api.moe_dispatch(x, ids, 257), ValueError),
+            (lambda: api.moe_dispatch(x, ids[:, :0], 2), E), (lambda: api.moe_dispatch(q8[:, :24].contiguous(), ids, 2), E), (lambda: api.moe_dispatch(x, ids, 2, out=Y[:7]), ValueError),
+            (lambda: api.moe_dispatch(x, ids, 2, out_scales=torch.zeros(8, device="cuda")), ValueError), (lambda: api.moe_dispatch(q8, ids, 2, act_scales=s8[:3]), ValueError),
+            (lambda: api.moe_dispatch(x, ids.repeat(1, 33).contiguous(), 2), E), (lambda: api.moe_dispatch(x, ids.repeat(1, 2)[:, ::2], 2), ValueError),
+            (lambda: api.moe_combine(Y.float(), ids, w), TypeError), (lambda: api.moe_combine(Y, ids.long(), w), TypeError), (lambda: api.moe_combine(Y, ids, w[:, :1]), ValueError),
+            (lambda: api.moe_combine(Y, ids[0], w), ValueError), (lambda: api.moe_combine(Y[:, :12], ids, w), E), (lambda: api.moe_combine(Y, ids, w, out=Y), ValueError),
+            (lambda: back(grad=x[:3]), ValueError), (lambda: back(grad=x.bfloat16()), TypeError), (lambda: back(weights=None), ValueError), (lambda: back(row_offsets=offsets.long()), TypeError),
+            (lambda: back(row_offsets=offsets[:0]), ValueError), (lambda: back(out_Y=Y[:, :32]), ValueError), (lambda: back(out_weights=w.half()), TypeError)]:
+        with pytest.raises(error):
+            bad()
+    # nothing to do
+    assert norm(x[:0])[0].shape == (0, 64) and api.w4a8_swiglu_quantize(x[:0])[0].shape == (0, 32)
+    rows, _, offsets, places = api.moe_dispatch(x[:0], ids[:0], 2)
+    assert rows.shape == (0, 64) and places.shape == (0, 2) and offsets.tolist() == [0, 0, 0]
+    assert api.moe_combine(Y, ids[:0], w[:0]).shape == (0, 64)
+    gY, gw = back(grad=x[:0], places=ids[:0], weights=w[:0], row_offsets=offsets)
+    assert (gY == 0).all() and gw.shape == (0, 2)
+
+
+def test_what_asks_for_a_gradient_is_refused():
+    import torch
+
+    x, Y = torch.randn((4, 64), device="cuda").half(), torch.randn((8, 64), device="cuda").half()
+    ids, w, weight = torch.tensor([[0, 1]] * 4, dtype=torch.int32, device="cuda"), torch.rand((4, 2), device="cuda"), torch.rand(64, device="cuda")
+    made = {"x": x, "residual": x.clone(), "weight": weight, "X": x, "Y": Y, "weights": w, "grad": x}
+    for names, call in [(("x", "weight", "residual"), lambda x, weight, residual: api.w4a8_norm_quantize(x, weight, residual)), (("x",), api.w4a8_swiglu_quantize),
+                        (("X",), lambda X: api.moe_dispatch(X, ids, 2)), (("Y", "weights"), lambda Y, weights: api.moe_combine(Y, ids, weights)),
+                        (("grad", "Y", "weights"), lambda grad, Y, weights: api.moe_combine_backward(grad, Y, ids, weights))]:
+        call(*(made[n] for n in names))
+        for name in names:
+            args = [made[n].clone().requires_grad_() if n == name else made[n] for n in names]
+            with pytest.raises(ValueError, match=name):
+                call(*args)
+            with torch.no_grad():
+                call(*args)
+            with torch.inference_mode():
+                call(*args)
+
+
+def test_through_the_native_module_and_without(monkeypatch):
+    """The native module answers the plain calls, and with the same bytes as the path behind it."""
+    import torch
+
+    api.lib()
+    native = api._native
+    x, ids, w = torch.randn((40, 256), device="cuda").half(), torch.randint(-1, 5, (40, 2), device="cuda").int(), torch.rand((40, 2), device="cuda")
+    wide, weight, Y = torch.randn((40, 528), device="cuda").bfloat16()[:, :512], torch.rand(256, device="cuda"), torch.randn((80, 256), device="cuda").half()
+    q8, s8 = api.w4a8_swiglu_quantize(wide)
+    kept = torch.zeros((80, 256), dtype=torch.int8, device="cuda"), torch.zeros(80, device="cuda")
+    places, offsets = api.moe_dispatch(x, ids, 4)[3], api.moe_dispatch(x, ids, 4)[2]
+    now = torch.cuda.current_stream().cuda_stream
+    calls = [lambda: api.w4a8_norm_quantize(x, weight, residual=x, want_y=True), lambda: api.w4a8_norm_quantize(wide, eps=1e-5, stream=now),
+             lambda: api.w4a8_swiglu_quantize(wide), lambda: api.moe_dispatch(q8, ids, 4, act_scales=s8, out=kept[0], out_scales=kept[1]),
+             lambda: api.moe_combine(Y, places, w), lambda: api.moe_combine(Y, places), lambda: api.moe_combine_backward(x, Y, places, w, row_offsets=offsets)]
+    for call in calls:
+        answers = []
+
+        class Watched:
+            def __getattr__(self, name):
+                def run(*a):
+                    answers.append(getattr(native, name)(*a))
+                    return answers[-1]
+                return run
+
+        class Nothing:
+            def __getattr__(self, name):
+                return lambda *a: None
+
+        monkeypatch.setattr(api, "_native", Watched())
+        fast = call()
+        assert len(answers) == 1 and answers[0] is not None
+        fast = [t if t is None else t.clone() for t in (fast if isinstance(fast, tuple) else (fast,))]
+        monkeypatch.setattr(api, "_native", Nothing())
+        general = call()
+        general = general if isinstance(general, tuple) else (general,)
+        monkeypatch.setattr(api, "_native", native)
+        assert len(fast) == len(general)
+        for f, g in zip(fast, general):
+            assert (f is None) == (g is None)
+            if f is not None:
+                assert f.dtype == g.dtype and f.shape == g.shape and torch.equal(f.view(torch.uint8), g.view(torch.uint8))
