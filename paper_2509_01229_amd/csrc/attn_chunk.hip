@@ -33,102 +33,125 @@ struct ChunkArgs {
     void *out;
     unsigned *tickets;
     float *parts;
-    int n_seqs, total_q, Hq, Hkv, group, width, pages, lg_page, tiles, splits;
+    int n_seqs, total_q, Hq, Hkv, group, width, pages, lg_page, tiles, slots;
     float scale_log2;
 };
 
-constexpr int kFew = 64, kKeys = 64;
+constexpr int kFew = 64, kKeys = 64, kWaves = 4, kRows = 32 * kWaves, kMostParts = 32;
 constexpr float kWeightBits = 6.0f;
 typedef f16 f16x2v __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ v16f mfma32(vec<f16, 8> a, vec<f16, 8> b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
-// 8 nibbles of a dword as 4 pairs of integers in FP16, pair r = nibbles r and r + 4, less the pair of zero points z (1024 more of each): a nibble
-// under the exponent of 1024 is 1024 + code, one four bits up 1024 + 16 code.
-__device__ __forceinline__ void unpack8(uint32_t w, f16x2v z, f16x2v z64, uint32_t (&o)[4])
+// 8 nibbles of a dword as 4 pairs of FP16 numbers: pair r = nibbles r and r + 4, which as subnormal numbers are 2^-24 of the code (r even) or
+// 2^-20 of it (r odd)
+__device__ __forceinline__ u32x4 halves8(uint32_t w)
 {
     const uint32_t w8 = w >> 8;
-    const f16x2v sixteenth = {(f16)0.0625f, (f16)0.0625f};
+    return u32x4{w & 0x000f000fu, w & 0x00f000f0u, w8 & 0x000f000fu, w8 & 0x00f000f0u};
+}
+// the same with the zero points of both halves taken off: exact, subnormal numbers all of them
+__device__ __forceinline__ u32x4 halves8(uint32_t w, uint32_t zz)
+{
+    const u32x4 x = halves8(w);
+    u32x4 o;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const uint32_t x = (r < 2 ? w : w8);
-        if (r & 1)
-            o[r] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2v, (x & 0x00f000f0u) | 0x64006400u), sixteenth, -z64));
-        else
-            o[r] = __builtin_bit_cast(uint32_t, (f16x2v)(__builtin_bit_cast(f16x2v, (x & 0x000f000fu) | 0x64006400u) - z));
+        const uint32_t code = x[r], zero = r & 1 ? zz << 4 : zz;
+        o[r] = __builtin_bit_cast(uint32_t, (f16x2v)(__builtin_bit_cast(f16x2v, code) - __builtin_bit_cast(f16x2v, zero)));
     }
-}
-// 1024 + z and 64 + z of two words' zero points
-__device__ __forceinline__ void zeros_of(uint32_t a, uint32_t b, f16x2v &z, f16x2v &z64)
-{
-    const uint32_t zz = (__builtin_amdgcn_perm(b, a, 0x0c040c00u) & 0x000f000fu);
-    z = __builtin_bit_cast(f16x2v, zz | 0x64006400u);
-    z64 = z - f16x2v{(f16)960.0f, (f16)960.0f};
+    return o;
 }
 
-// A wave's share of a tile's codes: 16 keys, or their values, or both; all from one page
-template <int D>
-struct Codes {
-    uint32_t c[D / 32];
-    u32x4 w;  // words: of the lane's key (the first), or of the lane's four tokens
-};
 typedef __amdgpu_buffer_rsrc_t buf_t;
-template <int D>
-__device__ __forceinline__ void load_codes(Codes<D> &x, buf_t head, int P, int j, int lane, bool value)
-{
-    const int at = (value ? P * (D / 2) : 0) + j * (D / 2);
-    if constexpr (D == 128) {
-        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(head, lane * 16, at, 0);
-        x.c[0] = v[0], x.c[1] = v[1], x.c[2] = v[2], x.c[3] = v[3];
-    } else {
-        const auto v = __builtin_amdgcn_raw_buffer_load_b64(head, lane * 8, at, 0);
-        x.c[0] = v[0], x.c[1] = v[1];
+template <int N>
+struct Dwords {
+    uint32_t x[N];
+    __device__ __forceinline__ void load(buf_t b, int lane_offset, int offset)
+    {
+        if constexpr (N == 4) {
+            const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, lane_offset, offset, 0);
+            x[0] = v[0], x[1] = v[1], x[2] = v[2], x[3] = v[3];
+        } else if constexpr (N == 2) {
+            const auto v = __builtin_amdgcn_raw_buffer_load_b64(b, lane_offset, offset, 0);
+            x[0] = v[0], x[1] = v[1];
+        } else {
+            x[0] = __builtin_amdgcn_raw_buffer_load_b32(b, lane_offset, offset, 0);
+        }
     }
-    if (value)
-        x.w = __builtin_amdgcn_raw_buffer_load_b128(head, 16 * (lane >> 4), P * (D + 4) + 4 * j, 0);
-    else
-        x.w[0] = __builtin_amdgcn_raw_buffer_load_b32(head, 4 * (lane >> 2), P * D + 4 * j, 0);
-}
+};
 // (not __syncthreads(): codes stay in flight)
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ int up(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1) / (unsigned)b); }
 
-template <int D, class T, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void kv4_chunks_kernel(const ChunkArgs a)
+template <int D, class T>
+__global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkArgs a)
 {
-    constexpr int CHUNKS = D / 8, ROWS = 32 * WAVES;
-    constexpr bool BOTH = WAVES == 4;  // a wave unpacks keys and values; of eight, four each
-    __shared__ __attribute__((aligned(16))) u32x4 s_k[2][kKeys][CHUNKS], s_v[2][D][kKeys / 8];
-    __shared__ __attribute__((aligned(16))) float s_sk[2][kKeys], s_lv[2][kKeys], s_rv[2][kKeys];
-    __shared__ __attribute__((aligned(16))) int s_far[2][4];  // scales that are far from 1, in a quarter of the tile (large ones: or before)
+    constexpr int KW = kKeys / kWaves, DW = D / 32, STEPS = D / 16, W = D / 16;  // (a wave unpacks KW keys; a lane DW dwords of codes)
+    // (rows of keys are 16 bytes longer than they need be: lanes that read or write together meet in no bank)
+    __shared__ __attribute__((aligned(16))) u32x4 s_k[2][kKeys][D / 8 + 1], s_v[2][D][kKeys / 8];
+    __shared__ __attribute__((aligned(16))) float s_sk[4][kKeys], s_lv[4][kKeys], s_rv[4][kKeys], s_none[kKeys], s_row[kRows];
+    __shared__ __attribute__((aligned(16))) uint32_t s_zk[4][kKeys];
+    __shared__ __attribute__((aligned(16))) uint16_t s_zv[4][kKeys];
+    __shared__ __attribute__((aligned(16))) int s_far[4][kWaves];  // scales that are far from 1, in a wave's keys of the tile (large ones: or before)
     __shared__ int s_bad, s_last, s_top;
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int P = 1 << a.lg_page, longest = a.width << a.lg_page;
+    const auto within = [&](int context) { return min(max(context, 0), longest); };
 
-    // the block's tile: as in attn_prompt.hip
+    // The block's tile of rows and its part of the keys.  Up to 64 sequences: a lane looks at each; with a workspace (slots > 0) the tiles of a
+    // sequence are cut into parts of at most `size` tiles of keys, the smallest size with which all parts run at a time.  More sequences are searched for
+    // as in attn_prompt.hip, and their keys are not cut.
     const auto start_of = [&](int s) { return min(max(a.starts[s], 0), a.total_q); };
     const bool few = a.n_seqs <= kFew;
-    int from = 0, len = 0, upto = 0, tiles = a.tiles;
+    int from = 0, len = 0, context = 0, mine = 0, parts = 1, upto = 0, all = a.tiles;
     if (few) {
         if (lane < a.n_seqs) {
             from = start_of(lane);
             len = max(min(a.starts[lane + 1], a.total_q) - from, 0);
+            context = a.context[lane];
+            mine = up(len * a.group, kRows);
         }
-        upto = sums_up_to((len * a.group + ROWS - 1) / ROWS);
-        tiles = min(__builtin_amdgcn_readlane(upto, 63), a.tiles);
+        const int keys = up(within(context), kKeys);
+        upto = sums_up_to(mine);
+        all = __builtin_amdgcn_readlane(upto, 63);
+        if (all > a.tiles) {  // (more than there can be: the sequences overlap)
+            mine = min(mine, a.tiles / a.n_seqs);
+            upto = sums_up_to(mine);
+            all = __builtin_amdgcn_readlane(upto, 63);
+        }
+        if (a.slots > all * a.Hkv) {
+            const int most = a.slots / a.Hkv;  // parts of a kv head
+            int size = max(up(__builtin_amdgcn_readlane(sums_up_to(mine * min(keys, 1 << 16)), 63), most), 2), sum;
+            do {
+                parts = min(max(up(keys, size), 1), kMostParts);
+                upto = sums_up_to(mine * parts);
+                sum = __builtin_amdgcn_readlane(upto, 63);
+                size += up(size, 8);
+            } while (sum > most);  // (one part each fits, and comes before size overflows: keys is below 2^24)
+            all = sum;
+        }
     }
-    const int blocks = tiles * a.Hkv * a.splits, per = (blocks + 7) >> 3, id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+    // Blocks with ids 8 apart run on one XCD: each XCD gets consecutive kv heads, and goes through a head's tiles from the last (the longest rows of
+    // keys) to the first.  Blocks that the grid has too many come last.
+    const int blocks = all * a.Hkv, per = (blocks + 7) >> 3, id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
     if ((int)blockIdx.x >> 3 >= per || id >= blocks) return;
-    const int whole = id / a.splits, part = id % a.splits;
-    const int hk = whole / tiles;
-    int tile = tiles - 1 - whole % tiles;
-    int seq, q0, len_q;
+    const int hk = __builtin_amdgcn_readfirstlane(id / all);
+    int tile = all - 1 - id % all, part = 0, n_parts = 1, seq, q0, len_q, whole = 0;
     if (few) {
         seq = __builtin_ctzll(__ballot(upto > tile) | 1ull << 63);
         q0 = __builtin_amdgcn_readlane(from, seq);
         len_q = __builtin_amdgcn_readlane(len, seq);
-        tile -= seq ? __builtin_amdgcn_readlane(upto, seq - 1) : 0;
+        n_parts = __builtin_amdgcn_readlane(parts, seq);
+        whole = hk * all + (seq ? __builtin_amdgcn_readlane(upto, seq - 1) : 0);  // (the sequence's first part)
+        tile -= whole - hk * all;
+        part = tile % n_parts;
+        tile /= n_parts;
+        whole += tile * n_parts;  // the tile's first part: its place in the workspace, and its ticket
+        context = __builtin_amdgcn_readlane(context, seq);
     } else {
-        const auto first_tile = [&](int s) { return (int)((unsigned)(start_of(s) * a.group) / (unsigned)ROWS) + s; };
+        const auto first_tile = [&](int s) { return (int)((unsigned)(start_of(s) * a.group) / (unsigned)kRows) + s; };
         int end = a.n_seqs;
         seq = 0;
         while (end - seq > 1) {
@@ -141,335 +164,359 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_chunks_kernel(const ChunkAr
         q0 = __builtin_amdgcn_readfirstlane(start_of(seq));
         len_q = __builtin_amdgcn_readfirstlane(max(min(a.starts[seq + 1], a.total_q) - q0, 0));
         tile -= __builtin_amdgcn_readfirstlane(first_tile(seq));
+        context = __builtin_amdgcn_readfirstlane(a.context[seq]);
     }
-    if (tile < 0 || tile * ROWS >= len_q * a.group) return;
+    const auto uniform = [](int &x) { x = __builtin_amdgcn_readfirstlane(x); };
+    uniform(tile), uniform(part), uniform(n_parts), uniform(seq), uniform(q0), uniform(len_q), uniform(whole), uniform(context);
+    if (tile < 0 || tile * kRows >= len_q * a.group) return;
 
-    const int P = 1 << a.lg_page, longest = a.width << a.lg_page;
-    const int context = __builtin_amdgcn_readfirstlane(a.context[seq]), ctx = min(max(context, 0), longest);
-    const int first = tile * ROWS, first_w = first + 32 * wave, rows = len_q * a.group, before = ctx - len_q;
-    const int row = first_w + n, query = min(row, rows - 1) / a.group, head = hk * a.group + min(row, rows - 1) % a.group;
+    const int ctx = within(context), first = tile * kRows, rows = len_q * a.group, before = ctx - len_q;
     const auto sees = [&](int r) { return min(r, rows - 1) / a.group + before + 1; };  // keys (none where it is not above 0)
-    const int limit = sees(row), until = sees(first + ROWS - 1);
-    const int wave_all = __builtin_amdgcn_readfirstlane(sees(first_w)), wave_any = __builtin_amdgcn_readfirstlane(sees(first_w + 31));
-    const bool any_row = first_w < rows;
+    const int row = first + 32 * wave + n, limit = sees(row), wave_all = __builtin_amdgcn_readfirstlane(sees(row - n));
+    const bool any_row = first + 32 * wave < rows;
 
-    const auto turn_k = [](int j) { return D == 128 ? j & 15 : j >> 1 & 7; };
-    const auto turn_v = [](int d) { return ((d >> 1) ^ (d >> 4)) & 7; };
-    const int tiles_k = max((until + kKeys - 1) / kKeys, 0);
-    const int t_last = (int)((unsigned)part * (unsigned)tiles_k / (unsigned)a.splits);
-    int t = (int)((unsigned)(part + 1) * (unsigned)tiles_k / (unsigned)a.splits) - 1, buf = 0;
+    // this part's tiles of keys: n_tiles of them, from t_first down (place p: tile t_first - p)
+    const int tiles_k = __builtin_amdgcn_readfirstlane(max((sees(first + kRows - 1) + kKeys - 1) / kKeys, 0));
+    const int t_first = (int)((unsigned)(part + 1) * (unsigned)tiles_k / (unsigned)n_parts) - 1;
+    const int n_tiles = t_first + 1 - (int)((unsigned)part * (unsigned)tiles_k / (unsigned)n_parts);
 
-    // the codes of this wave's 16 keys of a tile
+    // the codes of this wave's keys of a tile: all from one page
     typedef const __attribute__((address_space(4))) int *ints;
     const ints table = (ints)(uintptr_t)(a.table + (size_t)seq * a.width);
     const unsigned page_bytes = (unsigned)a.Hkv * (unsigned)kv4_head_bytes(P, D);
     const uint8_t *const cache = a.cache + (size_t)hk * kv4_head_bytes(P, D);
-    const int last_page = max((ctx - 1) >> a.lg_page, 0), keys_w = 16 * (wave & 3);
-    const bool value_wave = wave >= 4;
+    const int last_page = max((ctx - 1) >> a.lg_page, 0), keys_w = KW * wave;
     bool bad = context > longest, large = false;
-    Codes<D> ck, cv;  // (of eight waves each uses one)
-    const auto page_of = [&](int t) { return (unsigned)table[min((max(t, 0) * kKeys + keys_w) >> a.lg_page, last_page)]; };
-    const auto load = [&](int t, unsigned page) {
-        const bool any = t >= t_last, out_of_range = page >= (unsigned)a.pages;
+    const auto page_of = [&](int p) __attribute__((always_inline)) { return (unsigned)table[min((max(t_first - p, 0) * kKeys + keys_w) >> a.lg_page, last_page)]; };
+    const auto page_at = [&](int p, unsigned page) __attribute__((always_inline)) {
+        const bool any = p < n_tiles, out_of_range = page >= (unsigned)a.pages;
         bad |= any && out_of_range;
-        const buf_t at = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(cache + (uint64_t)(out_of_range ? 0u : page) * page_bytes), 0,
-                                                           any ? kv4_head_bytes(P, D) : 0, 0x00027000);
-        const int j = (t * kKeys + keys_w) & (P - 1);
-        if (BOTH || !value_wave) load_codes<D>(ck, at, P, j, lane, false);
-        if (BOTH) load_codes<D>(cv, at, P, j, lane, true);
-        if (!BOTH && value_wave) load_codes<D>(ck, at, P, j, lane, true);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(cache + (uint64_t)(out_of_range ? 0u : page) * page_bytes), 0,
+                                                 any ? kv4_head_bytes(P, D) : 0, 0x00027000);
     };
-    unsigned page = 0;
-    if (t >= t_last) {
-        load(t, page_of(t));
-        page = page_of(t - 1);
-    }
+    Dwords<DW> ck, cv;
+    uint32_t wk, wv;  // words of the lane's key, of its keys and its values
+    const int four = lane >> 4, column = lane & 15, key_w = keys_w + column;
+    const auto load_keys = [&](int p, unsigned page) __attribute__((always_inline)) {
+        const buf_t b = page_at(p, page);
+        const int j = ((t_first - p) * kKeys + keys_w) & (P - 1);
+        ck.load(b, lane * (4 * DW), j * (D / 2));
+        wk = __builtin_amdgcn_raw_buffer_load_b32(b, 4 * column, P * D + 4 * j, 0);
+        wv = __builtin_amdgcn_raw_buffer_load_b32(b, 4 * column, P * (D + 4) + 4 * j, 0);
+    };
+    const auto load_values = [&](int p, unsigned page) __attribute__((always_inline)) {
+        const buf_t b = page_at(p, page);
+        const int j = ((t_first - p) * kKeys + keys_w) & (P - 1);
+        cv.load(b, lane * (4 * DW), (P + j) * (D / 2));
+    };
 
-    // Queries, in the keys' order within 8 elements (a pair of a dword's nibbles is four apart).  FP16 as they are; BF16 as FP16 numbers, over a power
-    // of two for the block that brings its largest element to 2^14 .. 2^15, or one of its own for a row that is far smaller.
-    vec<f16, 8> q[D / 16];
-    float q_scale = fabsf(a.scale_log2), row_scale = 1.0f;
+    vec<f16, 8> q[STEPS + 1];
+    float q_scale = fabsf(a.scale_log2);
     bool uneven = false;
-    {
-        const T *src = static_cast<const T *>(a.q) + (long long)(q0 + query) * a.q_token + head * a.q_head + 8 * h;
-        u32x4 raw[D / 16];
+    const auto unpack_keys = [&](int buf, int i) __attribute__((always_inline)) { s_k[buf][keys_w + (lane >> 2)][DW * (lane & 3) + i] = halves8(ck.x[i]); };
+    // Values: [element][key]; a row's 16-byte pieces have the keys that a half of the lanes multiplies at once (two fours, 8 keys apart), and lie at
+    // their number XOR turn_v
+    const auto turn_v = [](int d) { return ((d >> 1) ^ (d >> 4)) & 7; };
+    const auto unpack_values = [&](int buf, int slot, int i) __attribute__((always_inline)) {
+        const uint2 zz = *reinterpret_cast<const uint2 *>(&s_zv[slot][keys_w + 4 * four]);
+        const u32x4 o[2] = {halves8(cv.x[i], zz.x), halves8(cv.x[W / 4 + i], zz.y)};
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) raw[i] = *reinterpret_cast<const u32x4 *>(src + 16 * i);
-        const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;
-        if (threadIdx.x == 0) s_bad = 0, s_top = 0;
-        if constexpr (!__is_same(T, f16)) {
-            int most = 0;  // bits of the row's largest finite element
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int lo = (int)(raw[i][e] & 0x7fffu), hi = (int)(raw[i][e] >> 16 & 0x7fffu);
-                    most = max(most, max(lo < 0x7f80 ? lo : 0, hi < 0x7f80 ? hi : 0));
-                }
-            }
-            const auto both = __builtin_amdgcn_permlane32_swap((unsigned)most, (unsigned)most, false, false);
-            most = max((int)both[0], (int)both[1]);
-            meet();
-            if (row < rows) atomicMax(&s_top, most);
-            meet();
-            const auto exponent = [](int bits) { return max(bits >> 7, 1) - 127; };
-            const int top = exponent(s_top), own = most && row < rows && exponent(most) < top - 14 ? exponent(most) : top;
-            uneven = __any(own != top);
-            const int down = 14 - own;  // up to 140: in two steps
-            const float by0 = power_of_two(down / 2), by1 = power_of_two(down - down / 2);
-            row_scale = power_of_two(max((own - top) / 2, -126)) * power_of_two(max(own - top - (own - top) / 2, -126));
-            q_scale = fminf(fmaxf(q_scale * power_of_two(max(top - 14, -126)), 0x1p-126f), 0x1p127f);
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t x = raw[i][e >> 1];
-                    q[i][2 * (e & 3) + (e >> 2)] = (f16)(__builtin_bit_cast(float, e & 1 ? x & 0xffff0000u : x << 16) * by0 * by1 * sign);
-                }
-        } else {
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) q[i][2 * (e & 3) + (e >> 2)] = __builtin_bit_cast(vec<f16, 8>, raw[i])[e] * (f16)sign;
-        }
-    }
-
-    const auto unpack_keys = [&](const Codes<D> &x, int buf) {
-        const int j = keys_w + (lane >> 2);
-        f16x2v z, z64;
-        zeros_of(x.w[0], x.w[0], z, z64);
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            uint32_t o[4];
-            unpack8(x.c[i], z, z64, o);
-            s_k[buf][j][((D / 32) * (lane & 3) + i) ^ turn_k(j)] = u32x4{o[0], o[1], o[2], o[3]};
-        }
-        const uint32_t word = x.w[0] & kScaleMask;
-        const float s = __builtin_bit_cast(float, word) * q_scale;
-        if ((lane & 3) == 0) s_sk[buf][j] = s > 0x1p127f ? 0x1p127f : s;  // (NaN stays)
-    };
-    const auto unpack_values = [&](const Codes<D> &x, int buf) {
-        constexpr int W = D / 16;  // elements of a column group
-        const int four = lane >> 4, d0 = W * (lane & 15);
-        f16x2v z[2], z64[2];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) zeros_of(x.w[2 * p], x.w[2 * p + 1], z[p], z64[p]);
-#pragma unroll
-        for (int i = 0; i < W / 4; ++i) {
-            uint32_t o[2][4];
-#pragma unroll
-            for (int p = 0; p < 2; ++p) unpack8(x.c[p * (W / 4) + i], z[p], z64[p], o[p]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = d0 + 4 * i + r;
-                reinterpret_cast<uint2 *>(&s_v[buf][d][(2 * (keys_w >> 4) + (four & 1)) ^ turn_v(d)])[four >> 1] = uint2{o[0][r], o[1][r]};
-            }
-        }
-        v4f scale;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t word = x.w[e] & kScaleMask;
-            const float s = __builtin_bit_cast(float, word);
-            scale[e] = s < 0x1p-100f ? 0x1p-100f : s;  // (NaN stays; a place that nothing was written to counts as zeros)
-        }
-        large |= __any(fmaxf(fmaxf(scale[0], scale[1]), fmaxf(scale[2], scale[3])) > 0x1p60f);
-        const bool small = __any(fminf(fminf(scale[0], scale[1]), fminf(scale[2], scale[3])) < 0x1p-40f);
-        if (lane == 0) s_far[buf][keys_w >> 4] = large || small;
-        if ((lane & 15) == 0) {
-            v4f lv, rv;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                lv[e] = __builtin_amdgcn_logf(scale[e]);
-                rv[e] = __builtin_amdgcn_rcpf(scale[e]);
-            }
-            *reinterpret_cast<v4f *>(&s_lv[buf][keys_w + 4 * four]) = lv;
-            *reinterpret_cast<v4f *>(&s_rv[buf][keys_w + 4 * four]) = rv;
+        for (int r = 0; r < 4; ++r) {
+            const int d = W * column + 4 * i + r;
+            reinterpret_cast<uint2 *>(&s_v[buf][d][(2 * wave + (four & 1)) ^ turn_v(d)])[four >> 1] = uint2{o[0][r], o[1][r]};
         }
     };
-    const auto unpack = [&](int buf) {
-        if (BOTH || !value_wave) unpack_keys(ck, buf);
-        if (BOTH) unpack_values(cv, buf);
-        if (!BOTH && value_wave) unpack_values(ck, buf);
+    const auto scales = [&](int slot) __attribute__((always_inline)) {  // (four lanes have each key, and write the same)
+        const uint32_t word_k = wk & kScaleMask, word_v = wv & kScaleMask, z = wk & 15u;
+        const float sk = __builtin_bit_cast(float, word_k) * q_scale;
+        float sv = __builtin_bit_cast(float, word_v);
+        sv = sv < 0x1p-100f ? 0x1p-100f : sv;                // (NaN stays; a place that nothing was written to counts as zeros)
+        s_sk[slot][key_w] = sk > 0x1p127f ? 0x1p127f : sk;   // (here, too)
+        s_zk[slot][key_w] = z | z << 16;
+        s_zv[slot][key_w] = (uint16_t)(wv & 15u);
+        s_lv[slot][key_w] = __builtin_amdgcn_logf(sv);
+        s_rv[slot][key_w] = sv > 0.0f ? __builtin_amdgcn_rcpf(sv) : 0.0f;  // (of NaN 0: who does not see it has no part of it)
+        large |= __any(sv > 0x1p60f);
+        s_far[slot][wave] = (int)large | (int)__any(sv < 0x1p-40f);
+    };
+    // An eighth of what a wave unpacks next to the products of place p + 1: keys of place p + 2 (into p's buffer) and all its scales, values of place p + 1
+    const auto unpack_part = [&](int p, int j) __attribute__((always_inline)) {
+        if (j < DW) unpack_keys(p & 1, j);
+        if (j == 4) scales((p + 2) & 3);
+        if (j >= 5 && j - 5 < W / 4) unpack_values(~p & 1, (p + 1) & 3, j - 5);
+    };
+    const auto next_loads = [&](int p, unsigned &page) __attribute__((always_inline)) {
+        load_values(p + 2, page);
+        page = page_of(p + 3);
+        load_keys(p + 3, page);
     };
 
-    v16f o[D / 32] = {};
-    float m = -__builtin_inff(), m_up = m, base = 0.0f, l = 0.0f;  // maximum of t, from where it moves, kWeightBits - m; this lane's part of sum x / sv
-
-    // Fragments: 32 keys (u) of elements 16 i ..; 32 elements (e) of 16 keys (u).  (Rows 32 apart turn their pieces alike, but for 2 e of the values'.)
+    // Fragments: 32 keys (u) of 16 elements (i); 32 elements (e) of 16 keys (u).  (Rows 32 apart turn their pieces alike, but for 2 e of the values'.)
     int v_at[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) v_at[x] = n * (kKeys / 8) + ((2 * x + h) ^ turn_v(n));
-    const auto keys = [&](int u, int i) {
-        const int c = 2 * i + h;
-        return __builtin_bit_cast(vec<f16, 8>, s_k[buf][32 * u + n][c ^ turn_k(n)]);
+    const auto keys = [&](int buf, int u, int i) { return __builtin_bit_cast(vec<f16, 8>, s_k[buf][32 * u + n][2 * i + h]); };
+    const auto values = [&](int buf, int u, int e) { return __builtin_bit_cast(vec<f16, 8>, (&s_v[buf][32 * e][0])[v_at[u ^ e]]); };
+    const auto zeros = [&](int slot, int u) {
+        const uint32_t zz = s_zk[slot][32 * u + n];
+        return __builtin_bit_cast(vec<f16, 8>, u32x4{zz, zz, 0, 0});
     };
-    const auto values = [&](int u, int e) { return __builtin_bit_cast(vec<f16, 8>, (&s_v[buf][32 * e][0])[v_at[u ^ e]]); };
-    const auto step = [&](int key) {
-        v16f s[2] = {};
-        vec<f16, 8> frag[2][2] = {{keys(0, 0), keys(1, 0)}};
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-            if (i + 1 < D / 16)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) frag[(i + 1) & 1][u] = keys(u, i + 1);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) s[u] = mfma32(frag[i & 1][u], q[i], s[u]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+
+    v16f o[D / 32], s[2];
+    vec<f16, 8> w[4];
+    float m = -__builtin_inff(), l = 0.0f;  // maximum of t, this lane's part of sum x / sv
+    // The softmax of place p's scores: s -> w, l, m
+    const auto softmax = [&](int p) __attribute__((always_inline)) {
+        const int slot = p & 3, key = (t_first - p) * kKeys;
+        const auto at = [&](int i) { return 32 * (i >> 2) + 8 * (i & 3) + 4 * h; };  // the lane's keys 4 i ..
         if (uneven) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) s[u] *= row_scale;
+            asm volatile("s_nop 0");  // (kept a branch)
+            s[0] *= s_row[row - first], s[1] *= s_row[row - first];
         }
-        const bool masked = key + kKeys > wave_all;  // some row of the wave does not see all of these keys
-        const int seen = limit - key - 4 * h;  // of the keys that a lane has from 4 h on
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int i = 0; i < 8; ++i) {
+            const v4f sk = *reinterpret_cast<const v4f *>(&s_sk[slot][at(i)]), lv = *reinterpret_cast<const v4f *>(&s_lv[slot][at(i)]);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const v4f sk = *reinterpret_cast<const v4f *>(&s_sk[buf][32 * u + 8 * g + 4 * h]), lv = *reinterpret_cast<const v4f *>(&s_lv[buf][32 * u + 8 * g + 4 * h]);
+            for (int e = 0; e < 4; ++e) s[i >> 2][4 * (i & 3) + e] = __builtin_fmaf(s[i >> 2][4 * (i & 3) + e], sk[e], lv[e]);
+        }
+        if (key + kKeys > wave_all) {  // some row of the wave does not see all of these keys
+            const int seen = limit - key - 4 * h;  // of the keys that a lane has from 4 h on
+            asm volatile("s_nop 0");
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s[u][4 * g + r] = __builtin_fmaf(s[u][4 * g + r], sk[r], lv[r]);
-                if (g & 1) __builtin_amdgcn_sched_barrier(0);
-            }
-        if (masked) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[u][i] = 32 * u + 8 * (i >> 2) + (i & 3) < seen ? s[u][i] : -__builtin_inff();
+            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = 8 * (i >> 2) + (i & 3) < seen ? s[i >> 4][i & 15] : -__builtin_inff();
         }
         float top = m;
 #pragma unroll
         for (int i = 0; i < 32; i += 2) top = fmaxf(fmaxf(top, s[i >> 4][i & 15]), s[i >> 4][(i & 15) + 1]);
-        if (__any(top > m_up)) {  // (first of all: m is minus infinity)
+        constexpr float kUp = 14.0f - kWeightBits;  // (from where the maximum moves)
+        if (__any(top > m + kUp)) {                 // (first of all: m is minus infinity)
             const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, top), __builtin_bit_cast(unsigned, top), false, false);
             top = fmaxf(__builtin_bit_cast(float, (unsigned)both[0]), __builtin_bit_cast(float, (unsigned)both[1]));
-            top = top > m_up ? top : m;  // (a row's results go by its own scores alone)
+            top = top > m + kUp ? top : m;  // (a row's results go by its own scores alone)
             // (in two steps for l: a factor of 2^-200 may still leave something of a sum that is 2^100)
             const float half = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m - top) * 0.5f), by = half * half;
             m = top;
-            m_up = top + (14.0f - kWeightBits);
-            base = top == -__builtin_inff() ? 0.0f : kWeightBits - top;
             l = l * half * half;
 #pragma unroll
             for (int e = 0; e < D / 32; ++e) o[e] *= by;
         }
-        const v4i far4 = *reinterpret_cast<const v4i *>(s_far[buf]);
-        if (masked || __builtin_amdgcn_readfirstlane(far4[0] | far4[1] | far4[2] | far4[3])) {
-            // the sum from the scores themselves (2^16 of it, which is 2^-130 .. 2^122); what is masked has no part in it
+        const float base = m == -__builtin_inff() ? 0.0f : kWeightBits - m, *sums = s_rv[slot];
+        const v4i far4 = *reinterpret_cast<const v4i *>(s_far[slot]);
+        if (__builtin_amdgcn_readfirstlane(far4[0] | far4[1] | far4[2] | far4[3])) {
+            // the sum from the scores themselves (2^16 of it, which is 2^-130 .. 2^122); the factors below are then zeros
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int i = 0; i < 8; ++i) {
+                const v4f lv = *reinterpret_cast<const v4f *>(&s_lv[slot][at(i)]);
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const v4f lv = *reinterpret_cast<const v4f *>(&s_lv[buf][32 * u + 8 * g + 4 * h]);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float t = s[u][4 * g + r], p = __builtin_amdgcn_exp2f(t - lv[r] + (base + 16.0f));
-                        l = __builtin_fmaf(32 * u + 8 * g + r < seen ? p : 0.0f, 0x1p-16f, l);
-                        s[u][4 * g + r] = __builtin_amdgcn_exp2f(t + base);
-                    }
-                    if (g & 1) __builtin_amdgcn_sched_barrier(0);
+                for (int e = 0; e < 4; ++e) {
+                    const float x = s[i >> 2][4 * (i & 3) + e], whole = __builtin_amdgcn_exp2f(x - lv[e] + (base + 16.0f));
+                    l = __builtin_fmaf(x == -__builtin_inff() ? 0.0f : whole, 0x1p-16f, l);  // (whatever is there)
                 }
-        } else {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const v4f rv = *reinterpret_cast<const v4f *>(&s_rv[buf][32 * u + 8 * g + 4 * h]);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float x = __builtin_amdgcn_exp2f(s[u][4 * g + r] + base);
-                        l = __builtin_fmaf(x, rv[r], l);
-                        s[u][4 * g + r] = x;
-                    }
-                    if (g & 1) __builtin_amdgcn_sched_barrier(0);
-                }
+            }
+            sums = s_none;
         }
-        vec<f16, 8> p[4];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) p[i >> 3][i & 7] = (f16)s[i >> 4][i & 15];
+        for (int i = 0; i < 8; ++i) {
+            const v4f rv = *reinterpret_cast<const v4f *>(&sums[at(i)]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+            for (int e = 0; e < 4; ++e) {
+                const float x = __builtin_amdgcn_exp2f(s[i >> 2][4 * (i & 3) + e] + base);
+                l = __builtin_fmaf(x, rv[e], l);
+                w[i >> 1][4 * (i & 1) + e] = (f16)x;
+            }
+        }
+        asm volatile("" : "+v"(l), "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));  // (here, not among the products, where the scores would have to stay)
+    };
+    // The second product of place p and the first one of place p + 1, next to which the codes behind them are unpacked: eight slices, whose fragments are read
+    // one slice ahead.  The order is that of the statements between scheduling barriers.
+    const auto products = [&](int p) __attribute__((always_inline)) {
+        constexpr int E = D / 64;
+        const int buf = p & 1;
+        vec<f16, 8> kf[2][2], vf[2][E];
+        const auto fragments = [&](int j) __attribute__((always_inline)) {
+            if (j * STEPS % 8 == 0)
 #pragma unroll
-            for (int e = 0; e < D / 32; ++e) o[e] = mfma32(values(u, e), p[u], o[e]);
+                for (int u = 0; u < 2; ++u) kf[j * STEPS / 8 & 1][u] = keys(buf ^ 1, u, j * STEPS / 8);
+#pragma unroll
+            for (int e = 0; e < E; ++e) vf[j & 1][e] = values(buf, j >> 1, (j & 1) * E + e);
+        };
+#pragma unroll
+        for (int u = 0; u < 2; ++u) s[u] = mfma32(zeros((p + 1) & 3, u), q[STEPS], v16f{});
+        fragments(0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = j * STEPS / 8;
+            if (j < 7) fragments(j + 1);
+            if (j * STEPS % 8 == 0)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) s[u] = mfma32(kf[i & 1][u], q[i], s[u]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[(j & 1) * E + e] = mfma32(vf[j & 1][e], w[j >> 1], o[(j & 1) * E + e]);
+            unpack_part(p, j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
 
-    if (t >= t_last) {
-        unpack(0);
-        load(t - 1, page);
-        page = page_of(t - 2);
-    }
-    for (; t >= t_last; --t, buf ^= 1) {
-        meet();  // (the tile is there, and all waves have read the one before it)
-        if (t > t_last) {  // the next tile's codes are unpacked, those of the one after it loaded
-            unpack(buf ^ 1);
-            load(t - 2, page);
-            page = page_of(t - 3);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if (any_row && t * kKeys < wave_any) step(t * kKeys);  // (else: no row of the wave sees any of them)
-    }
+    // Results: a row's, and where a part of the keys leaves what it has (a lane without a row leaves and reads nothing)
+    const auto write_row = [&]() __attribute__((always_inline)) {
+        const float by = l == 0.0f ? 0.0f : 1.0f / l;
+        T *const dst = static_cast<T *>(a.out) + ((size_t)(q0 + row / a.group) * a.Hq + hk * a.group + row % a.group) * D;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                vec<T, 4> y;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) y[x] = (T)(o[e][4 * i + x] * (x & 1 ? 0x1p20f : 0x1p24f) * by);
+                *reinterpret_cast<vec<T, 4> *>(dst + 32 * e + 8 * i + 4 * h) = y;
+            }
+    };
+    constexpr int FLOATS = 64 * kWaves * (D / 2 + 4), kShared = 16;  // of a part; sc1
+    const auto left_parts = __builtin_amdgcn_make_buffer_rsrc(a.parts + (size_t)whole * FLOATS, 0, n_parts * FLOATS * 4, 0x00027000);
+    const auto part_at = [&](int p, int piece) { return row < rows ? (p * FLOATS + (piece * 64 * kWaves + (int)threadIdx.x) * 4) * 4 : n_parts * FLOATS * 4; };
 
+    if (threadIdx.x == 0) s_bad = s_top = 0;
+    if (threadIdx.x < kKeys) s_none[threadIdx.x] = 0.0f;
+    // Queries, in the keys' order within 8 elements (a pair of a dword's nibbles is four apart), over a power of two for the block that brings its
+    // largest element to 4 .. 8, what meets even pairs times 16: what is above 2^-17 of the largest is held exactly.  A row whose largest element is below
+    // 2^-8 of the block's has a power of its own, and a factor for its scores.  A last operand holds what the zero points are multiplied with, minus 16 times
+    // the sum of the row's elements, as three numbers (33 bits of it).
+    {
+        float f[STEPS][8];
+        int most = 0;  // bits of the row's largest finite element
+        {
+            const int at = min(row, rows - 1);
+            const T *src = static_cast<const T *>(a.q) + (long long)(q0 + at / a.group) * a.q_token + (hk * a.group + at % a.group) * a.q_head + 8 * h;
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                const u32x4 raw = *reinterpret_cast<const u32x4 *>(src + 16 * i);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (__is_same(T, f16))
+                        f[i][e] = (float)__builtin_bit_cast(vec<f16, 8>, raw)[e];
+                    else
+                        f[i][e] = __builtin_bit_cast(float, e & 1 ? raw[e >> 1] & 0xffff0000u : raw[e >> 1] << 16);
+                    const int bits = __builtin_bit_cast(int, f[i][e]) & 0x7fffffff;
+                    most = max(most, bits < 0x7f800000 ? bits : 0);
+                }
+            }
+        }
+        const auto both = __builtin_amdgcn_permlane32_swap((unsigned)most, (unsigned)most, false, false);
+        most = max((int)both[0], (int)both[1]);
+        meet();
+        if (row < rows) atomicMax(&s_top, most);
+        meet();
+        const auto exponent = [](int bits) { return max(bits >> 23, 1) - 129; };
+        const int top = exponent(__builtin_amdgcn_readfirstlane(s_top)), own = most && exponent(most) < top - 8 ? exponent(most) : top;
+        q_scale = fminf(fmaxf(q_scale * 0x1p20f * power_of_two(max(top, -126)), 0x1p-126f), 0x1p127f);
+        s_row[row - first] = power_of_two(max(own - top, -126));
+        uneven = __any(own != top);
+        const float by0 = power_of_two(-own / 2) * (a.scale_log2 < 0.0f ? -1.0f : 1.0f), by1 = power_of_two(-own - -own / 2);  // (up to 2^128: in two steps)
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const f16 x = (f16)(f[i][e] * by0 * by1);
+                sum += (float)x;
+                q[i][2 * (e & 3) + (e >> 2)] = e & 1 ? x : x * (f16)16.0f;
+            }
+        const auto halves = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, sum), __builtin_bit_cast(unsigned, sum), false, false);
+        sum = -16.0f * (__builtin_bit_cast(float, (unsigned)halves[0]) + __builtin_bit_cast(float, (unsigned)halves[1]));
+        const f16 s0 = (f16)sum, s1 = (f16)(sum - (float)s0), s2 = (f16)(sum - (float)s0 - (float)s1);
+        q[STEPS] = vec<f16, 8>{};
+        if (h == 0) q[STEPS][0] = s0, q[STEPS][1] = s1, q[STEPS][2] = s2;
+    }
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) o[e] = v16f{};
+    if (n_tiles > 0) {
+        // the first two tiles' keys and scales, the first one's values
+        unsigned page = page_of(0);
+        load_keys(0, page);
+        load_values(0, page);
+#pragma unroll
+        for (int i = 0; i < DW; ++i) unpack_keys(0, i);
+        scales(0);
+        page = page_of(1);
+        load_keys(1, page);
+        meet();  // (a wave writes the zero points that it reads, but the compiler has to know)
+#pragma unroll
+        for (int i = 0; i < W / 4; ++i) unpack_values(0, 0, i);
+        load_values(1, page);
+#pragma unroll
+        for (int i = 0; i < DW; ++i) unpack_keys(1, i);
+        scales(1);
+        page = page_of(2);
+        load_keys(2, page);
+        meet();
+        if (any_row) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                s[u] = mfma32(zeros(0, u), q[STEPS], v16f{});
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i) s[u] = mfma32(keys(0, u, i), q[i], s[u]);
+            }
+            for (int p = 0; p < n_tiles; ++p) {
+                softmax(p);
+                meet();  // (what the next products read is there, and all waves are done with what they write over)
+                products(p);
+                next_loads(p, page);
+            }
+        } else {
+            for (int p = 0; p < n_tiles; ++p) {
+                meet();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) unpack_part(p, j);
+                next_loads(p, page);
+            }
+        }
+    }
     if (bad) s_bad = 1;
     meet();
     const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, l), __builtin_bit_cast(unsigned, l), false, false);
     l = __builtin_bit_cast(float, (unsigned)both[0]) + __builtin_bit_cast(float, (unsigned)both[1]);
     if (s_bad) l = __builtin_nanf("");
-    if (a.splits > 1) {
-        // every part leaves its maxima, sums and results, past the L2s; the last to arrive at the tile's ticket joins them, in their order
-        constexpr int FLOATS = 64 * WAVES * (D / 2 + 4);  // of a part
-        float *const parts = a.parts + (size_t)whole * a.splits * FLOATS;
-        const auto all = __builtin_amdgcn_make_buffer_rsrc(parts, 0, a.splits * FLOATS * 4, 0x00027000);
-        const int none = row < rows ? 0 : a.splits * FLOATS * 4;  // (a lane without a row leaves and reads nothing)
-        const auto at = [&](int p, int piece) { return (p * FLOATS + (piece * 64 * WAVES + (int)threadIdx.x) * 4) * 4 + none; };
-        constexpr int kShared = 16;  // sc1
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v4f{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]}), all,
-                                                       at(part, 4 * e + i), 0, kShared);
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v4f{m, l, 0.0f, 0.0f}), all, at(part, D / 8), 0, kShared);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (threadIdx.x == 0) {
-            const unsigned arrived = __hip_atomic_fetch_add(a.tickets + whole, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            s_last = arrived == (unsigned)a.splits - 1;
-            if (s_last) __hip_atomic_store(a.tickets + whole, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (!s_last) return;
-        m = -__builtin_inff();
-        l = 0.0f;
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) o[e] = v16f{};
-        for (int p = 0; p < a.splits; ++p) {
-            const v4f ml = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(all, at(p, D / 8), 0, kShared));
-            v4f x[D / 8];
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i) x[i] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(all, at(p, i), 0, kShared));
-            const float now = fmaxf(m, ml[0]);
-            const float old = m == now ? 1.0f : __builtin_amdgcn_exp2f((m - now) * 0.5f);
-            const float by = ml[0] == now ? 1.0f : __builtin_amdgcn_exp2f((ml[0] - now) * 0.5f);
-            m = now;
-            l = l * old * old + ml[1] * by * by;
-#pragma unroll
-            for (int e = 0; e < D / 32; ++e)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[e][i] = o[e][i] * (old * old) + x[4 * e + (i >> 2)][i & 3] * (by * by);
-        }
+    if (n_parts == 1) {
+        if (row < rows) write_row();
+        return;
     }
-    if (row >= rows) return;
-    const float by = l == 0.0f ? 0.0f : 1.0f / l;
-    T *dst = static_cast<T *>(a.out) + ((size_t)(q0 + query) * a.Hq + head) * D;
+    // Every part leaves its maxima, sums and results, past the L2s; the last to arrive at the tile's ticket joins them, in their order
 #pragma unroll
     for (int e = 0; e < D / 32; ++e)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            vec<T, 4> y;
+        for (int i = 0; i < 4; ++i)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v4f{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]}), left_parts,
+                                                   part_at(part, 4 * e + i), 0, kShared);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v4f{m, l, 0.0f, 0.0f}), left_parts, part_at(part, D / 8), 0, kShared);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (threadIdx.x == 0) {
+        const unsigned arrived = __hip_atomic_fetch_add(a.tickets + whole, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_last = arrived == (unsigned)n_parts - 1;
+        if (s_last) __hip_atomic_store(a.tickets + whole, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (!__builtin_amdgcn_readfirstlane(s_last)) return;
+    m = -__builtin_inff();
+    l = 0.0f;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = (T)(o[e][4 * i + r] * by);
-            *reinterpret_cast<vec<T, 4> *>(dst + 32 * e + 8 * i + 4 * h) = y;
-        }
+    for (int e = 0; e < D / 32; ++e) o[e] = v16f{};
+    for (int p = 0; p < n_parts; ++p) {
+        const v4f ml = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(left_parts, part_at(p, D / 8), 0, kShared));
+        v4f x[D / 8];
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) x[i] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(left_parts, part_at(p, i), 0, kShared));
+        const float now = fmaxf(m, ml[0]);
+        const float old = m == now ? 1.0f : __builtin_amdgcn_exp2f((m - now) * 0.5f);
+        const float by = ml[0] == now ? 1.0f : __builtin_amdgcn_exp2f((ml[0] - now) * 0.5f);
+        m = now;
+        l = l * old * old + ml[1] * by * by;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[e][i] = o[e][i] * (old * old) + x[4 * e + (i >> 2)][i & 3] * (by * by);
+    }
+    if (row < rows) write_row();
 }
 
 }  // namespace lqq
@@ -478,33 +525,27 @@ using namespace lqq;
 
 namespace {
 constexpr size_t kTickets = 32768;  // bytes at the head of the workspace, those of the GEMM's
-// Waves of a block: eight where they have rows for most of the tiles
-int waves_of(int total_q, int n_seqs, int group) { return (long long)total_q * group >= 256LL * n_seqs ? 8 : 4; }
 // Tiles of a kv head, at most (more than 64 sequences: as they are searched for)
-long long tiles_of(int total_q, int n_seqs, int group, int waves)
+long long tiles_of(int total_q, int n_seqs, int group)
 {
-    const long long rows = (long long)total_q * group, each = 32 * waves;
-    return n_seqs <= kFew ? (rows + (long long)n_seqs * (each - 1)) / each : rows / each + n_seqs;
+    const long long rows = (long long)total_q * group;
+    return n_seqs <= kFew ? (rows + (long long)n_seqs * (kRows - 1)) / kRows : rows / kRows + n_seqs;
 }
-// Parts of the keys, where the tiles are fewer than the blocks that run at a time: as many as fill the CUs, none with fewer than four tiles of keys where all
-// contexts are as long as the table allows
-int splits_of(long long blocks, int waves, int longest)
+// Blocks that run at a time: what the keys are cut into, where there are fewer tiles than that (0: they are not cut)
+int slots_of(long long tiles, int n_seqs, int Hkv)
 {
-    const long long at_once = waves == 8 ? 256 : 512;
-    if (blocks < 1 || blocks >= at_once) return 1;
-    return (int)std::max<long long>(1, std::min<long long>({at_once / blocks, (long long)longest / (4 * kKeys), 32}));
+    constexpr int kSlots = 512;
+    return n_seqs <= kFew && tiles * Hkv < kSlots ? kSlots : 0;
 }
-size_t part_bytes(int head_dim, int waves) { return sizeof(float) * 64 * waves * (head_dim / 2 + 4); }
+size_t part_bytes(int head_dim) { return sizeof(float) * 64 * kWaves * (head_dim / 2 + 4); }
 }  // namespace
 
 extern "C" size_t kv4_attention_chunks_workspace_size(int n_seqs, int total_q, int Hq, int Hkv, int head_dim, int page_size, int table_width)
 {
     if (n_seqs < 1 || total_q < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv || !head_dim_ok(head_dim) || !page_ok(page_size) || table_width < 1 || table_width > (1 << 30) / page_size)
         return 0;
-    const int waves = waves_of(total_q, n_seqs, Hq / Hkv);
-    const long long blocks = tiles_of(total_q, n_seqs, Hq / Hkv, waves) * Hkv;
-    const int splits = splits_of(blocks, waves, table_width * page_size);
-    return splits == 1 ? 0 : kTickets + (size_t)blocks * splits * part_bytes(head_dim, waves);
+    const int slots = slots_of(tiles_of(total_q, n_seqs, Hq / Hkv), n_seqs, Hkv);
+    return slots ? kTickets + slots * part_bytes(head_dim) : 0;
 }
 
 extern "C" int kv4_attention_chunks(int dtype, int n_seqs, int total_q, int Hq, int Hkv, int head_dim, const void *q, long long q_token, long long q_head,
@@ -527,22 +568,22 @@ extern "C" int kv4_attention_chunks(int dtype, int n_seqs, int total_q, int Hq, 
         return fail(LQ_ERR_ALIGN, "q, cache, out and workspace must be 16-byte aligned");
     if (((uintptr_t)starts_q | (uintptr_t)block_table | (uintptr_t)context) & 3) return fail(LQ_ERR_ALIGN, "starts_q, block_table and context must be 4-byte aligned");
     if ((total_q > 1 && q_token % 8) || (Hq > 1 && q_head % 8)) return fail(LQ_ERR_ALIGN, "q: strides must be multiples of 8 elements, got %lld and %lld", q_token, q_head);
-    const int group = Hq / Hkv, waves = waves_of(total_q, n_seqs, group);
-    const long long tiles = tiles_of(total_q, n_seqs, group, waves);
+    const int group = Hq / Hkv;
+    const long long tiles = tiles_of(total_q, n_seqs, group);
     if (tiles * Hkv > (1 << 22) || (long long)total_q * group > (1 << 30)) return fail(LQ_ERR_INVALID, "too many rows: %d queries of %d sequences, %d heads", total_q, n_seqs, Hq);
     const size_t need = kv4_attention_chunks_workspace_size(n_seqs, total_q, Hq, Hkv, head_dim, page_size, table_width);
-    const int splits = need && workspace && workspace_bytes >= need ? splits_of(tiles * Hkv, waves, table_width * page_size) : 1;
+    const int slots = need && workspace && workspace_bytes >= need ? slots_of(tiles, n_seqs, Hkv) : 0;
     const ChunkArgs a{q, q_token, q_head, starts_q, block_table, context, static_cast<const uint8_t *>(cache), out,
-                      static_cast<unsigned *>(workspace), splits > 1 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + kTickets) : nullptr,
-                      n_seqs, total_q, Hq, Hkv, group, table_width, num_pages, log2_of(page_size), (int)tiles, splits, scale * 1.44269504f};
-    const dim3 grid((unsigned)((tiles * Hkv * splits + 7) / 8 * 8));
+                      static_cast<unsigned *>(workspace), slots ? reinterpret_cast<float *>(static_cast<char *>(workspace) + kTickets) : nullptr,
+                      n_seqs, total_q, Hq, Hkv, group, table_width, num_pages, log2_of(page_size), (int)tiles, slots, scale * 1.44269504f};
+    const dim3 grid((unsigned)((std::max<long long>(tiles * Hkv, slots) + 7) / 8 * 8));
     (void)hipGetLastError();
-    const WorkspaceTurn turn(splits > 1 ? workspace : nullptr, hip_stream);
-    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, static_cast<hipStream_t>(hip_stream), a); };
+    const WorkspaceTurn turn(slots ? workspace : nullptr, hip_stream);
+    const auto go = [&](auto kernel) __attribute__((always_inline)) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), 0, static_cast<hipStream_t>(hip_stream), a); };
     const auto of = [&](auto x, auto d) {
         using T = decltype(x);
         constexpr int D = decltype(d)::value;
-        waves == 8 ? go(kv4_chunks_kernel<D, T, 8>) : go(kv4_chunks_kernel<D, T, 4>);
+        go(kv4_chunks_kernel<D, T>);
     };
     using Wide = std::integral_constant<int, 128>;
     using Narrow = std::integral_constant<int, 64>;
