@@ -37,7 +37,7 @@ struct ChunkArgs {
     float scale_log2;
 };
 
-constexpr int kFew = 64, kKeys = 64, kWaves = 4, kRows = 32 * kWaves, kMostParts = 32;
+constexpr int kFew = 64, kLittle = 32, kKeys = 64, kWaves = 4, kRows = 32 * kWaves, kMostParts = 32;
 constexpr float kWeightBits = 6.0f;
 typedef f16 f16x2v __attribute__((ext_vector_type(2)));
 
@@ -88,8 +88,18 @@ template <int D, class T>
 __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkArgs a)
 {
     constexpr int KW = kKeys / kWaves, DW = D / 32, STEPS = D / 16, W = D / 16;  // (a wave unpacks KW keys; a lane DW dwords of codes)
-    // (rows of keys are 16 bytes longer than they need be: lanes that read or write together meet in no bank)
-    __shared__ __attribute__((aligned(16))) u32x4 s_k[2][kKeys][D / 8 + 1], s_v[2][D][kKeys / 8];
+    // Unpacked codes of two tiles (rows of keys are 16 bytes longer than they need be: lanes that read or write together meet in no bank); or, of a tile with
+    // few rows, the waves' results
+    struct Tiles {
+        u32x4 k[2][kKeys][D / 8 + 1], v[2][D][kKeys / 8];
+    };
+    union Pool {
+        Tiles tiles;
+        float o[kWaves][32][D + 4];
+    };
+    __shared__ __attribute__((aligned(16))) Pool s_pool;
+    auto &s_k = s_pool.tiles.k;
+    auto &s_v = s_pool.tiles.v;
     __shared__ __attribute__((aligned(16))) float s_sk[4][kKeys], s_lv[4][kKeys], s_rv[4][kKeys], s_none[kKeys], s_row[kRows];
     __shared__ __attribute__((aligned(16))) uint32_t s_zk[4][kKeys];
     __shared__ __attribute__((aligned(16))) uint16_t s_zv[4][kKeys];
@@ -113,7 +123,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
             context = a.context[lane];
             mine = up(len * a.group, kRows);
         }
-        const int keys = up(within(context), kKeys);
+        const bool little = len * a.group <= kLittle;
+        const int keys = up(within(context), little ? 4 * kKeys : kKeys);  // tiles of keys, by what they cost
         upto = sums_up_to(mine);
         all = __builtin_amdgcn_readlane(upto, 63);
         if (all > a.tiles) {  // (more than there can be: the sequences overlap)
@@ -123,9 +134,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
         }
         if (a.slots > all * a.Hkv) {
             const int most = a.slots / a.Hkv;  // parts of a kv head
-            int size = max(up(__builtin_amdgcn_readlane(sums_up_to(mine * min(keys, 1 << 16)), 63), most), 2), sum;
+            int size = max(up(__builtin_amdgcn_readlane(sums_up_to(mine * min(keys, 1 << 16)), 63), most), 1), sum;
             do {
-                parts = min(max(up(keys, size), 1), kMostParts);
+                parts = min(max(up(keys, little ? size : max(size, 2)), 1), kMostParts);
                 upto = sums_up_to(mine * parts);
                 sum = __builtin_amdgcn_readlane(upto, 63);
                 size += up(size, 8);
@@ -172,7 +183,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
 
     const int ctx = within(context), first = tile * kRows, rows = len_q * a.group, before = ctx - len_q;
     const auto sees = [&](int r) { return min(r, rows - 1) / a.group + before + 1; };  // keys (none where it is not above 0)
-    const int row = first + 32 * wave + n, limit = sees(row), wave_all = __builtin_amdgcn_readfirstlane(sees(row - n));
+    const bool little = rows - first <= kLittle;  // all waves have the same rows, and keys of their own
+    const int row = first + (little ? 0 : 32 * wave) + n, limit = sees(row), wave_all = __builtin_amdgcn_readfirstlane(sees(row - n));
     const bool any_row = first + 32 * wave < rows;
 
     // this part's tiles of keys: n_tiles of them, from t_first down (place p: tile t_first - p)
@@ -196,7 +208,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
     };
     Dwords<DW> ck, cv;
     uint32_t wk, wv;  // words of the lane's key, of its keys and its values
-    const int four = lane >> 4, column = lane & 15, key_w = keys_w + column;
+    const int four = lane >> 4, column = lane & 15;
     const auto load_keys = [&](int p, unsigned page) __attribute__((always_inline)) {
         const buf_t b = page_at(p, page);
         const int j = ((t_first - p) * kKeys + keys_w) & (P - 1);
@@ -226,7 +238,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
             reinterpret_cast<uint2 *>(&s_v[buf][d][(2 * wave + (four & 1)) ^ turn_v(d)])[four >> 1] = uint2{o[0][r], o[1][r]};
         }
     };
-    const auto scales = [&](int slot) __attribute__((always_inline)) {  // (four lanes have each key, and write the same)
+    const auto scales = [&](int slot, int key_w) __attribute__((always_inline)) {  // (lanes that have the same key write the same)
         const uint32_t word_k = wk & kScaleMask, word_v = wv & kScaleMask, z = wk & 15u;
         const float sk = __builtin_bit_cast(float, word_k) * q_scale;
         float sv = __builtin_bit_cast(float, word_v);
@@ -237,12 +249,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
         s_lv[slot][key_w] = __builtin_amdgcn_logf(sv);
         s_rv[slot][key_w] = sv > 0.0f ? __builtin_amdgcn_rcpf(sv) : 0.0f;  // (of NaN 0: who does not see it has no part of it)
         large |= __any(sv > 0x1p60f);
-        s_far[slot][wave] = (int)large | (int)__any(sv < 0x1p-40f);
+        return (int)large | (int)__any(sv < 0x1p-40f);
     };
     // An eighth of what a wave unpacks next to the products of place p + 1: keys of place p + 2 (into p's buffer) and all its scales, values of place p + 1
     const auto unpack_part = [&](int p, int j) __attribute__((always_inline)) {
         if (j < DW) unpack_keys(p & 1, j);
-        if (j == 4) scales((p + 2) & 3);
+        if (j == 4) s_far[(p + 2) & 3][wave] = scales((p + 2) & 3, keys_w + column);
         if (j >= 5 && j - 5 < W / 4) unpack_values(~p & 1, (p + 1) & 3, j - 5);
     };
     const auto next_loads = [&](int p, unsigned &page) __attribute__((always_inline)) {
@@ -266,28 +278,29 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
     vec<f16, 8> w[4];
     float m = -__builtin_inff(), l = 0.0f;  // maximum of t, this lane's part of sum x / sv
     // The softmax of place p's scores: s -> w, l, m
-    const auto softmax = [&](int p) __attribute__((always_inline)) {
-        const int slot = p & 3, key = (t_first - p) * kKeys;
+    const auto softmax = [&](int slot, int key, bool far, auto n_u) __attribute__((always_inline)) {
+        constexpr int U = decltype(n_u)::value;  // times 32 keys
         const auto at = [&](int i) { return 32 * (i >> 2) + 8 * (i & 3) + 4 * h; };  // the lane's keys 4 i ..
         if (uneven) {
             asm volatile("s_nop 0");  // (kept a branch)
-            s[0] *= s_row[row - first], s[1] *= s_row[row - first];
+#pragma unroll
+            for (int u = 0; u < U; ++u) s[u] *= s_row[row - first];
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4 * U; ++i) {
             const v4f sk = *reinterpret_cast<const v4f *>(&s_sk[slot][at(i)]), lv = *reinterpret_cast<const v4f *>(&s_lv[slot][at(i)]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[i >> 2][4 * (i & 3) + e] = __builtin_fmaf(s[i >> 2][4 * (i & 3) + e], sk[e], lv[e]);
         }
-        if (key + kKeys > wave_all) {  // some row of the wave does not see all of these keys
+        if (key + 32 * U > wave_all) {  // some row of the wave does not see all of these keys
             const int seen = limit - key - 4 * h;  // of the keys that a lane has from 4 h on
             asm volatile("s_nop 0");
 #pragma unroll
-            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = 8 * (i >> 2) + (i & 3) < seen ? s[i >> 4][i & 15] : -__builtin_inff();
+            for (int i = 0; i < 16 * U; ++i) s[i >> 4][i & 15] = 8 * (i >> 2) + (i & 3) < seen ? s[i >> 4][i & 15] : -__builtin_inff();
         }
         float top = m;
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) top = fmaxf(fmaxf(top, s[i >> 4][i & 15]), s[i >> 4][(i & 15) + 1]);
+        for (int i = 0; i < 16 * U; i += 2) top = fmaxf(fmaxf(top, s[i >> 4][i & 15]), s[i >> 4][(i & 15) + 1]);
         constexpr float kUp = 14.0f - kWeightBits;  // (from where the maximum moves)
         if (__any(top > m + kUp)) {                 // (first of all: m is minus infinity)
             const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, top), __builtin_bit_cast(unsigned, top), false, false);
@@ -301,11 +314,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
             for (int e = 0; e < D / 32; ++e) o[e] *= by;
         }
         const float base = m == -__builtin_inff() ? 0.0f : kWeightBits - m, *sums = s_rv[slot];
-        const v4i far4 = *reinterpret_cast<const v4i *>(s_far[slot]);
-        if (__builtin_amdgcn_readfirstlane(far4[0] | far4[1] | far4[2] | far4[3])) {
+        if (far) {
             // the sum from the scores themselves (2^16 of it, which is 2^-130 .. 2^122); the factors below are then zeros
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4 * U; ++i) {
                 const v4f lv = *reinterpret_cast<const v4f *>(&s_lv[slot][at(i)]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -316,7 +328,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
             sums = s_none;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4 * U; ++i) {
             const v4f rv = *reinterpret_cast<const v4f *>(&sums[at(i)]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -325,7 +337,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
                 w[i >> 1][4 * (i & 1) + e] = (f16)x;
             }
         }
-        asm volatile("" : "+v"(l), "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));  // (here, not among the products, where the scores would have to stay)
+        if constexpr (U == 2) asm volatile("" : "+v"(l), "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));  // (here, not among the products, where the scores would have to stay)
     };
     // The second product of place p and the first one of place p + 1, next to which the codes behind them are unpacked: eight slices, whose fragments are read
     // one slice ahead.  The order is that of the statements between scheduling barriers.
@@ -387,10 +399,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
         int most = 0;  // bits of the row's largest finite element
         {
             const int at = min(row, rows - 1);
-            const T *src = static_cast<const T *>(a.q) + (long long)(q0 + at / a.group) * a.q_token + (hk * a.group + at % a.group) * a.q_head + 8 * h;
+            const T *src = static_cast<const T *>(a.q) + (long long)(q0 + at / a.group) * a.q_token + (hk * a.group + at % a.group) * a.q_head + (little ? D / 2 : 8) * h;
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                const u32x4 raw = *reinterpret_cast<const u32x4 *>(src + 16 * i);
+                const u32x4 raw = *reinterpret_cast<const u32x4 *>(src + (little ? 8 : 16) * i);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     if constexpr (__is_same(T, f16))
@@ -430,14 +442,78 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
     }
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) o[e] = v16f{};
-    if (n_tiles > 0) {
+    if (little) {
+        // Tiles of 32 keys, a wave's own, which go from the cache into the products as they are: lane n, h has key n's dwords STEPS h on, and for the second
+        // product elements D / 32 n on of the four keys 8 u + 4 h (+ 16 in the second half).
+        const int tiles32 = __builtin_amdgcn_readfirstlane(max((sees(first + kLittle - 1) + 31) / 32, 0));
+        const int from32 = (int)((unsigned)part * (unsigned)tiles32 / (unsigned)n_parts);
+        int t = (int)((unsigned)(part + 1) * (unsigned)tiles32 / (unsigned)n_parts) - 1 - wave;
+        const auto pages_of = [&](int t, int u) __attribute__((always_inline)) { return (unsigned)table[min((max(t, 0) * 32 + 16 * u) >> a.lg_page, last_page)]; };
+        const auto head_of = [&](unsigned page) __attribute__((always_inline)) { return cache + (uint64_t)(page >= (unsigned)a.pages ? 0u : page) * page_bytes; };
+        const auto place_of = [&](int t, int u) { return (max(t, 0) * 32 + 16 * u) & (P - 1); };
+        uint32_t k[STEPS], v[2][2][2];
+        unsigned page[2];
+        const auto load_k = [&](int t) __attribute__((always_inline)) {  // (of a tile that is not there: the first page, which all waves have at hand)
+            const bool any = t >= from32;
+            const uint8_t *const head0 = any ? head_of(page[0]) : cache, *const head1 = any ? head_of(page[1]) : cache;
+            const uint8_t *const head = n & 16 ? head1 : head0;
+            const int j = (n & 16 ? place_of(t, 1) : place_of(t, 0)) + (n & 15);
+            bad |= any && (page[0] >= (unsigned)a.pages || page[1] >= (unsigned)a.pages);
+#pragma unroll
+            for (int i = 0; i < STEPS; i += 4) {
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(head + j * (D / 2) + h * (D / 4) + 4 * i);
+                k[i] = x[0], k[i + 1] = x[1], k[i + 2] = x[2], k[i + 3] = x[3];
+            }
+            wk = *reinterpret_cast<const uint32_t *>(head + P * D + 4 * j);
+            wv = *reinterpret_cast<const uint32_t *>(head + P * (D + 4) + 4 * j);
+        };
+        const auto load_v = [&](int t, const unsigned (&page)[2]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const buf_t b = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(head_of(page[u])), 0, t >= from32 ? kv4_head_bytes(P, D) : 0, 0x00027000);
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const int at = (2 * g + h) * (2 * D) + (n >> 1) * (D / 8) + (D == 128 ? 4 * (n & 1) : 0), piece = (P + place_of(t, u)) * (D / 2);
+                    v[u][g][0] = __builtin_amdgcn_raw_buffer_load_b32(b, at, piece, 0);
+                    v[u][g][1] = __builtin_amdgcn_raw_buffer_load_b32(b, at + D / 16, piece, 0);
+                }
+            }
+        };
+        page[0] = pages_of(t, 0), page[1] = pages_of(t, 1);
+        load_k(t);
+        load_v(t, page);
+        for (; t >= from32; t -= kWaves) {
+            const unsigned of_next[2] = {pages_of(t - kWaves, 0), pages_of(t - kWaves, 1)};
+            const uint32_t zz = (wk & 15u) * 0x10001u;
+            s[0] = mfma32(__builtin_bit_cast(vec<f16, 8>, u32x4{zz, zz, 0, 0}), q[STEPS], v16f{});
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) s[0] = mfma32(__builtin_bit_cast(vec<f16, 8>, halves8(k[i])), q[i], s[0]);
+            const bool far = scales(wave, n);
+            page[0] = of_next[0], page[1] = of_next[1];
+            load_k(t - kWaves);
+            softmax(wave, 32 * t, far, std::integral_constant<int, 1>{});
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                u32x4 x[2][2];  // of four keys: pairs of them, elements
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const uint2 z4 = *reinterpret_cast<const uint2 *>(&s_zv[wave][16 * u + 8 * g + 4 * h]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) x[g][i] = halves8(D == 128 ? v[u][g][i] : v[u][g][i] >> (8 * (n & 1)), i ? z4.y : z4.x);
+                }
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) o[e] = mfma32(__builtin_bit_cast(vec<f16, 8>, u32x4{x[0][0][e], x[0][1][e], x[1][0][e], x[1][1][e]}), w[u], o[e]);
+            }
+            load_v(t - kWaves, page);
+        }
+    } else if (n_tiles > 0) {
         // the first two tiles' keys and scales, the first one's values
         unsigned page = page_of(0);
         load_keys(0, page);
         load_values(0, page);
 #pragma unroll
         for (int i = 0; i < DW; ++i) unpack_keys(0, i);
-        scales(0);
+        s_far[0][wave] = scales(0, keys_w + column);
         page = page_of(1);
         load_keys(1, page);
         meet();  // (a wave writes the zero points that it reads, but the compiler has to know)
@@ -446,7 +522,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
         load_values(1, page);
 #pragma unroll
         for (int i = 0; i < DW; ++i) unpack_keys(1, i);
-        scales(1);
+        s_far[1][wave] = scales(1, keys_w + column);
         page = page_of(2);
         load_keys(2, page);
         meet();
@@ -458,7 +534,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
                 for (int i = 0; i < STEPS; ++i) s[u] = mfma32(keys(0, u, i), q[i], s[u]);
             }
             for (int p = 0; p < n_tiles; ++p) {
-                softmax(p);
+                const v4i far = *reinterpret_cast<const v4i *>(s_far[p & 3]);
+                softmax(p & 3, (t_first - p) * kKeys, __builtin_amdgcn_readfirstlane(far[0] | far[1] | far[2] | far[3]), std::integral_constant<int, 2>{});
                 meet();  // (what the next products read is there, and all waves are done with what they write over)
                 products(p);
                 next_loads(p, page);
@@ -477,11 +554,100 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
     const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, l), __builtin_bit_cast(unsigned, l), false, false);
     l = __builtin_bit_cast(float, (unsigned)both[0]) + __builtin_bit_cast(float, (unsigned)both[1]);
     if (s_bad) l = __builtin_nanf("");
+    // Every part leaves its maxima, sums and results, past the L2s; the last to arrive at the tile's ticket joins them, in their order
+    const auto last_to_arrive = [&]() __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (threadIdx.x == 0) {
+            const unsigned arrived = __hip_atomic_fetch_add(a.tickets + whole, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_last = arrived == (unsigned)n_parts - 1;
+            if (s_last) __hip_atomic_store(a.tickets + whole, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        return __builtin_amdgcn_readfirstlane(s_last) != 0;
+    };
+    // what a maximum that moves to top takes off, as the root of it: a sum takes it in two steps (as above)
+    const auto root_of = [](float m, float top) { return m == top ? 1.0f : __builtin_amdgcn_exp2f((m - top) * 0.5f); };
+    if (little) {
+        // the waves' results, and those of the parts: a thread has pieces of four elements of the rows
+        if (h == 0) s_lv[wave][n] = m, s_rv[wave][n] = l;
+        meet();
+        const auto top_of = [&](int r) { return fmaxf(fmaxf(s_lv[0][r], s_lv[1][r]), fmaxf(s_lv[2][r], s_lv[3][r])); };
+        {
+            const float root = root_of(m, top_of(n)), by = root * root;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                vec<float, D / 32> x;
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) x[e] = o[e][i] * by;
+                *reinterpret_cast<vec<float, D / 32> *>(&s_pool.o[wave][n][(D / 32) * (8 * (i >> 2) + 4 * h + (i & 3))]) = x;
+            }
+        }
+        meet();
+        constexpr int PIECES = D / 32, STRIDE = D + 4;
+        const auto write = [&](int r, int c, v4f x, float l) __attribute__((always_inline)) {
+            const float by = l == 0.0f ? 0.0f : 1.0f / l;
+            vec<T, 4> y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (T)(x[e] * (e & 1 ? 0x1p20f : 0x1p24f) * by);
+            const int at = first + r;
+            if (at < rows) *reinterpret_cast<vec<T, 4> *>(static_cast<T *>(a.out) + ((size_t)(q0 + at / a.group) * a.Hq + hk * a.group + at % a.group) * D + 4 * c) = y;
+        };
+        const auto place = [&](int i, int &r, int &c) { r = ((int)threadIdx.x + 64 * kWaves * i) / (D / 4), c = ((int)threadIdx.x + 64 * kWaves * i) % (D / 4); };
+        const auto at_part = [&](int p, int r, int c) { return first + r < rows && p < n_parts ? (p * FLOATS + r * STRIDE + 4 * c) * 4 : n_parts * FLOATS * 4; };
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            int r, c;
+            place(i, r, c);
+            const float top = top_of(r);
+            v4f x{};
+            float sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) {
+                const float root = root_of(s_lv[k][r], top);
+                sum += s_rv[k][r] * root * root;
+                x += *reinterpret_cast<const v4f *>(&s_pool.o[k][r][4 * c]);
+            }
+            if (n_parts == 1) {
+                write(r, c, x, sum);
+                continue;
+            }
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), left_parts, at_part(part, r, c), 0, kShared);
+            if (c == 0) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v4f{top, sum, 0.0f, 0.0f}), left_parts, at_part(part, r, D / 4), 0, kShared);
+        }
+        if (n_parts == 1 || !last_to_arrive()) return;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            int r, c;
+            place(i, r, c);
+            float top = -__builtin_inff(), sum = 0.0f;
+            v4f x{};
+            for (int p = 0; p < n_parts; p += 4) {
+                v4f ml[4], y[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    ml[k] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(left_parts, at_part(p + k, r, D / 4), 0, kShared));
+                    y[k] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(left_parts, at_part(p + k, r, c), 0, kShared));
+                    if (p + k >= n_parts) ml[k][0] = -__builtin_inff();
+                }
+                const float now = fmaxf(fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0])), top), old = root_of(top, now);
+                top = now;
+                sum = sum * old * old;
+                x *= old * old;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float by = root_of(ml[k][0], now);
+                    sum += ml[k][1] * by * by;
+                    x += y[k] * (by * by);
+                }
+            }
+            write(r, c, x, sum);
+        }
+        return;
+    }
     if (n_parts == 1) {
         if (row < rows) write_row();
         return;
     }
-    // Every part leaves its maxima, sums and results, past the L2s; the last to arrive at the tile's ticket joins them, in their order
 #pragma unroll
     for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -489,14 +655,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v4f{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]}), left_parts,
                                                    part_at(part, 4 * e + i), 0, kShared);
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v4f{m, l, 0.0f, 0.0f}), left_parts, part_at(part, D / 8), 0, kShared);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (threadIdx.x == 0) {
-        const unsigned arrived = __hip_atomic_fetch_add(a.tickets + whole, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = arrived == (unsigned)n_parts - 1;
-        if (s_last) __hip_atomic_store(a.tickets + whole, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (!__builtin_amdgcn_readfirstlane(s_last)) return;
+    if (!last_to_arrive()) return;
     m = -__builtin_inff();
     l = 0.0f;
 #pragma unroll
@@ -507,8 +666,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) x[i] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(left_parts, part_at(p, i), 0, kShared));
         const float now = fmaxf(m, ml[0]);
-        const float old = m == now ? 1.0f : __builtin_amdgcn_exp2f((m - now) * 0.5f);
-        const float by = ml[0] == now ? 1.0f : __builtin_amdgcn_exp2f((ml[0] - now) * 0.5f);
+        const float old = root_of(m, now), by = root_of(ml[0], now);
         m = now;
         l = l * old * old + ml[1] * by * by;
 #pragma unroll
