@@ -37,7 +37,7 @@ struct ChunkArgs {
     float scale_log2;
 };
 
-constexpr int kFew = 64, kLittle = 32, kKeys = 64, kWaves = 4, kRows = 32 * kWaves, kMostParts = 32;
+constexpr int kFew = 64, kLittle = 32, kLeast = 4, kKeys = 64, kWaves = 4, kRows = 32 * kWaves, kMostParts = 32;
 constexpr float kWeightBits = 6.0f;
 typedef f16 f16x2v __attribute__((ext_vector_type(2)));
 
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
             const int most = a.slots / a.Hkv;  // parts of a kv head
             int size = max(up(__builtin_amdgcn_readlane(sums_up_to(mine * min(keys, 1 << 16)), 63), most), 1), sum;
             do {
-                parts = min(max(up(keys, little ? size : max(size, 2)), 1), kMostParts);
+                parts = min(max(up(keys, max(size, little ? kLeast : 2)), 1), kMostParts);
                 upto = sums_up_to(mine * parts);
                 sum = __builtin_amdgcn_readlane(upto, 63);
                 size += up(size, 8);
@@ -388,8 +388,53 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
     const auto left_parts = __builtin_amdgcn_make_buffer_rsrc(a.parts + (size_t)whole * FLOATS, 0, n_parts * FLOATS * 4, 0x00027000);
     const auto part_at = [&](int p, int piece) { return row < rows ? (p * FLOATS + (piece * 64 * kWaves + (int)threadIdx.x) * 4) * 4 : n_parts * FLOATS * 4; };
 
+    // Tiles of few rows: of 32 keys, a wave's own, which go from the cache into the products as they are: lane n, h has key n's dwords STEPS h on, and for
+    // the second product elements D / 32 n on of the four keys 8 g + 4 h of both halves.
+    const int tiles32 = __builtin_amdgcn_readfirstlane(max((sees(first + kLittle - 1) + 31) / 32, 0));
+    const int from32 = (int)((unsigned)part * (unsigned)tiles32 / (unsigned)n_parts);
+    int t = (int)((unsigned)(part + 1) * (unsigned)tiles32 / (unsigned)n_parts) - 1 - wave;
+    const auto pages_of = [&](int t, int u) __attribute__((always_inline)) { return (unsigned)table[min((max(t, 0) * 32 + 16 * u) >> a.lg_page, last_page)]; };
+    const auto head_of = [&](unsigned page) __attribute__((always_inline)) { return cache + (uint64_t)(page >= (unsigned)a.pages ? 0u : page) * page_bytes; };
+    const auto place_of = [&](int t, int u) { return (max(t, 0) * 32 + 16 * u) & (P - 1); };
+    uint32_t k[STEPS], v[2][2][2];
+    unsigned pages[2];
+    const auto load_own = [&](int t) __attribute__((always_inline)) {  // (of a tile that is not there: the first page's keys, which all waves have at hand)
+        const bool any = t >= from32;
+        const uint8_t *const head0 = any ? head_of(pages[0]) : cache, *const head1 = any ? head_of(pages[1]) : cache, *const head = n & 16 ? head1 : head0;
+        const int j = (n & 16 ? place_of(t, 1) : place_of(t, 0)) + (n & 15);
+        bad |= any && (pages[0] >= (unsigned)a.pages || pages[1] >= (unsigned)a.pages);
+#pragma unroll
+        for (int i = 0; i < STEPS; i += 4) {
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(head + j * (D / 2) + h * (D / 4) + 4 * i);
+            k[i] = x[0], k[i + 1] = x[1], k[i + 2] = x[2], k[i + 3] = x[3];
+        }
+        wk = *reinterpret_cast<const uint32_t *>(head + P * D + 4 * j);
+        wv = *reinterpret_cast<const uint32_t *>(head + P * (D + 4) + 4 * j);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const buf_t b = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(u ? head1 : head0), 0, any ? kv4_head_bytes(P, D) : 0, 0x00027000);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const int at = (2 * g + h) * (2 * D) + (n >> 1) * (D / 8) + (D == 128 ? 4 * (n & 1) : 0), piece = (P + place_of(t, u)) * (D / 2);
+                v[u][g][0] = __builtin_amdgcn_raw_buffer_load_b32(b, at, piece, 0);
+                v[u][g][1] = __builtin_amdgcn_raw_buffer_load_b32(b, at + D / 16, piece, 0);
+            }
+        }
+    };
+    // (the first loads, before those of the queries)
+    unsigned page = 0;
+    if (little) {
+        pages[0] = pages_of(t, 0), pages[1] = pages_of(t, 1);
+        load_own(t);
+        pages[0] = pages_of(t - kWaves, 0), pages[1] = pages_of(t - kWaves, 1);
+    } else if (n_tiles > 0) {
+        page = page_of(0);
+        load_keys(0, page);
+        load_values(0, page);
+    }
+
     if (threadIdx.x == 0) s_bad = s_top = 0;
-    if (threadIdx.x < kKeys) s_none[threadIdx.x] = 0.0f;
+    s_none[lane] = 0.0f;
     // Queries, in the keys' order within 8 elements (a pair of a dword's nibbles is four apart), over a power of two for the block that brings its
     // largest element to 4 .. 8, what meets even pairs times 16: what is above 2^-17 of the largest is held exactly.  A row whose largest element is below
     // 2^-8 of the block's has a power of its own, and a factor for its scores.  A last operand holds what the zero points are multiplied with, minus 16 times
@@ -416,11 +461,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
         }
         const auto both = __builtin_amdgcn_permlane32_swap((unsigned)most, (unsigned)most, false, false);
         most = max((int)both[0], (int)both[1]);
-        meet();
-        if (row < rows) atomicMax(&s_top, most);
-        meet();
+        int top_bits = __builtin_amdgcn_readlane(lanes_up_to(row < rows ? most : 0, [](int x, int y) { return max(x, y); }), 63);
+        if (!little) {
+            meet();
+            if (lane == 0) atomicMax(&s_top, top_bits);
+            meet();
+            top_bits = __builtin_amdgcn_readfirstlane(s_top);
+        }
         const auto exponent = [](int bits) { return max(bits >> 23, 1) - 129; };
-        const int top = exponent(__builtin_amdgcn_readfirstlane(s_top)), own = most && exponent(most) < top - 8 ? exponent(most) : top;
+        const int top = exponent(top_bits), own = most && exponent(most) < top - 8 ? exponent(most) : top;
         q_scale = fminf(fmaxf(q_scale * 0x1p20f * power_of_two(max(top, -126)), 0x1p-126f), 0x1p127f);
         s_row[row - first] = power_of_two(max(own - top, -126));
         uneven = __any(own != top);
@@ -443,54 +492,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) o[e] = v16f{};
     if (little) {
-        // Tiles of 32 keys, a wave's own, which go from the cache into the products as they are: lane n, h has key n's dwords STEPS h on, and for the second
-        // product elements D / 32 n on of the four keys 8 u + 4 h (+ 16 in the second half).
-        const int tiles32 = __builtin_amdgcn_readfirstlane(max((sees(first + kLittle - 1) + 31) / 32, 0));
-        const int from32 = (int)((unsigned)part * (unsigned)tiles32 / (unsigned)n_parts);
-        int t = (int)((unsigned)(part + 1) * (unsigned)tiles32 / (unsigned)n_parts) - 1 - wave;
-        const auto pages_of = [&](int t, int u) __attribute__((always_inline)) { return (unsigned)table[min((max(t, 0) * 32 + 16 * u) >> a.lg_page, last_page)]; };
-        const auto head_of = [&](unsigned page) __attribute__((always_inline)) { return cache + (uint64_t)(page >= (unsigned)a.pages ? 0u : page) * page_bytes; };
-        const auto place_of = [&](int t, int u) { return (max(t, 0) * 32 + 16 * u) & (P - 1); };
-        uint32_t k[STEPS], v[2][2][2];
-        unsigned page[2];
-        const auto load_k = [&](int t) __attribute__((always_inline)) {  // (of a tile that is not there: the first page, which all waves have at hand)
-            const bool any = t >= from32;
-            const uint8_t *const head0 = any ? head_of(page[0]) : cache, *const head1 = any ? head_of(page[1]) : cache;
-            const uint8_t *const head = n & 16 ? head1 : head0;
-            const int j = (n & 16 ? place_of(t, 1) : place_of(t, 0)) + (n & 15);
-            bad |= any && (page[0] >= (unsigned)a.pages || page[1] >= (unsigned)a.pages);
-#pragma unroll
-            for (int i = 0; i < STEPS; i += 4) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(head + j * (D / 2) + h * (D / 4) + 4 * i);
-                k[i] = x[0], k[i + 1] = x[1], k[i + 2] = x[2], k[i + 3] = x[3];
-            }
-            wk = *reinterpret_cast<const uint32_t *>(head + P * D + 4 * j);
-            wv = *reinterpret_cast<const uint32_t *>(head + P * (D + 4) + 4 * j);
-        };
-        const auto load_v = [&](int t, const unsigned (&page)[2]) __attribute__((always_inline)) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const buf_t b = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(head_of(page[u])), 0, t >= from32 ? kv4_head_bytes(P, D) : 0, 0x00027000);
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const int at = (2 * g + h) * (2 * D) + (n >> 1) * (D / 8) + (D == 128 ? 4 * (n & 1) : 0), piece = (P + place_of(t, u)) * (D / 2);
-                    v[u][g][0] = __builtin_amdgcn_raw_buffer_load_b32(b, at, piece, 0);
-                    v[u][g][1] = __builtin_amdgcn_raw_buffer_load_b32(b, at + D / 16, piece, 0);
-                }
-            }
-        };
-        page[0] = pages_of(t, 0), page[1] = pages_of(t, 1);
-        load_k(t);
-        load_v(t, page);
         for (; t >= from32; t -= kWaves) {
-            const unsigned of_next[2] = {pages_of(t - kWaves, 0), pages_of(t - kWaves, 1)};
+            uint32_t v_now[2][2][2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v_now[i >> 2][i >> 1 & 1][i & 1] = v[i >> 2][i >> 1 & 1][i & 1];
             const uint32_t zz = (wk & 15u) * 0x10001u;
             s[0] = mfma32(__builtin_bit_cast(vec<f16, 8>, u32x4{zz, zz, 0, 0}), q[STEPS], v16f{});
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) s[0] = mfma32(__builtin_bit_cast(vec<f16, 8>, halves8(k[i])), q[i], s[0]);
             const bool far = scales(wave, n);
-            page[0] = of_next[0], page[1] = of_next[1];
-            load_k(t - kWaves);
+            load_own(t - kWaves);
+            pages[0] = pages_of(t - 2 * kWaves, 0), pages[1] = pages_of(t - 2 * kWaves, 1);
             softmax(wave, 32 * t, far, std::integral_constant<int, 1>{});
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -499,18 +511,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
                 for (int g = 0; g < 2; ++g) {
                     const uint2 z4 = *reinterpret_cast<const uint2 *>(&s_zv[wave][16 * u + 8 * g + 4 * h]);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) x[g][i] = halves8(D == 128 ? v[u][g][i] : v[u][g][i] >> (8 * (n & 1)), i ? z4.y : z4.x);
+                    for (int i = 0; i < 2; ++i) x[g][i] = halves8(D == 128 ? v_now[u][g][i] : v_now[u][g][i] >> (8 * (n & 1)), i ? z4.y : z4.x);
                 }
 #pragma unroll
                 for (int e = 0; e < D / 32; ++e) o[e] = mfma32(__builtin_bit_cast(vec<f16, 8>, u32x4{x[0][0][e], x[0][1][e], x[1][0][e], x[1][1][e]}), w[u], o[e]);
             }
-            load_v(t - kWaves, page);
         }
     } else if (n_tiles > 0) {
         // the first two tiles' keys and scales, the first one's values
-        unsigned page = page_of(0);
-        load_keys(0, page);
-        load_values(0, page);
 #pragma unroll
         for (int i = 0; i < DW; ++i) unpack_keys(0, i);
         s_far[0][wave] = scales(0, keys_w + column);
@@ -549,11 +557,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
             }
         }
     }
-    if (bad) s_bad = 1;
-    meet();
+    if (!little) {
+        if (bad) s_bad = 1;
+        meet();
+        bad = s_bad;
+    }
     const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, l), __builtin_bit_cast(unsigned, l), false, false);
     l = __builtin_bit_cast(float, (unsigned)both[0]) + __builtin_bit_cast(float, (unsigned)both[1]);
-    if (s_bad) l = __builtin_nanf("");
+    if (bad) l = __builtin_nanf("");
     // Every part leaves its maxima, sums and results, past the L2s; the last to arrive at the tile's ticket joins them, in their order
     const auto last_to_arrive = [&]() __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -570,17 +581,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
     if (little) {
         // the waves' results, and those of the parts: a thread has pieces of four elements of the rows
         if (h == 0) s_lv[wave][n] = m, s_rv[wave][n] = l;
-        meet();
         const auto top_of = [&](int r) { return fmaxf(fmaxf(s_lv[0][r], s_lv[1][r]), fmaxf(s_lv[2][r], s_lv[3][r])); };
-        {
-            const float root = root_of(m, top_of(n)), by = root * root;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                vec<float, D / 32> x;
+        for (int i = 0; i < 16; ++i) {
+            vec<float, D / 32> x;
 #pragma unroll
-                for (int e = 0; e < D / 32; ++e) x[e] = o[e][i] * by;
-                *reinterpret_cast<vec<float, D / 32> *>(&s_pool.o[wave][n][(D / 32) * (8 * (i >> 2) + 4 * h + (i & 3))]) = x;
-            }
+            for (int e = 0; e < D / 32; ++e) x[e] = o[e][i];
+            *reinterpret_cast<vec<float, D / 32> *>(&s_pool.o[wave][n][(D / 32) * (8 * (i >> 2) + 4 * h + (i & 3))]) = x;
         }
         meet();
         constexpr int PIECES = D / 32, STRIDE = D + 4;
@@ -605,7 +612,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
             for (int k = 0; k < kWaves; ++k) {
                 const float root = root_of(s_lv[k][r], top);
                 sum += s_rv[k][r] * root * root;
-                x += *reinterpret_cast<const v4f *>(&s_pool.o[k][r][4 * c]);
+                x += *reinterpret_cast<const v4f *>(&s_pool.o[k][r][4 * c]) * (root * root);
             }
             if (n_parts == 1) {
                 write(r, c, x, sum);
