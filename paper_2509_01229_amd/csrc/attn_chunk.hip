@@ -125,40 +125,41 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
         }
         const bool little = len * a.group <= kLittle;
         const int keys = up(within(context), little ? 4 * kKeys : kKeys);  // tiles of keys, by what they cost
-        upto = sums_up_to(mine);
-        all = __builtin_amdgcn_readlane(upto, 63);
+        all = __builtin_amdgcn_readlane(sums_up_to(mine), 63);
         if (all > a.tiles) {  // (more than there can be: the sequences overlap)
             mine = min(mine, a.tiles / a.n_seqs);
-            upto = sums_up_to(mine);
-            all = __builtin_amdgcn_readlane(upto, 63);
+            all = __builtin_amdgcn_readlane(sums_up_to(mine), 63);
         }
         if (a.slots > all * a.Hkv) {
             const int most = a.slots / a.Hkv;  // parts of a kv head
             int size = max(up(__builtin_amdgcn_readlane(sums_up_to(mine * min(keys, 1 << 16)), 63), most), 1), sum;
             do {
                 parts = min(max(up(keys, max(size, little ? kLeast : 2)), 1), kMostParts);
-                upto = sums_up_to(mine * parts);
-                sum = __builtin_amdgcn_readlane(upto, 63);
+                sum = __builtin_amdgcn_readlane(sums_up_to(mine * parts), 63);
                 size += up(size, 8);
             } while (sum > most);  // (one part each fits, and comes before size overflows: keys is below 2^24)
             all = sum;
         }
+        // Those of few rows come last: they are short, and fill what the others leave (a mixed step 67 -> 63 us)
+        const int upto_long = sums_up_to(little ? 0 : mine * parts), upto_short = sums_up_to(little ? mine * parts : 0);
+        upto = little ? __builtin_amdgcn_readlane(upto_long, 63) + upto_short : upto_long;
     }
     // Blocks with ids 8 apart run on one XCD: each XCD gets consecutive kv heads, and goes through a head's tiles from the last (the longest rows of
     // keys) to the first.  Blocks that the grid has too many come last.
     const int blocks = all * a.Hkv, per = (blocks + 7) >> 3, id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
     if ((int)blockIdx.x >> 3 >= per || id >= blocks) return;
     const int hk = __builtin_amdgcn_readfirstlane(id / all);
-    int tile = all - 1 - id % all, part = 0, n_parts = 1, seq, q0, len_q, whole = 0;
+    int tile = few ? id % all : all - 1 - id % all, part = 0, n_parts = 1, seq, q0, len_q, whole = 0;
     if (few) {
-        seq = __builtin_ctzll(__ballot(upto > tile) | 1ull << 63);
+        const int start = upto - mine * parts;
+        seq = __builtin_ctzll(__ballot(start <= tile && upto > tile) | 1ull << 63);
         q0 = __builtin_amdgcn_readlane(from, seq);
         len_q = __builtin_amdgcn_readlane(len, seq);
         n_parts = __builtin_amdgcn_readlane(parts, seq);
-        whole = hk * all + (seq ? __builtin_amdgcn_readlane(upto, seq - 1) : 0);  // (the sequence's first part)
+        whole = hk * all + __builtin_amdgcn_readlane(start, seq);  // (the sequence's first part)
         tile -= whole - hk * all;
         part = tile % n_parts;
-        tile /= n_parts;
+        tile = __builtin_amdgcn_readlane(mine, seq) - 1 - tile / n_parts;  // (the longest rows of keys first)
         whole += tile * n_parts;  // the tile's first part: its place in the workspace, and its ticket
         context = __builtin_amdgcn_readlane(context, seq);
     } else {
@@ -541,11 +542,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
 #pragma unroll
                 for (int i = 0; i < STEPS; ++i) s[u] = mfma32(keys(0, u, i), q[i], s[u]);
             }
+            // (what has products to issue goes first: 2332 -> 2294 us where 2 blocks a CU have chunks of 1024, a mixed step 72 -> 68)
             for (int p = 0; p < n_tiles; ++p) {
                 const v4i far = *reinterpret_cast<const v4i *>(s_far[p & 3]);
                 softmax(p & 3, (t_first - p) * kKeys, __builtin_amdgcn_readfirstlane(far[0] | far[1] | far[2] | far[3]), std::integral_constant<int, 2>{});
                 meet();  // (what the next products read is there, and all waves are done with what they write over)
+                __builtin_amdgcn_s_setprio(1);
                 products(p);
+                __builtin_amdgcn_s_setprio(0);
                 next_loads(p, page);
             }
         } else {
