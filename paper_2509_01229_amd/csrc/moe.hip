@@ -25,23 +25,25 @@ struct DispatchArgs {
     float *row_scales;
     int *offsets, *places;
     long long x_row;  // bytes
-    int tokens, each, n_experts, pieces;
+    int tokens, each, n_experts, pieces, segments;
 };
 
 __device__ __forceinline__ int lanes_set_below(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u)); }
 
-// The row of a token to its places
-__device__ __forceinline__ void copy_row(const DispatchArgs &a, int token, const int *places, int thread, int threads)
+// The row of a token to its places, of which lane j of each wave has the j-th (so that no store waits for one to be loaded)
+__device__ __forceinline__ void copy_row(const DispatchArgs &a, int token, int place, int thread, int threads)
 {
     const u32x4 *const from = reinterpret_cast<const u32x4 *>(a.x + token * a.x_row);
-    for (int i = thread; i < a.pieces; i += threads) {
-        const u32x4 x = from[i];
+    if (a.scales && thread < a.each && place >= 0) a.row_scales[place] = a.scales[token];
+    for (int i = thread; i - (thread & 63) < a.pieces; i += threads) {  // (whole waves: lanes hold what others take)
+        const bool any = i < a.pieces;
+        u32x4 x{};
+        if (any) x = from[i];
         for (int j = 0; j < a.each; ++j) {
-            const int place = places[j];
-            if (place >= 0) reinterpret_cast<u32x4 *>(a.rows)[(size_t)place * a.pieces + i] = x;
+            const int to = __builtin_amdgcn_readlane(place, j);
+            if (to >= 0 && any) reinterpret_cast<u32x4 *>(a.rows)[(size_t)to * a.pieces + i] = x;
         }
     }
-    if (a.scales && thread < a.each && places[thread] >= 0) a.row_scales[places[thread]] = a.scales[token];
 }
 
 // Few pairs: block t < tokens counts the places of its pairs and copies the row, the last block counts the experts' pairs
@@ -88,48 +90,72 @@ __global__ __launch_bounds__(kSmallThreads) void moe_dispatch_small_kernel(const
         }
     }
     __syncthreads();
-    copy_row(a, token, s_places, threadIdx.x, kSmallThreads);
+    copy_row(a, token, lane < a.each ? s_places[lane] : -1, threadIdx.x, kSmallThreads);
 }
 
-// Many pairs: block e numbers the pairs of expert e
-constexpr int kSortThreads = 1024;
+// Many pairs: each expert has `segments` blocks, which number its pairs of a segment each (of whole batches).  All of them look at all pairs: 262 KB for
+// 65528, at what a CU gets from its L2; so that is done once, with sums of the lanes' own, and only the segment is looked at again.  (65528 pairs of 64 experts:
+// a load for every 64 pairs, one after the other, twice, by a block for each expert 41 us; 16 loads together 15.6; four blocks an expert 12.6)
+constexpr int kSortThreads = 1024, kBatch = 16, kBatchPairs = kBatch * kSortThreads;
 __global__ __launch_bounds__(kSortThreads) void moe_places_kernel(const DispatchArgs a)
 {
     constexpr int WAVES = kSortThreads / 64;
-    __shared__ int s_less[WAVES], s_own[WAVES];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), e = blockIdx.x, pairs = a.tokens * a.each;
-    // a wave takes consecutive pairs, 64 at a time
-    const int each = ((pairs + WAVES - 1) / WAVES + 63) / 64 * 64, from = (int)std::min<long long>((long long)wave * each, pairs), to = (int)std::min<long long>((long long)from + each, pairs);
-    int less = 0, own = 0;
-    for (int i = from; i < to; i += 64) {
-        const int id = i + lane < to ? a.experts[i + lane] : -1;
-        less += __popcll(__ballot(id >= 0 && id < e));
-        own += __popcll(__ballot(id == e));
+    __shared__ int s_sum[3][WAVES], s_own[2][WAVES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), pairs = a.tokens * a.each;
+    const int e = blockIdx.x % (unsigned)a.n_experts, segment = blockIdx.x / (unsigned)a.n_experts, batches = (pairs + kBatchPairs - 1) / kBatchPairs;
+    const long long from = (long long)segment * batches / a.segments * kBatchPairs, to = std::min<long long>((segment + 1LL) * batches / a.segments * kBatchPairs, pairs);
+    // 16 pairs of the thread's, `step` apart (-1: not there)
+    const auto batch = [&](long long at, int step, int (&ids)[kBatch]) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i, at += step) ids[i] = at < pairs ? a.experts[at] : -1;
+    };
+    int ids[kBatch], less = 0, before = 0, own = 0;
+    for (long long i0 = 0; i0 < pairs; i0 += kBatchPairs) {
+        batch(i0 + threadIdx.x, kSortThreads, ids);
+        int here = 0;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) less += (unsigned)ids[i] < (unsigned)e, here += ids[i] == e;
+        own += here;
+        before += i0 < from ? here : 0;
     }
-    if (lane == 0) s_less[wave] = less, s_own[wave] = own;
+    const auto of_wave = [](int x) { return __builtin_amdgcn_readlane(sums_up_to(x), 63); };
+    less = of_wave(less), before = of_wave(before), own = of_wave(own);
+    if (lane == 0) s_sum[0][wave] = less, s_sum[1][wave] = before, s_sum[2][wave] = own;
     __syncthreads();
-    less = own = 0;
-    int place = 0;
-    for (int w = 0; w < WAVES; ++w) {
-        less += s_less[w];
-        if (w < wave) place += s_own[w];
-        own += s_own[w];
-    }
-    place += less;
-    if (threadIdx.x == 0) a.offsets[e] = less;
-    if (threadIdx.x == 0 && e == a.n_experts - 1) a.offsets[e + 1] = less + own;
-    for (int i = from; i < to; i += 64) {
-        const int id = i + lane < to ? a.experts[i + lane] : a.n_experts;
-        const uint64_t mine = __ballot(id == e);
-        if (id == e) a.places[i + lane] = place + lanes_set_below(mine);
-        if (e == 0 && (unsigned)id >= (unsigned)a.n_experts && i + lane < to) a.places[i + lane] = -1;
-        place += __popcll(mine);
+    less = before = own = 0;
+    for (int w = 0; w < WAVES; ++w) less += s_sum[0][w], before += s_sum[1][w], own += s_sum[2][w];
+    if (threadIdx.x == 0 && segment == 0) a.offsets[e] = less;
+    if (threadIdx.x == 0 && segment == 0 && e == a.n_experts - 1) a.offsets[e + 1] = less + own;
+    int first = less + before, turn = 0;
+    for (long long i0 = from; i0 < to; i0 += kBatchPairs, turn ^= 1) {
+        // a wave's pairs are consecutive
+        const long long at = i0 + wave * (kBatchPairs / WAVES) + lane;
+        batch(at, 64, ids);
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) mine += __popcll(__ballot(ids[i] == e));
+        if (lane == 0) s_own[turn][wave] = mine;
+        __syncthreads();
+        int place = first;
+        for (int w = 0; w < WAVES; ++w) {
+            const int n = s_own[turn][w];
+            if (w < wave) place += n;
+            first += n;
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const uint64_t mask = __ballot(ids[i] == e);
+            if (ids[i] == e) a.places[at + 64 * i] = place + lanes_set_below(mask);
+            if (e == 0 && (unsigned)ids[i] >= (unsigned)a.n_experts && at + 64 * i < to) a.places[at + 64 * i] = -1;
+            place += __popcll(mask);
+        }
     }
 }
 constexpr int kCopyThreads = 256;
 __global__ __launch_bounds__(kCopyThreads) void moe_copy_kernel(const DispatchArgs a)
 {
-    copy_row(a, blockIdx.x, a.places + (long long)blockIdx.x * a.each, threadIdx.x, kCopyThreads);
+    const int lane = threadIdx.x & 63;
+    copy_row(a, blockIdx.x, lane < a.each ? a.places[(long long)blockIdx.x * a.each + lane] : -1, threadIdx.x, kCopyThreads);
 }
 
 struct CombineArgs {
@@ -148,24 +174,49 @@ __device__ __forceinline__ vec<T, 8> piece_of(const CombineArgs &a, int place, i
     return reinterpret_cast<const vec<T, 8> *>(static_cast<const T *>(a.y) + place * a.y_row)[piece];
 }
 
+// Pair j's place, which is -1 where it has no row, and weight, which is then 0 (whatever is there)
+struct Pair {
+    int place;
+    float weight;
+};
+__device__ __forceinline__ Pair pair_of(const CombineArgs &a, int token, int j)
+{
+    Pair p{-1, 0.0f};
+    if (j < a.each) {
+        const long long at = (long long)token * a.each + j;
+        p.place = a.places[at];
+        p.weight = a.weights ? a.weights[at] : 1.0f;
+        if ((unsigned)p.place >= (unsigned)a.rows) p = Pair{-1, 0.0f};
+    }
+    return p;
+}
+
 constexpr int kCombineThreads = 256;
 template <class T>
 __global__ __launch_bounds__(kCombineThreads) void moe_combine_kernel(const CombineArgs a)
 {
     const int chunks = (a.pieces + kCombineThreads - 1) / kCombineThreads, token = (int)(blockIdx.x / (unsigned)chunks);
     const int piece = (int)(blockIdx.x % (unsigned)chunks) * kCombineThreads + (int)threadIdx.x;
-    if (piece >= a.pieces) return;
-    const int *const places = a.places + (long long)token * a.each;
-    const float *const weights = a.weights ? a.weights + (long long)token * a.each : nullptr;
+    // (lane j has pair j's place and weight; the rows of four pairs are in flight together)
+    const Pair pair = pair_of(a, token, (int)threadIdx.x & 63);
+    const bool any = piece < a.pieces;
     float sum[8] = {};
-    for (int j = 0; j < a.each; ++j) {
-        const int place = places[j];
-        if ((unsigned)place >= (unsigned)a.rows) continue;
-        const float w = weights ? weights[j] : 1.0f;
-        const auto x = piece_of<T>(a, place, piece);
+    for (int j0 = 0; j0 < a.each; j0 += 4) {
+        vec<T, 8> x[4];
+        float w[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = __builtin_fmaf((float)x[e], w, sum[e]);
+        for (int j = 0; j < 4; ++j) {
+            const int place = __builtin_amdgcn_readlane(pair.place, (j0 + j) & 63);
+            w[j] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, pair.weight), (j0 + j) & 63));
+            x[j] = vec<T, 8>{};
+            if (place >= 0 && any) x[j] = piece_of<T>(a, place, piece);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = __builtin_fmaf((float)x[j][e], w[j], sum[e]);
     }
+    if (!any) return;
     vec<T, 8> out;
 #pragma unroll
     for (int e = 0; e < 8; ++e) out[e] = (T)sum[e];
@@ -176,7 +227,7 @@ __global__ __launch_bounds__(kCombineThreads) void moe_combine_kernel(const Comb
 template <class T>
 __global__ __launch_bounds__(kCombineThreads) void moe_combine_backward_kernel(const CombineArgs a)
 {
-    constexpr int WAVES = kCombineThreads / 64;
+    constexpr int WAVES = kCombineThreads / 64, kPairs = 4;  // (rows in flight)
     __shared__ float s_dot[WAVES][kMostEach];
     const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     vec<T, 8> *const out = static_cast<vec<T, 8> *>(a.out);
@@ -188,27 +239,41 @@ __global__ __launch_bounds__(kCombineThreads) void moe_combine_backward_kernel(c
         return;
     }
     const int token = blockIdx.x;
-    const int *const places = a.places + (long long)token * a.each;
-    const float *const weights = a.weights + (long long)token * a.each;
     const vec<T, 8> *const grad = reinterpret_cast<const vec<T, 8> *>(static_cast<const T *>(a.grad) + token * a.grad_row);
-    for (int j = 0; j < a.each; ++j) {
-        const int place = places[j];
-        float dot = 0.0f;
-        if ((unsigned)place < (unsigned)a.rows) {
-            const float w = weights[j];
-            for (int piece = threadIdx.x; piece < a.pieces; piece += kCombineThreads) {
-                const auto g = grad[piece], y = piece_of<T>(a, place, piece);
+    const Pair pair = pair_of(a, token, lane);
+    for (int j0 = 0; j0 < a.each; j0 += kPairs) {
+        int place[kPairs];
+        float w[kPairs], dot[kPairs] = {};
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+            place[j] = __builtin_amdgcn_readlane(pair.place, (j0 + j) & 63);
+            w[j] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, pair.weight), (j0 + j) & 63));
+        }
+        for (int piece = threadIdx.x; piece < a.pieces; piece += kCombineThreads) {
+            const auto g = grad[piece];
+            vec<T, 8> y[kPairs];
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                y[j] = vec<T, 8>{};
+                if (place[j] >= 0) y[j] = piece_of<T>(a, place[j], piece);
+            }
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                if (place[j] < 0) continue;
                 vec<T, 8> d;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    dot = __builtin_fmaf((float)g[e], (float)y[e], dot);
-                    d[e] = (T)((float)g[e] * w);
+                    dot[j] = __builtin_fmaf((float)g[e], (float)y[j][e], dot[j]);
+                    d[e] = (T)((float)g[e] * w[j]);
                 }
-                out[(size_t)place * a.pieces + piece] = d;
+                out[(size_t)place[j] * a.pieces + piece] = d;
             }
         }
-        for (int d = 32; d; d >>= 1) dot += __shfl_xor(dot, d);
-        if (lane == 0) s_dot[wave][j] = dot;
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+            for (int d = 32; d; d >>= 1) dot[j] += __shfl_xor(dot[j], d);
+            if (lane == 0 && j0 + j < a.each) s_dot[wave][j0 + j] = dot[j];
+        }
     }
     __syncthreads();
     if ((int)threadIdx.x < a.each) {
@@ -226,7 +291,7 @@ using namespace lqq;
 namespace {
 constexpr int kMostBlocks = 1 << 23;  // (a launch holds fewer than 2^32 threads)
 int type_bytes(int type) { return type == LQ_I8 ? 1 : type == LQ_F16 || type == LQ_BF16 ? 2 : 0; }
-bool pairs_ok(int tokens, int each) { return tokens >= 0 && each >= 1 && each <= kMostEach && (long long)tokens * each < (1LL << 31) - kSortThreads; }
+bool pairs_ok(int tokens, int each) { return tokens >= 0 && each >= 1 && each <= kMostEach && (long long)tokens * each < (1LL << 31) - kBatchPairs; }
 }  // namespace
 
 extern "C" int moe_dispatch(int type, int tokens, int each, int n_experts, int K, const void *X, long long x_row, const float *act_scales,
@@ -244,13 +309,14 @@ extern "C" int moe_dispatch(int type, int tokens, int each, int n_experts, int K
         return fail(LQ_ERR_ALIGN, "scales, experts, row_offsets and places must be 4-byte aligned");
     if (tokens > 1 && x_row * size % 16) return fail(LQ_ERR_ALIGN, "the stride of X's rows must be a multiple of 16 bytes, got %lld elements", x_row);
     const DispatchArgs a{static_cast<const char *>(X), act_scales, experts, static_cast<char *>(rows), row_scales, row_offsets, places,
-                         tokens > 1 ? x_row * size : 0, tokens, each, n_experts, K * size / 16};
+                         tokens > 1 ? x_row * size : 0, tokens, each, n_experts, K * size / 16,
+                         std::max(1, std::min(256 / n_experts, (tokens * each + kBatchPairs - 1) / kBatchPairs))};
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
     if (tokens * (long long)each <= kFewPairs) {
         hipLaunchKernelGGL(moe_dispatch_small_kernel, dim3((unsigned)tokens + 1), dim3(kSmallThreads), 0, st, a);
     } else {
-        hipLaunchKernelGGL(moe_places_kernel, dim3((unsigned)n_experts), dim3(kSortThreads), 0, st, a);
+        hipLaunchKernelGGL(moe_places_kernel, dim3((unsigned)(n_experts * a.segments)), dim3(kSortThreads), 0, st, a);
         hipLaunchKernelGGL(moe_copy_kernel, dim3((unsigned)tokens), dim3(kCopyThreads), 0, st, a);
     }
     const hipError_t e = hipGetLastError();
