@@ -42,6 +42,10 @@ CHUNKS = [
     ([70, 257], [1000, 300], 256, 8, 1),                             # pages longer than a tile of keys
     ([300, 31], [300, 2000], 16, 24, 8),
     ([9, 2, 130], [3000, 4097, 2500], 64, 3, 1),                     # few queries, many keys: parts of the keys
+    ([1], [9000], 16, 8, 2),                                         # few rows of one sequence: many parts
+    ([8, 9, 32, 33], [1030, 2100, 31, 40], 256, 4, 1),               # 32 rows, 36, 128, 132: tiles with few rows behind full ones
+    ([65, 64, 63, 1], [1100, 65, 1200, 2], 32, 4, 2),
+    ([1, 2, 3, 4, 5], [33, 64, 129, 4, 2], 16, 32, 1),               # 32 rows a token
 ]
 
 
@@ -72,6 +76,19 @@ def test_chunks(dtype, D, case):
     kept = slice(3, int(starts[-1]))
     assert torch.equal(again[kept], out[kept]) and torch.equal(api.kv4_attention_chunks(dq, *args)[kept], out[kept])
     _check(_np(api.kv4_attention_chunks(dq, *args, workspace=ws[:16])), q, starts, contexts, keys, values, dtype)  # (too small: without parts)
+
+
+def test_many_sequences_of_few_rows():
+    """More sequences than a wave has lanes, each with one block for all of its keys."""
+    rng = np.random.default_rng(71)
+    D, Hq, Hkv, page, dtype = 128, 8, 2, 16, A.BF16
+    new, contexts = rng.integers(1, 4, 70), rng.integers(1, 900, 70).tolist()
+    contexts[3], new[3] = 5000, 1
+    cache, table, keys, values = _filled(rng, contexts, page, Hkv, D, dtype)
+    starts = _starts(new)
+    q = _draw(rng, (starts[-1], Hq, D), dtype)
+    got = _np(api.kv4_attention_chunks(_gpu(q, dtype), cache, _gpu(table), _ints(contexts), _ints(starts)))
+    _check(got, q, starts, contexts, keys, values, dtype)
 
 
 @pytest.mark.parametrize("n,longest", [(65, 40), (150, 90), (4500, 2)])
@@ -109,12 +126,13 @@ def test_the_same_as_the_attention_of_new_tokens(dtype, n):
         _check(got, q, starts, contexts, keys, values, dtype)
 
 
+@pytest.mark.parametrize("n", [40, 7])
 @pytest.mark.parametrize("dtype", TYPES)
-def test_weights_of_all_sizes(dtype):
+def test_weights_of_all_sizes(dtype, n):
     """Scores far apart, in rising and falling order (the running maximum moves often, or never), and values whose scales differ by
     2^20 (FP16: 2^12) from token to token."""
     rng = np.random.default_rng(5)
-    D, page, Hq, Hkv, c, n = 128, 32, 4, 2, 700, 40
+    D, page, Hq, Hkv, c = 128, 32, 4, 2, 700
     for order in (1, -1):
         q = _draw(rng, (n, Hq, D), dtype)
         k = rng.standard_normal((c, Hkv, D)).astype(np.float32) * 0.1
@@ -128,13 +146,14 @@ def test_weights_of_all_sizes(dtype):
         _check(_np(got), q, [0, n], [c], [k], [v], dtype)
 
 
+@pytest.mark.parametrize("n", [5, 70])
 @pytest.mark.parametrize("split", [False, True])
-def test_values_near_the_ends_of_bf16(split):
+def test_values_near_the_ends_of_bf16(split, n):
     """Values of 2^126 and of 2^-110, alone and next to rows of zeros (whose scale is 2^-100) and to each other; queries of 2^100 beside ones of 2^-20."""
     rng = np.random.default_rng(6)
-    D, page, c, n = 64, 16, 400 if split else 40, 5
+    D, page, c = 64, 16, 400 if split else 40
     q, k = _draw(rng, (n, 2, D), A.BF16), _draw(rng, (c, 1, D), A.BF16)
-    q = A.round_to(q * np.float32(2.0) ** np.array([100, 98, 60, -20, 100], dtype=np.float32)[:, None, None], A.BF16)
+    q = A.round_to(q * np.float32(2.0) ** np.resize(np.array([100, 98, 60, -20, 100], dtype=np.float32), n)[:, None, None], A.BF16)
     q[2] = 0
     for sizes in ([126], [-110], [126, None], [-110, None], [30, None, -60], [126, -90, None], [60, 20, None, -20]):
         v = _draw(rng, (c, 1, D), A.BF16).clip(-1.5, 1.5)
@@ -148,7 +167,14 @@ def test_values_near_the_ends_of_bf16(split):
         kk, vv = (A.dequantise(*A.quantise(x)) for x in (k, v))
         want, spread = A.attention(q, kk, vv, 2.0 ** -103, c - n + 1 + np.arange(n))
         got = got.double().cpu().numpy()
-        assert (np.abs(got - want) <= 1.1 * (A.UNIT[A.BF16] * np.abs(want) + 2.0 ** -11 * spread)).all(), sizes
+        # A weight times its value's scale is an FP16 number whose step is 2^-24 at least, and the largest of a row's is 2^6 at least: half a step is 2^-31 of
+        # it, and each key's moves a result by that times 15 at most.  (So a value that is 2^-31 of another's scale may vanish, also where that one's code is 0.)
+        limit = c - n + 1 + np.arange(n)
+        scores = np.where(np.arange(c) < limit[:, None, None], q.astype(np.float64) @ kk[:, 0].astype(np.float64).T * 2.0 ** -103, -np.inf)
+        p = np.where(limit[:, None, None] > 0, np.exp(scores - np.maximum(scores.max(-1, keepdims=True), -1e300)), 0.0)
+        largest = (p * A.quantise(v)[1].astype(np.float64).reshape(c)).max(-1) / np.maximum(p.sum(-1), 1.0)
+        tol = 1.1 * (A.UNIT[A.BF16] * np.abs(want) + 2.0 ** -11 * spread) + (15 * 2.0 ** -31 * c * largest)[..., None]
+        assert (np.abs(got - want) <= tol).all(), sizes
 
 
 def test_places_that_nothing_was_written_to_count_as_zeros():
@@ -167,11 +193,12 @@ def test_places_that_nothing_was_written_to_count_as_zeros():
     _check(_np(got), q, [0, n], [c], [kk], [vv], A.F16)
 
 
+@pytest.mark.parametrize("n", [80, 13])
 @pytest.mark.parametrize("dtype", TYPES)
-def test_nan_stays_with_those_that_see_it(dtype):
+def test_nan_stays_with_those_that_see_it(dtype, n):
     """A key, or a value, that is not finite: only for the queries that see it; and a query that is not: only for itself."""
     rng = np.random.default_rng(7)
-    D, page, Hq, Hkv, contexts, new = 128, 16, 4, 2, [190, 60], [80, 3]
+    D, page, Hq, Hkv, contexts, new = 128, 16, 4, 2, [190, 60], [n, 3]
     cache, table, keys, values = _filled(rng, contexts, page, Hkv, D, dtype)
     starts = _starts(new)
     q = _draw(rng, (starts[-1], Hq, D), dtype)
@@ -184,14 +211,14 @@ def test_nan_stays_with_those_that_see_it(dtype):
             spoilt[int(table[0, key // page]), 1, at:at + 4] = _gpu(np.array([0x7FC00000], dtype="<u4").view(np.uint8))
             got = call(q, spoilt)
             sees = np.zeros(got.shape[:2], dtype=bool)
-            sees[:80, 2:] = (110 + np.arange(80) >= key)[:, None]
+            sees[:n, 2:] = (190 - n + np.arange(n) >= key)[:, None]
             assert np.isnan(got[sees]).all() and np.array_equal(got[~sees], clean[~sees]), (which, key)
     for bad in (np.nan, np.inf):
         q2 = q.copy()
-        q2[40, 1, 9] = bad
+        q2[n // 2, 1, 9] = bad
         got = call(q2, cache)
-        assert np.isnan(got[40, 1]).all()
-        got[40, 1] = clean[40, 1]
+        assert np.isnan(got[n // 2, 1]).all()
+        got[n // 2, 1] = clean[n // 2, 1]
         assert np.array_equal(got, clean)
 
 
@@ -205,6 +232,43 @@ def test_tables_that_name_no_page():
     table[0, 1], table[2, 8] = -1, cache.shape[0]
     got = _np(api.kv4_attention_chunks(q, cache, _gpu(table), _ints([140, 100, 140, 16 * table.shape[1] + 1]), _ints(starts)))
     assert np.isnan(got[:20]).all() and np.array_equal(got[20:50], good[20:50]) and np.isnan(got[50 + 8:]).all()
+
+
+def test_tables_that_name_no_page_few_rows():
+    """The same where each wave of a block has keys of its own: a page that one wave meets, pages behind the context, a context longer than the table."""
+    rng = np.random.default_rng(80)
+    D, page, Hq, Hkv, contexts, new = 128, 16, 2, 1, [1400, 100, 140, 40], [3, 5, 16, 4]
+    cache, table, keys, values = _filled(rng, contexts, page, Hkv, D, A.F16)
+    starts = _starts(new)
+    q = _gpu(_draw(rng, (starts[-1], Hq, D), A.F16), A.F16)
+    good = _np(api.kv4_attention_chunks(q, cache, _gpu(table), _ints(contexts), _ints(starts)))
+    _check(good, _np(q), starts, contexts, keys, values, A.F16)
+    for at in (0, 37, 87):
+        wrong = table.copy()
+        wrong[0, at], wrong[2, 8] = -1, cache.shape[0]
+        got = _np(api.kv4_attention_chunks(q, cache, _gpu(wrong), _ints([1400, 100, 140, 16 * table.shape[1] + 1]), _ints(starts)))
+        assert np.isnan(got[:3]).all() and np.array_equal(got[3:8], good[3:8]) and np.isnan(got[8 + 4:]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [3, 60])
+def test_rows_of_unlike_size(dtype, n):
+    """One query that is 2^6 to 2^14 times the others of its block, and elements of a row as far apart: the others keep their own accuracy.  (Its own
+    scores are thousands, which FP32 holds to 2^-12: it is left out.)"""
+    rng = np.random.default_rng(n)
+    c, Hq, Hkv, D = 300, 4, 2, 64
+    cache, table, keys, values = _filled(rng, [c], 16, Hkv, D, dtype)
+    for bits in (6, 8, 9, 14):
+        q = _draw(rng, (n, Hq, D), dtype) * np.float32(2.0 ** (3 - bits))
+        q[n // 2, 1] *= np.float32(2.0 ** bits)
+        q[n // 3, 2, ::2] *= np.float32(2.0 ** -5)
+        q = A.round_to(q, dtype)
+        scale = 2.0 ** (bits - 6)
+        got = _np(api.kv4_attention_chunks(_gpu(q, dtype), cache, _gpu(table), _ints([c]), _ints([0, n]), scale=scale))
+        want, spread = A.attention(q, keys[0], values[0], scale, c - n + 1 + np.arange(n))
+        assert np.isfinite(got[n // 2, 1]).all()
+        got[n // 2, 1] = want[n // 2, 1]
+        _close(got, want, spread, dtype, 2.0 ** -11, f"2^{bits}")
 
 
 @pytest.mark.parametrize("scale", [0.0, -0.11, 1e-30, 3.0])
