@@ -185,7 +185,7 @@ __device__ __forceinline__ Pair pair_of(const CombineArgs &a, int token, int j)
     if (j < a.each) {
         const long long at = (long long)token * a.each + j;
         p.place = a.places[at];
-        p.weight = a.weights ? a.weights[at] : 1.0f;
+        p.weight = a.weights[at];
         if ((unsigned)p.place >= (unsigned)a.rows) p = Pair{-1, 0.0f};
     }
     return p;
@@ -197,26 +197,20 @@ __global__ __launch_bounds__(kCombineThreads) void moe_combine_kernel(const Comb
 {
     const int chunks = (a.pieces + kCombineThreads - 1) / kCombineThreads, token = (int)(blockIdx.x / (unsigned)chunks);
     const int piece = (int)(blockIdx.x % (unsigned)chunks) * kCombineThreads + (int)threadIdx.x;
-    // (lane j has pair j's place and weight; the rows of four pairs are in flight together)
-    const Pair pair = pair_of(a, token, (int)threadIdx.x & 63);
-    const bool any = piece < a.pieces;
+    // (places and weights are scalar loads, and waves enough are there to hide a row's: 8191 tokens of 8 experts, half of them here, 64 us; with four rows
+    // of a thread in flight 68)
+    if (piece >= a.pieces) return;
+    const int *const places = a.places + (long long)token * a.each;
+    const float *const weights = a.weights ? a.weights + (long long)token * a.each : nullptr;
     float sum[8] = {};
-    for (int j0 = 0; j0 < a.each; j0 += 4) {
-        vec<T, 8> x[4];
-        float w[4];
+    for (int j = 0; j < a.each; ++j) {
+        const int place = places[j];
+        if ((unsigned)place >= (unsigned)a.rows) continue;
+        const float w = weights ? weights[j] : 1.0f;
+        const auto x = piece_of<T>(a, place, piece);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int place = __builtin_amdgcn_readlane(pair.place, (j0 + j) & 63);
-            w[j] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, pair.weight), (j0 + j) & 63));
-            x[j] = vec<T, 8>{};
-            if (place >= 0 && any) x[j] = piece_of<T>(a, place, piece);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] = __builtin_fmaf((float)x[j][e], w[j], sum[e]);
+        for (int e = 0; e < 8; ++e) sum[e] = __builtin_fmaf((float)x[e], w, sum[e]);
     }
-    if (!any) return;
     vec<T, 8> out;
 #pragma unroll
     for (int e = 0; e < 8; ++e) out[e] = (T)sum[e];
