@@ -132,9 +132,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
         }
         if (a.slots > all * a.Hkv) {
             const int most = a.slots / a.Hkv;  // parts of a kv head
+            // Joining a part costs about what a tile of keys does (1.4 us: 68 KB from behind the L2 for one CU), so that parts and tiles of each are as many.  (One
+            // sequence of 2048 keys, 32/8 heads, 128 new tokens, tiles of a part: 2 42.5 us, 6 25.0, 9 27.5, 17 39.0; of 16384, 64 new ones: 8 76, 16 50.9, 24 59.1, 48
+            // 85.8; of 1024, 64/8 heads, 64 new ones: 2 21.7, 4 21.1, 8 26.1.)  Few rows: from 1024 keys on (17 tokens of 517, 32 heads: one part 13.8 us, two 16.0,
+            // three 15.8).
+            const int least = little ? kLeast : max(2, (int)__builtin_sqrtf((float)keys));
             int size = max(up(__builtin_amdgcn_readlane(sums_up_to(mine * min(keys, 1 << 16)), 63), most), 1), sum;
             do {
-                parts = min(max(up(keys, max(size, little ? kLeast : 2)), 1), kMostParts);
+                parts = min(max(up(keys, max(size, least)), 1), kMostParts);
                 sum = __builtin_amdgcn_readlane(sums_up_to(mine * parts), 63);
                 size += up(size, 8);
             } while (sum > most);  // (one part each fits, and comes before size overflows: keys is below 2^24)
@@ -626,26 +631,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
             if (c == 0) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v4f{top, sum, 0.0f, 0.0f}), left_parts, at_part(part, r, D / 4), 0, kShared);
         }
         if (n_parts == 1 || !last_to_arrive()) return;
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
+        constexpr int kAtOnce = 8;  // parts whose loads are in flight together
+        for (int i = 0; i < PIECES && first + 64 * kWaves * i / (D / 4) < rows; ++i) {
             int r, c;
             place(i, r, c);
             float top = -__builtin_inff(), sum = 0.0f;
             v4f x{};
-            for (int p = 0; p < n_parts; p += 4) {
-                v4f ml[4], y[4];
+            for (int p = 0; p < n_parts; p += kAtOnce) {
+                vec<float, 2> ml[kAtOnce];
+                v4f y[kAtOnce];
+                float now = top;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    ml[k] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(left_parts, at_part(p + k, r, D / 4), 0, kShared));
+                for (int k = 0; k < kAtOnce; ++k) {
+                    ml[k] = __builtin_bit_cast(vec<float, 2>, __builtin_amdgcn_raw_buffer_load_b64(left_parts, at_part(p + k, r, D / 4), 0, kShared));
                     y[k] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(left_parts, at_part(p + k, r, c), 0, kShared));
-                    if (p + k >= n_parts) ml[k][0] = -__builtin_inff();
                 }
-                const float now = fmaxf(fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0])), top), old = root_of(top, now);
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    if (p + k >= n_parts) ml[k][0] = -__builtin_inff();
+                    now = fmaxf(now, ml[k][0]);
+                }
+                const float old = root_of(top, now);
                 top = now;
                 sum = sum * old * old;
                 x *= old * old;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < kAtOnce; ++k) {
                     const float by = root_of(ml[k][0], now);
                     sum += ml[k][1] * by * by;
                     x += y[k] * (by * by);
