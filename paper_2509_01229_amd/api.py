@@ -603,6 +603,12 @@ def _on_this_device(**tensors):
             raise ValueError(f"{name} is on {t.device}, and the current device is cuda:{here}: call it under torch.cuda.device({name}.device)")
 
 
+def _countable(t, name):
+    """The C calls count in 32 bits."""
+    if max(t.shape, default=0) >= 2 ** 31:
+        raise ValueError(f"{name} is too large: {tuple(t.shape)}")
+
+
 def _rows(t, name, dtypes=None, shape=None):
     """A matrix on the GPU whose rows may have a stride of their own: its pointer and that stride."""
     import torch
@@ -616,6 +622,7 @@ def _rows(t, name, dtypes=None, shape=None):
         raise ValueError(f"{name} must have shape {tuple(shape) if shape is not None else '[rows, elements]'}, got {tuple(t.shape)}")
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: the elements of a row must be consecutive")
+    _countable(t, name)
     return ctypes.c_void_p(t.data_ptr()), t.stride(0)
 
 
@@ -690,6 +697,7 @@ def moe_dispatch(X, experts, n_experts: int, act_scales=None, out=None, out_scal
     (T, K), code = X.shape, {torch.int8: LQ_I8, torch.float16: LQ_F16, torch.bfloat16: LQ_BF16}[X.dtype]
     if not isinstance(experts, torch.Tensor) or experts.dim() != 2:
         raise ValueError("experts must be [tokens, experts of each]")
+    _countable(experts, "experts")
     each = experts.shape[1]
     ids = _dev(experts, torch.int32, (T, each), "experts")
     if not 1 <= n_experts <= 256:
@@ -711,6 +719,7 @@ def _places(places, weights):
 
     if not isinstance(places, torch.Tensor) or places.dim() != 2:
         raise ValueError("places must be [tokens, rows of each]")
+    _countable(places, "places")
     return (*places.shape, _dev(places, torch.int32, name="places"), _dev(weights, torch.float32, tuple(places.shape), "weights"))
 
 
@@ -758,7 +767,10 @@ def moe_combine_backward(grad, Y, places, weights, row_offsets=None, out_Y=None,
         raise ValueError(f"row_offsets must be [experts + 1], got {tuple(row_offsets.shape)}")
     used = None if row_offsets is None else ctypes.c_void_p(_dev(row_offsets, torch.int32, name="row_offsets").value + 4 * (row_offsets.shape[0] - 1))
     if out_Y is None:
-        out_Y = (torch.zeros if used is None else torch.empty)((R, N), dtype=Y.dtype, device=Y.device)
+        out_Y = torch.empty((R, N), dtype=Y.dtype, device=Y.device)
+        if used is None:  # (on the call's stream, which writes to it next)
+            with torch.cuda.stream(None if stream is None else torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()):
+                out_Y.zero_()
     out_weights = torch.empty((T, each), dtype=torch.float32, device=Y.device) if out_weights is None else out_weights
     _check(lib().moe_combine_backward(_dtype_code(Y), T, each, R, N, *dg, *dy, dp, dw, used, _dev(out_Y, Y.dtype, (R, N), "out_Y"),
                                       _dev(out_weights, torch.float32, (T, each), "out_weights"), _stream(stream)))
@@ -997,6 +1009,8 @@ def kv4_attention_chunks(q, cache, block_table, context, starts_q, scale=None, o
     S = starts_q.shape[0] - 1
     if block_table.dim() != 2:
         raise ValueError(f"block_table must be [sequences, width], got {tuple(block_table.shape)}")
+    for name, t in (("q", q), ("cache", cache), ("starts_q", starts_q), ("block_table", block_table)):
+        _countable(t, name)
     width = block_table.shape[1]
     out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device) if out is None else out
     need = int(lib().kv4_attention_chunks_workspace_size(S, T, Hq, Hkv, D, page, width))

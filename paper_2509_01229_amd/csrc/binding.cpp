@@ -510,6 +510,7 @@ PyObject *chunks(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (PyErr_Occurred()) return nullptr;
         Py_RETURN_NONE;
     }
+    if (workspace.defined() && !here(workspace)) Py_RETURN_NONE;
     at::Tensor out = a[6] != Py_None ? tensor(a[6]) : at::Tensor();
     int rc;
     {

@@ -310,6 +310,38 @@ def test_a_graph_follows_its_inputs():
         assert torch.equal(q, want[0]) and torch.equal(s, want[1]) and torch.equal(h, want[2]) and torch.equal(y, want[3])
 
 
+def test_more_rows_than_the_calls_count():
+    """(Rows that are one row in memory.)"""
+    import torch
+
+    row = torch.ones((1, 8), dtype=torch.float16, device="cuda")
+    for rows in (2 ** 31, 2 ** 32 + 3):
+        many = row.expand(rows, 8)
+        for call in (lambda: api.w4a8_norm_quantize(many), lambda: api.w4a8_swiglu_quantize(row.repeat(1, 2).expand(rows, 16)),
+                     lambda: api.moe_combine(many, _gpu(np.zeros((1, 1), dtype=np.int32)))):
+            with pytest.raises(ValueError, match="too large"):
+                call()
+
+
+def test_gradients_on_another_stream():
+    """What no place names is zeroed on the stream that the call is given, not on the current one, which is at work."""
+    import torch
+
+    rng = np.random.default_rng(30)
+    Y, grad = _gpu(_draw(rng, (9, 64), A.F16), A.F16), _gpu(_draw(rng, (3, 64), A.F16), A.F16)
+    places, w = _gpu(np.array([[0, 4], [8, -1], [2, 7]], dtype=np.int32)), _gpu(rng.random((3, 2)).astype(np.float32))
+    want = api.moe_combine_backward(grad, Y, places, w)
+    side = torch.cuda.Stream()
+    for _ in range(2):
+        torch.cuda.synchronize()
+        big = torch.zeros(1 << 28, device="cuda")
+        for _ in range(20):
+            big.add_(1.0)                                   # (milliseconds)
+        got = api.moe_combine_backward(grad, Y, places, w, stream=side.cuda_stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and not got[0][[1, 3, 5, 6]].any()
+
+
 def test_refusals():
     import torch
 
