@@ -4,18 +4,31 @@
 //     o_i = sum_j softmax_j(scale * q_i . k_j) v_j,   k_j = (code - z) * s of the key, v_j likewise,   j < context - n + 1 + i
 // for new token i of a sequence's n.
 //
-// A block takes rows, queries times the heads that share a kv head, a wave 32 of them; it goes through the keys from the last to the first, 64 at
-// a time: their codes are loaded while the tile before is in the making, unpacked into LDS as FP16 integers (code - z, exact) while
-// the one before that is worked on, and go into 32x32x16 MFMAs with the keys' side as the first operand (S^T = K Q^T, O^T = V^T P^T): a lane's
-// scores are 32 keys of one row, in the order in which the weights enter the second product.  Value codes lie in a page as pairs of tokens,
-// and so they are unpacked to [element][keys]: both operands come out of LDS in 16-byte reads.
+// A block takes 128 rows, queries times the heads that share a kv head, a wave 32 of them; it goes through the keys from the last to the first, 64 at a
+// time.  Their codes are loaded while the tile before the last is worked on, and unpacked into LDS next to the products of the tile before: a wave unpacks a
+// quarter of them.  Both products run on 32x32x16 MFMAs with the cache as the first operand (S^T = K Q^T, O^T = V^T P^T): a lane's scores are 32
+// keys of one row, in the order in which the weights enter the second product.  Value codes lie in a page as pairs of tokens, and so they are unpacked to
+// [element][keys]: both operands come out of LDS in 16-byte reads.  Codes are masked out of their dword (5 instructions for 8) and go in as the subnormal FP16
+// numbers that they then are, which the matrix cores multiply exactly; what the keys' zero points take off the scores is one more product, with the sum of a query's
+// elements; the values' are taken off the codes (4 more instructions), as their sums may cancel.
 //
 // The scales never meet the codes.  The keys' are applied to the scores; the values' enter as logarithms,
 //     t_j = scale * q . (code - z) * s_j + log2(sv_j),   x_j = 2^(t_j - m),   o = sum x_j (code - z) / sum x_j / sv_j,
 // one fused multiply-add each, so that what is rounded to FP16 for the second product is a weight times its value's scale, relative to the largest
-// such product (2^6 .. 2^14), and the values have no rounding at all.  sum x_j / sv_j stays in FP32's range for all scales there are, 2^-100 .. 2^124; but
-// where the scales of a sequence are further apart than 2^100 an x_j may vanish whose weight counts, and the terms of the sum are taken from the scores
-// without the values' scales instead.
+// such product (2^6 .. 2^14; what is below 2^-31 of the largest may vanish), and the values have no rounding at all.  sum x_j / sv_j stays in FP32's range for all
+// scales there are, 2^-100 .. 2^124; but where the scales of a sequence are further apart than 2^100 an x_j may vanish whose weight counts, and the terms of the sum
+// are taken from the scores without the values' scales instead.
+//
+// Tiles of at most 32 rows (single tokens, short chunks, ends of long ones) would leave three waves of four without products: there each wave has keys of its
+// own, 32 at a time, straight from the cache into the operands' registers, and the waves' results are joined in LDS at the end.  (24 sequences, three of them
+// chunks, 97 -> 73 us; 17 tokens of 517, 32 heads, 18.2 -> 15.6.)
+//
+// Measured, heads of 128 (by machine; the clock is 1.95 to 2.2 GHz under this load): two chunks of 2048 over up to 16384, 64/8 heads, BF16, 2230 to 2470 us (820 to 900
+// TFLOP/s); 512 tokens over 1536 earlier ones, 32/8 heads, 39 us; 24 sequences with up to 4096 tokens, 640 new ones, 63; 17 of 517, 32/32 heads, 12.3.  A wave
+// takes 34 MFMAs (1088 cycles) and 250 vector instructions with 34 exponentials or the like (1330) for 32 rows and 64 keys, and 56 reads of LDS (448 cycles of the four that share it: 58%
+// with the writes); two waves a SIMD make that in 2600 cycles each, so that MFMAs (42%) and vector instructions (51 to 56%) hardly overlap.  Tried, and slower
+// or within 1%: two rows tiles a wave with one wave a SIMD (3480 us when this took 2660; halves the LDS reads), 8 waves of two groups half a tile apart
+// (2840), fragments read two slices ahead, one of the two blocks of a CU ahead of the other by priority.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -547,7 +560,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
 #pragma unroll
                 for (int i = 0; i < STEPS; ++i) s[u] = mfma32(keys(0, u, i), q[i], s[u]);
             }
-            // (what has products to issue goes first: 2332 -> 2294 us where 2 blocks a CU have chunks of 1024, a mixed step 72 -> 68)
+            // (what has products to issue goes first: 2332 -> 2294 us for two chunks of 2048, a mixed step 72 -> 68)
             for (int p = 0; p < n_tiles; ++p) {
                 const v4i far = *reinterpret_cast<const v4i *>(s_far[p & 3]);
                 softmax(p & 3, (t_first - p) * kKeys, __builtin_amdgcn_readfirstlane(far[0] | far[1] | far[2] | far[3]), std::integral_constant<int, 2>{});
