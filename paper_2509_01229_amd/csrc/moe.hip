@@ -151,11 +151,13 @@ __global__ __launch_bounds__(kSortThreads) void moe_places_kernel(const Dispatch
         }
     }
 }
-constexpr int kCopyThreads = 256;
+// A block copies a token's row.  Threads: 512, and 1024 for rows of more than 8 KB (4096 tokens of 8 experts: rows of 8 KB 72 us, with 256 threads 79; of
+// 16 KB 133, with 512 138 to 144, with 256 145 to 154; of 4 KB 40, with 256 and with 1024 41).
+constexpr int kCopyThreads = 1024;
 __global__ __launch_bounds__(kCopyThreads) void moe_copy_kernel(const DispatchArgs a)
 {
     const int lane = threadIdx.x & 63;
-    copy_row(a, blockIdx.x, lane < a.each ? a.places[(long long)blockIdx.x * a.each + lane] : -1, threadIdx.x, kCopyThreads);
+    copy_row(a, blockIdx.x, lane < a.each ? a.places[(long long)blockIdx.x * a.each + lane] : -1, threadIdx.x, blockDim.x);
 }
 
 struct CombineArgs {
@@ -218,17 +220,21 @@ __global__ __launch_bounds__(kCombineThreads) void moe_combine_kernel(const Comb
 }
 
 // The gradients: a block takes a token; the blocks behind the tokens clear the rows that no expert has
+// Threads: 512, and 256 where a row has no more pieces than that (2047 tokens of 8192 elements, 4 experts each, 65 us, with 256 threads 70, with 1024 63; 4096 of 1024, 8 each,
+// with 256 32, with 512 36; 4096 of 4096, 2 each, 36, 37 and 39).
+constexpr int kGradThreads = 512;
 template <class T>
-__global__ __launch_bounds__(kCombineThreads) void moe_combine_backward_kernel(const CombineArgs a)
+__global__ __launch_bounds__(kGradThreads) void moe_combine_backward_kernel(const CombineArgs a)
 {
-    constexpr int WAVES = kCombineThreads / 64, kPairs = 4;  // (rows in flight)
-    __shared__ float s_dot[WAVES][kMostEach];
+    constexpr int kPairs = 4;  // (rows in flight)
+    __shared__ float s_dot[kGradThreads / 64][kMostEach];
+    const int threads = blockDim.x;
     const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     vec<T, 8> *const out = static_cast<vec<T, 8> *>(a.out);
     if ((int)blockIdx.x >= a.tokens) {
         const int used = min(max(*a.used, 0), a.rows);
-        for (long long i = (long long)used * a.pieces + (blockIdx.x - a.tokens) * kCombineThreads + threadIdx.x; i < (long long)a.rows * a.pieces;
-             i += (long long)(gridDim.x - a.tokens) * kCombineThreads)
+        for (long long i = (long long)used * a.pieces + (long long)(blockIdx.x - a.tokens) * threads + threadIdx.x; i < (long long)a.rows * a.pieces;
+             i += (long long)(gridDim.x - a.tokens) * threads)
             out[i] = vec<T, 8>{};
         return;
     }
@@ -243,7 +249,7 @@ __global__ __launch_bounds__(kCombineThreads) void moe_combine_backward_kernel(c
             place[j] = __builtin_amdgcn_readlane(pair.place, (j0 + j) & 63);
             w[j] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, pair.weight), (j0 + j) & 63));
         }
-        for (int piece = threadIdx.x; piece < a.pieces; piece += kCombineThreads) {
+        for (int piece = threadIdx.x; piece < a.pieces; piece += threads) {
             const auto g = grad[piece];
             vec<T, 8> y[kPairs];
 #pragma unroll
@@ -272,8 +278,7 @@ __global__ __launch_bounds__(kCombineThreads) void moe_combine_backward_kernel(c
     __syncthreads();
     if ((int)threadIdx.x < a.each) {
         float dot = s_dot[0][threadIdx.x];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) dot += s_dot[w][threadIdx.x];
+        for (int w = 1; w < threads / 64; ++w) dot += s_dot[w][threadIdx.x];
         a.grad_weights[(long long)token * a.each + threadIdx.x] = dot;
     }
 }
@@ -311,7 +316,7 @@ extern "C" int moe_dispatch(int type, int tokens, int each, int n_experts, int K
         hipLaunchKernelGGL(moe_dispatch_small_kernel, dim3((unsigned)tokens + 1), dim3(kSmallThreads), 0, st, a);
     } else {
         hipLaunchKernelGGL(moe_places_kernel, dim3((unsigned)(n_experts * a.segments)), dim3(kSortThreads), 0, st, a);
-        hipLaunchKernelGGL(moe_copy_kernel, dim3((unsigned)tokens), dim3(kCopyThreads), 0, st, a);
+        hipLaunchKernelGGL(moe_copy_kernel, dim3((unsigned)tokens), dim3(a.pieces > 512 ? kCopyThreads : kCopyThreads / 2), 0, st, a);
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? LQ_OK : fail(LQ_ERR_HIP, "dispatch launch failed: %s", hipGetErrorString(e));
@@ -360,7 +365,7 @@ extern "C" int moe_combine_backward(int dtype, int tokens, int each, int rows, i
     const CombineArgs a{Y, grad, places, rows_used, weights, grad_Y, grad_weights, rows > 1 ? y_row : 0, tokens > 1 ? grad_row : 0, tokens, each, rows, pieces};
     (void)hipGetLastError();
     hipLaunchKernelGGL(dtype == LQ_F16 ? moe_combine_backward_kernel<f16> : moe_combine_backward_kernel<bf16>, dim3((unsigned)(tokens + clearing)),
-                       dim3(kCombineThreads), 0, static_cast<hipStream_t>(hip_stream), a);
+                       dim3(pieces > 256 ? kGradThreads : 256), 0, static_cast<hipStream_t>(hip_stream), a);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? LQ_OK : fail(LQ_ERR_HIP, "gradient launch failed: %s", hipGetErrorString(e));
 }
