@@ -23,6 +23,7 @@
 // own, 32 at a time, straight from the cache into the operands' registers, and the waves' results are joined in LDS at the end.  (24 sequences, three of them
 // chunks, 97 -> 73 us; 17 tokens of 517, 32 heads, 18.2 -> 15.6.)
 //
+// Heads of 64 leave room for three blocks a CU: two chunks of 2048 over up to 16384, 64/8 heads, 1516 us, with two 1620.
 // Measured, heads of 128 (by machine; the clock is 1.95 to 2.2 GHz under this load): two chunks of 2048 over up to 16384, 64/8 heads, BF16, 2230 to 2470 us (820 to 900
 // TFLOP/s); 512 tokens over 1536 earlier ones, 32/8 heads, 39 us; 24 sequences with up to 4096 tokens, 640 new ones, 63; 17 of 517, 32/32 heads, 12.3.  A wave
 // takes 34 MFMAs (1088 cycles) and 250 vector instructions with 34 exponentials or the like (1330) for 32 rows and 64 keys, and 56 reads of LDS (448 cycles of the four that share it: 58%
@@ -100,7 +101,7 @@ __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts
 __device__ __forceinline__ int up(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1) / (unsigned)b); }
 
 template <int D, class T>
-__global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkArgs a)
+__global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kernel(const ChunkArgs a)
 {
     constexpr int KW = kKeys / kWaves, DW = D / 32, STEPS = D / 16, W = D / 16;  // (a wave unpacks KW keys; a lane DW dwords of codes)
     // Unpacked codes of two tiles (rows of keys are 16 bytes longer than they need be: lanes that read or write together meet in no bank); or, of a tile with
@@ -207,6 +208,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
     const bool little = rows - first <= kLittle;  // all waves have the same rows, and keys of their own
     const int row = first + (little ? 0 : 32 * wave) + n, limit = sees(row), wave_all = __builtin_amdgcn_readfirstlane(sees(row - n));
     const bool any_row = first + 32 * wave < rows;
+    // (computed again where it is needed again: registers that the loops do not have)
+    const auto thread_again = []() __attribute__((always_inline)) {
+        int thread = threadIdx.x;
+        asm volatile("" : "+v"(thread));
+        return thread;
+    };
+    const auto row_of = [&](int thread) { return first + (little ? 0 : 32 * wave) + (thread & 31); };
 
     // this part's tiles of keys: n_tiles of them, from t_first down (place p: tile t_first - p)
     const int tiles_k = __builtin_amdgcn_readfirstlane(max((sees(first + kRows - 1) + kKeys - 1) / kKeys, 0));
@@ -299,7 +307,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
     vec<f16, 8> w[4];
     float m = -__builtin_inff(), l = 0.0f;  // maximum of t, this lane's part of sum x / sv
     // The softmax of place p's scores: s -> w, l, m
-    const auto softmax = [&](int slot, int key, bool far, auto n_u) __attribute__((always_inline)) {
+    const auto softmax = [&](int slot, int key, int limit, bool far, auto n_u) __attribute__((always_inline)) {
         constexpr int U = decltype(n_u)::value;  // times 32 keys
         const auto at = [&](int i) { return 32 * (i >> 2) + 8 * (i & 3) + 4 * h; };  // the lane's keys 4 i ..
         if (uneven) {
@@ -394,7 +402,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
     // Results: a row's, and where a part of the keys leaves what it has (a lane without a row leaves and reads nothing)
     const auto write_row = [&]() __attribute__((always_inline)) {
         const float by = l == 0.0f ? 0.0f : 1.0f / l;
+        const int thread = thread_again(), row = row_of(thread), h = thread >> 5 & 1;
         T *const dst = static_cast<T *>(a.out) + ((size_t)(q0 + row / a.group) * a.Hq + hk * a.group + row % a.group) * D;
+        if (row >= rows) return;
 #pragma unroll
         for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -407,7 +417,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
     };
     constexpr int FLOATS = 64 * kWaves * (D / 2 + 4), kShared = 16;  // of a part; sc1
     const auto left_parts = __builtin_amdgcn_make_buffer_rsrc(a.parts + (size_t)whole * FLOATS, 0, n_parts * FLOATS * 4, 0x00027000);
-    const auto part_at = [&](int p, int piece) { return row < rows ? (p * FLOATS + (piece * 64 * kWaves + (int)threadIdx.x) * 4) * 4 : n_parts * FLOATS * 4; };
 
     // Tiles of few rows: of 32 keys, a wave's own, which go from the cache into the products as they are: lane n, h has key n's dwords STEPS h on, and for
     // the second product elements D / 32 n on of the four keys 8 g + 4 h of both halves.
@@ -513,6 +522,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) o[e] = v16f{};
     if (little) {
+        const int limit_again = sees(row_of(thread_again()));
         for (; t >= from32; t -= kWaves) {
             uint32_t v_now[2][2][2];
 #pragma unroll
@@ -524,7 +534,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
             const bool far = scales(wave, n);
             load_own(t - kWaves);
             pages[0] = pages_of(t - 2 * kWaves, 0), pages[1] = pages_of(t - 2 * kWaves, 1);
-            softmax(wave, 32 * t, far, std::integral_constant<int, 1>{});
+            softmax(wave, 32 * t, limit_again, far, std::integral_constant<int, 1>{});
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 u32x4 x[2][2];  // of four keys: pairs of them, elements
@@ -565,7 +575,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
             // (what has products to issue goes first: 2332 -> 2294 us for two chunks of 2048, a mixed step 72 -> 68)
             for (int p = 0; p < n_tiles; ++p) {
                 const v4i far = *reinterpret_cast<const v4i *>(s_far[p & 3]);
-                softmax(p & 3, (t_first - p) * kKeys, __builtin_amdgcn_readfirstlane(far[0] | far[1] | far[2] | far[3]), std::integral_constant<int, 2>{});
+                softmax(p & 3, (t_first - p) * kKeys, limit, __builtin_amdgcn_readfirstlane(far[0] | far[1] | far[2] | far[3]), std::integral_constant<int, 2>{});
                 meet();  // (what the next products read is there, and all waves are done with what they write over)
                 __builtin_amdgcn_s_setprio(1);
                 products(p);
@@ -682,9 +692,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
         return;
     }
     if (n_parts == 1) {
-        if (row < rows) write_row();
+        write_row();
         return;
     }
+    const bool there = row_of(thread_again()) < rows;
+    const auto part_at = [&](int p, int piece) { return there ? (p * FLOATS + (piece * 64 * kWaves + (int)threadIdx.x) * 4) * 4 : n_parts * FLOATS * 4; };
 #pragma unroll
     for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -711,7 +723,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_chunks_kernel(const ChunkA
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[e][i] = o[e][i] * (old * old) + x[4 * e + (i >> 2)][i & 3] * (by * by);
     }
-    if (row < rows) write_row();
+    write_row();
 }
 
 }  // namespace lqq
