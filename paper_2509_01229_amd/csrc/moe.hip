@@ -15,7 +15,7 @@
 
 namespace lqq {
 
-constexpr int kMostExperts = 256, kMostEach = 64, kFewPairs = 1024;
+constexpr int kMostExperts = 256, kMostEach = 64, kFewPairs = 2048;
 
 struct DispatchArgs {
     const char *x;
@@ -46,8 +46,11 @@ __device__ __forceinline__ void copy_row(const DispatchArgs &a, int token, int p
     }
 }
 
-// Few pairs: block t < tokens counts the places of its pairs and copies the row, the last block counts the experts' pairs
+// Few pairs, up to 64 * IDS of them: block t < tokens counts the places of its pairs and copies the row, the last block counts the experts' pairs.  All pairs are
+// looked at, whether they are there or not: 32 pairs take 2.6 us as up to 128, 3.4 as up to 1024 and 4.9 as up to 2048; 1600 pairs 8.6 as up to 2048, 10.4 by the
+// kernels for many (16 and 64 experts, rows of 4096 INT8), 13.7 as up to 4096.
 constexpr int kSmallThreads = 256;
+template <int IDS>
 __global__ __launch_bounds__(kSmallThreads) void moe_dispatch_small_kernel(const DispatchArgs a)
 {
     __shared__ int s_places[kMostEach], s_count[kMostExperts];
@@ -72,14 +75,14 @@ __global__ __launch_bounds__(kSmallThreads) void moe_dispatch_small_kernel(const
         }
         return;
     }
-    int ids[kFewPairs / 64];
+    int ids[IDS];
 #pragma unroll
-    for (int i = 0; i < kFewPairs / 64; ++i) ids[i] = 64 * i + lane < pairs ? a.experts[64 * i + lane] : -1;
+    for (int i = 0; i < IDS; ++i) ids[i] = 64 * i + lane < pairs ? a.experts[64 * i + lane] : -1;
     for (int j = wave; j < a.each; j += WAVES) {
         const int p = token * a.each + j, e = a.experts[p];
         int before = 0;
 #pragma unroll
-        for (int i = 0; i < kFewPairs / 64; ++i) {
+        for (int i = 0; i < IDS; ++i) {
             const bool counts = ids[i] >= 0 && (ids[i] < e || (ids[i] == e && 64 * i + lane < p));
             before += __popcll(__ballot(counts));
         }
@@ -313,7 +316,9 @@ extern "C" int moe_dispatch(int type, int tokens, int each, int n_experts, int K
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
     if (tokens * (long long)each <= kFewPairs) {
-        hipLaunchKernelGGL(moe_dispatch_small_kernel, dim3((unsigned)tokens + 1), dim3(kSmallThreads), 0, st, a);
+        const int pairs = tokens * each;
+        hipLaunchKernelGGL(pairs <= 128 ? moe_dispatch_small_kernel<2> : pairs <= 1024 ? moe_dispatch_small_kernel<16> : moe_dispatch_small_kernel<kFewPairs / 64>,
+                           dim3((unsigned)tokens + 1), dim3(kSmallThreads), 0, st, a);
     } else {
         hipLaunchKernelGGL(moe_places_kernel, dim3((unsigned)(n_experts * a.segments)), dim3(kSortThreads), 0, st, a);
         hipLaunchKernelGGL(moe_copy_kernel, dim3((unsigned)tokens), dim3(a.pieces > 512 ? kCopyThreads : kCopyThreads / 2), 0, st, a);

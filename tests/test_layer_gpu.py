@@ -144,6 +144,7 @@ def test_swiglu_of_large_gates():
 ROUTES = [
     # tokens, experts a token, experts
     (1, 1, 1), (1, 2, 8), (16, 2, 8), (37, 8, 64), (512, 2, 8), (513, 2, 8), (128, 8, 256), (1000, 3, 5), (4099, 1, 17), (700, 64, 200), (2500, 8, 128),
+    (64, 2, 8), (43, 3, 8), (1024, 2, 20), (683, 3, 20),  # on both sides of 128 and 2048 pairs
     (4096, 4, 3), (4097, 4, 3), (9001, 4, 6), (4500, 8, 256), (20000, 1, 128),  # several blocks an expert, and one for several batches of pairs
 ]
 
