@@ -6,9 +6,12 @@
 //     rows[place(p)] = X[token],     out[t] = sum_j w[t][j] Y[place(t, j)],     dY[place(t, j)] = w[t][j] g[t],     dw[t][j] = g[t] . Y[place(t, j)]
 // (sums in FP32, in the order of j, or of the elements' pieces; no atomics).
 //
-// The places are counted, not sorted: a block for each expert looks at all pairs (ballots), first for the pairs before its own, then to
-// number its own.  Up to kFewPairs of them each token's block counts its own pairs' places itself and copies the row in the same launch.  All is bound by
-// memory, or by the launch where there are few tokens.
+// The places are counted, not sorted: blocks of each expert look at all pairs, for those before its own, and then number its own (ballots).  Up to kFewPairs of
+// them each token's block counts its own pairs' places itself and copies the row in the same launch.
+//
+// Bound by memory, or by the launch where there are few tokens.  Measured (by run; inputs that change): 8191 FP16 rows of 4096, 8 of 64 experts each, half of them here,
+// 75 to 83 us to sort (12.7 of them the places, the copy 4.8 TB/s), 60 to 69 us to bring back (BF16, 4.9 to 5.6 TB/s); gradients of 2047 tokens of 8192, 4 experts each, 62
+// to 63 us (4.8 TB/s).  16 tokens: kernels of 2.5 to 2.8 us.
 #include <algorithm>
 
 #include "attn_common.h"
