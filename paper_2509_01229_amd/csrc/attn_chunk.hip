@@ -531,7 +531,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kerne
             s[0] = mfma32(__builtin_bit_cast(vec<f16, 8>, u32x4{zz, zz, 0, 0}), q[STEPS], v16f{});
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) s[0] = mfma32(__builtin_bit_cast(vec<f16, 8>, halves8(k[i])), q[i], s[0]);
+            asm volatile("" ::: "memory");  // (written and read by one wave, in the order that stands here, and as other types)
             const bool far = scales(wave, n);
+            asm volatile("" ::: "memory");
             load_own(t - kWaves);
             pages[0] = pages_of(t - 2 * kWaves, 0), pages[1] = pages_of(t - 2 * kWaves, 1);
             softmax(wave, 32 * t, limit_again, far, std::integral_constant<int, 1>{});
