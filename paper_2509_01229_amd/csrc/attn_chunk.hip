@@ -104,7 +104,7 @@ template <int D, class T>
 __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kernel(const ChunkArgs a)
 {
     constexpr int KW = kKeys / kWaves, DW = D / 32, STEPS = D / 16, W = D / 16;  // (a wave unpacks KW keys; a lane DW dwords of codes)
-    // Unpacked codes of two tiles (rows of keys are 16 bytes longer than they need be: lanes that read or write together meet in no bank); or, of a tile with
+    // Unpacked codes of two tiles (rows of keys are 16 bytes longer than they need be: lanes that read together meet in no bank); or, of a tile with
     // few rows, the waves' results
     struct Tiles {
         u32x4 k[2][kKeys][D / 8 + 1], v[2][D][kKeys / 8];
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kerne
         const int upto_long = sums_up_to(little ? 0 : mine * parts), upto_short = sums_up_to(little ? mine * parts : 0);
         upto = little ? __builtin_amdgcn_readlane(upto_long, 63) + upto_short : upto_long;
     }
-    // Blocks with ids 8 apart run on one XCD: each XCD gets consecutive kv heads, and goes through a head's tiles from the last (the longest rows of
+    // Blocks with ids 8 apart run on one XCD: each XCD gets consecutive kv heads, and goes through a sequence's tiles from the last (the longest rows of
     // keys) to the first.  Blocks that the grid has too many come last.
     const int blocks = all * a.Hkv, per = (blocks + 7) >> 3, id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
     if ((int)blockIdx.x >> 3 >= per || id >= blocks) return;
