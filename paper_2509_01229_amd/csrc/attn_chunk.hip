@@ -237,7 +237,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kerne
     };
     Dwords<DW> ck, cv;
     uint32_t wk, wv;  // words of the lane's key, of its keys and its values
-    const int four = lane >> 4, column = lane & 15;
+    // The lane's four keys and column group of the values (heads of 128: 16 lanes that write together have both halves of 8 pieces; for 64 it takes the register
+    // that the third block of a CU needs)
+    const int four = D == 128 ? (lane >> 2 & 2) | lane >> 5 : lane >> 4, column = D == 128 ? (lane & 7) | (lane >> 1 & 8) : lane & 15;
     const auto load_keys = [&](int p, unsigned page) __attribute__((always_inline)) {
         const buf_t b = page_at(p, page);
         const int j = ((t_first - p) * kKeys + keys_w) & (P - 1);
@@ -248,13 +250,16 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kerne
     const auto load_values = [&](int p, unsigned page) __attribute__((always_inline)) {
         const buf_t b = page_at(p, page);
         const int j = ((t_first - p) * kKeys + keys_w) & (P - 1);
-        cv.load(b, lane * (4 * DW), (P + j) * (D / 2));
+        cv.load(b, (D == 128 ? 16 * four + column : lane) * (4 * DW), (P + j) * (D / 2));
     };
 
     vec<f16, 8> q[STEPS + 1];
     float q_scale = fabsf(a.scale_log2);
     bool uneven = false;
-    const auto unpack_keys = [&](int buf, int i) __attribute__((always_inline)) { s_k[buf][keys_w + (lane >> 2)][DW * (lane & 3) + i] = halves8(ck.x[i]); };
+    // (heads of 128: pieces 8 on lie at their number XOR 2, so that the eight lanes of two keys that write together meet in no bank)
+    const auto unpack_keys = [&](int buf, int i) __attribute__((always_inline)) {
+        s_k[buf][keys_w + (lane >> 2)][(DW * (lane & 3) + i) ^ (D == 128 ? lane & 2 : 0)] = halves8(ck.x[i]);
+    };
     // Values: [element][key]; a row's 16-byte pieces have the keys that a half of the lanes multiplies at once (two fours, 8 keys apart), and lie at
     // their number XOR turn_v
     const auto turn_v = [](int d) { return ((d >> 1) ^ (d >> 4)) & 7; };
@@ -296,7 +301,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kerne
     int v_at[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) v_at[x] = n * (kKeys / 8) + ((2 * x + h) ^ turn_v(n));
-    const auto keys = [&](int buf, int u, int i) { return __builtin_bit_cast(vec<f16, 8>, s_k[buf][32 * u + n][2 * i + h]); };
+    const auto keys = [&](int buf, int u, int i) { return __builtin_bit_cast(vec<f16, 8>, s_k[buf][32 * u + n][(2 * i ^ (D == 128 && i >= STEPS / 2 ? 2 : 0)) + h]); };
     const auto values = [&](int buf, int u, int e) { return __builtin_bit_cast(vec<f16, 8>, (&s_v[buf][32 * e][0])[v_at[u ^ e]]); };
     const auto zeros = [&](int slot, int u) {
         const uint32_t zz = s_zk[slot][32 * u + n];
