@@ -26,8 +26,8 @@
 // Heads of 64 leave room for three blocks a CU: two chunks of 2048 over up to 16384, 64/8 heads, 1516 us, with two 1620.
 // Measured, heads of 128 (by machine; the clock is 1.95 to 2.2 GHz under this load): two chunks of 2048 over up to 16384, 64/8 heads, BF16, 2230 to 2470 us (820 to 900
 // TFLOP/s); 512 tokens over 1536 earlier ones, 32/8 heads, 39 us; 24 sequences with up to 4096 tokens, 640 new ones, 63; 17 of 517, 32/32 heads, 12.3.  A wave
-// takes 34 MFMAs (1088 cycles) and 250 vector instructions with 34 exponentials or the like (1330) for 32 rows and 64 keys, and 56 reads of LDS (448 cycles of the four that share it: 49%
-// with the writes, none of which meet in a bank); two waves a SIMD make that in 2600 cycles each, so that MFMAs (43%) and vector instructions (51 to 57%) hardly overlap.  Tried, and slower or
+// takes 34 MFMAs (1088 cycles) and 250 vector instructions with 34 exponentials or the like (1330) for 32 rows and 64 keys, and 56 reads of LDS of 16 bytes a lane
+// (49% of its cycles, with the writes; none meet in a bank); two waves a SIMD make that in 2600 cycles each, so that MFMAs (43%) and vector instructions (51 to 57%) hardly overlap.  Tried, and slower or
 // within 1% (2270 us beside them): two tiles of rows a wave with one wave a SIMD (3480 when this took 2660; halves the LDS reads); blocks of 8 waves and 256 rows, of which four
 // unpack keys and four values (2524), the same half a tile apart with two barriers a tile (2461: a softmax alone takes a wave 2500 cycles, a quarter of them
 // waiting for the keys' scales, and that is then the time of every half); fragments read two slices ahead; one of the two blocks of a CU ahead by priority; the maximum
