@@ -294,7 +294,15 @@ __global__ __launch_bounds__(kGradThreads) void moe_combine_backward_kernel(cons
 using namespace lqq;
 
 namespace {
-constexpr int kMostBlocks = 1 << 23;  // (a launch holds fewer than 2^32 threads)
+constexpr int kMostBlocks = 1 << 23;
+// A launch holds fewer than 2^32 threads: so many blocks of a size are one (half of what there could be)
+constexpr long long blocks_of_launch(int threads) { return (1LL << 31) / threads; }
+// launch(first, n) for the tokens, as many at a time as a launch holds
+template <class F>
+void in_launches(int tokens, long long at_once, F launch)
+{
+    for (long long first = 0; first < tokens; first += at_once) launch(first, (int)std::min<long long>(at_once, tokens - first));
+}
 int type_bytes(int type) { return type == LQ_I8 ? 1 : type == LQ_F16 || type == LQ_BF16 ? 2 : 0; }
 bool pairs_ok(int tokens, int each) { return tokens >= 0 && each >= 1 && each <= kMostEach && (long long)tokens * each < (1LL << 31) - kBatchPairs; }
 }  // namespace
@@ -324,7 +332,14 @@ extern "C" int moe_dispatch(int type, int tokens, int each, int n_experts, int K
                            dim3((unsigned)tokens + 1), dim3(kSmallThreads), 0, st, a);
     } else {
         hipLaunchKernelGGL(moe_places_kernel, dim3((unsigned)(n_experts * a.segments)), dim3(kSortThreads), 0, st, a);
-        hipLaunchKernelGGL(moe_copy_kernel, dim3((unsigned)tokens), dim3(a.pieces > 512 ? kCopyThreads : kCopyThreads / 2), 0, st, a);
+        const int threads = a.pieces > 512 ? kCopyThreads : kCopyThreads / 2;
+        in_launches(tokens, blocks_of_launch(threads), [&](long long first, int n) {
+            DispatchArgs b = a;
+            b.x += first * a.x_row;
+            if (a.scales) b.scales += first;
+            b.places += first * each;
+            hipLaunchKernelGGL(moe_copy_kernel, dim3((unsigned)n), dim3((unsigned)threads), 0, st, b);
+        });
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? LQ_OK : fail(LQ_ERR_HIP, "dispatch launch failed: %s", hipGetErrorString(e));

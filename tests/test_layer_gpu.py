@@ -445,3 +445,31 @@ def test_through_the_native_module_and_without(monkeypatch):
             assert (f is None) == (g is None)
             if f is not None:
                 assert f.dtype == g.dtype and f.shape == g.shape and torch.equal(f.view(torch.uint8), g.view(torch.uint8))
+
+
+# ------------------------------------------------------------------------------- millions of tokens
+def test_dispatch_of_millions_of_tokens():
+    """More tokens than one launch holds where a row has 1024 threads.  Nearly all of them go to experts that are elsewhere, so that the rows are few; the tokens' rows overlap
+    in memory, eight elements apart."""
+    import ctypes
+
+    import torch
+
+    T, each, E, K = 2 ** 22 + 5, 2, 3, 4104
+    rng = np.random.default_rng(40)
+    ids = torch.full((T, each), -1, dtype=torch.int32)
+    tokens = sorted({0, 1, 2 ** 21 - 1, 2 ** 21, 2 ** 21 + 1, 2 ** 22 - 1, 2 ** 22, T - 1, *rng.integers(0, T, 50).tolist()})
+    ids[tokens] = torch.from_numpy(rng.integers(-1, E + 1, (len(tokens), each)).astype(np.int32))
+    offsets, places, source = R.dispatch(ids.numpy(), E)
+    buffer = torch.randn(8 * T + K, device="cuda").half()
+    scales, ids = torch.rand(T, device="cuda"), ids.cuda()
+    rows, row_scales = torch.full((len(source) + 2, K), 99.0, dtype=torch.float16, device="cuda"), torch.full((len(source) + 2,), 99.0, device="cuda")
+    got_offsets, got_places = torch.empty(E + 1, dtype=torch.int32, device="cuda"), torch.empty((T, each), dtype=torch.int32, device="cuda")
+    pointer = lambda t: ctypes.c_void_p(t.data_ptr())  # noqa: E731
+    rc = api.lib().moe_dispatch(api.LQ_F16, T, each, E, K, pointer(buffer), 8, pointer(scales), pointer(ids), pointer(rows), pointer(row_scales),
+                                pointer(got_offsets), pointer(got_places), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    assert rc == 0
+    assert np.array_equal(got_offsets.cpu().numpy(), offsets) and np.array_equal(got_places.cpu().numpy(), places)
+    n, source = len(source), _gpu(source)
+    assert torch.equal(rows[:n], buffer.as_strided((T, K), (8, 1))[source]) and (rows[n:] == 99).all()
+    assert torch.equal(row_scales[:n], scales[source]) and (row_scales[n:] == 99).all()
