@@ -294,7 +294,7 @@ __global__ __launch_bounds__(kGradThreads) void moe_combine_backward_kernel(cons
 using namespace lqq;
 
 namespace {
-constexpr int kMostBlocks = 1 << 23;
+constexpr int kMostTokens = 1 << 23;
 // A launch holds fewer than 2^32 threads: so many blocks of a size are one (half of what there could be)
 constexpr long long blocks_of_launch(int threads) { return (1LL << 31) / threads; }
 // launch(first, n) for the tokens, as many at a time as a launch holds
@@ -312,7 +312,7 @@ extern "C" int moe_dispatch(int type, int tokens, int each, int n_experts, int K
 {
     const int size = type_bytes(type);
     if (!size) return fail(LQ_ERR_INVALID, "type must be LQ_F16, LQ_BF16 or LQ_I8, got %d", type);
-    if (!pairs_ok(tokens, each) || tokens > kMostBlocks - 1) return fail(LQ_ERR_INVALID, "bad shape: %d tokens of %d experts each (1 to %d; up to 2^23 tokens)", tokens, each, kMostEach);
+    if (!pairs_ok(tokens, each) || tokens >= kMostTokens) return fail(LQ_ERR_INVALID, "bad shape: %d tokens of %d experts each (1 to %d; up to 2^23 tokens)", tokens, each, kMostEach);
     if (n_experts < 1 || n_experts > kMostExperts) return fail(LQ_ERR_INVALID, "n_experts must be 1 to %d, got %d", kMostExperts, n_experts);
     if (K < 1 || K > (1 << 24) || K * size % 16) return fail(LQ_ERR_INVALID, "bad shape: rows of %d elements (a multiple of 16 bytes)", K);
     if (!row_offsets || (tokens && (!X || !experts || !rows || !places))) return fail(LQ_ERR_INVALID, "null pointer");
@@ -357,9 +357,7 @@ extern "C" int moe_combine(int dtype, int tokens, int each, int rows, int N, con
                            void *out, void *hip_stream)
 {
     if (const int rc = combine_shape(dtype, tokens, each, rows, N); rc != LQ_OK) return rc;
-    const int pieces = N / 8;
-    const long long blocks = (long long)tokens * ((pieces + kCombineThreads - 1) / kCombineThreads);
-    if (blocks > kMostBlocks) return fail(LQ_ERR_INVALID, "too large: %d tokens of %d elements", tokens, N);
+    const int pieces = N / 8, chunks = (pieces + kCombineThreads - 1) / kCombineThreads;  // (up to 2^13 blocks a token)
     if (tokens == 0) return LQ_OK;
     if ((rows && !Y) || !places || !out) return fail(LQ_ERR_INVALID, "null pointer");
     if (((uintptr_t)Y | (uintptr_t)out) & 15) return fail(LQ_ERR_ALIGN, "Y and out must be 16-byte aligned");
@@ -367,8 +365,14 @@ extern "C" int moe_combine(int dtype, int tokens, int each, int rows, int N, con
     if (rows > 1 && y_row % 8) return fail(LQ_ERR_ALIGN, "the stride of Y's rows must be a multiple of 8 elements, got %lld", y_row);
     const CombineArgs a{Y, nullptr, places, nullptr, weights, out, nullptr, rows > 1 ? y_row : 0, 0, tokens, each, rows, pieces};
     (void)hipGetLastError();
-    hipLaunchKernelGGL(dtype == LQ_F16 ? moe_combine_kernel<f16> : moe_combine_kernel<bf16>, dim3((unsigned)blocks), dim3(kCombineThreads), 0,
-                       static_cast<hipStream_t>(hip_stream), a);
+    in_launches(tokens, blocks_of_launch(kCombineThreads) / chunks, [&](long long first, int n) {
+        CombineArgs b = a;
+        b.places += first * each;
+        if (weights) b.weights += first * each;
+        b.out = static_cast<char *>(out) + 2 * first * N;
+        hipLaunchKernelGGL(dtype == LQ_F16 ? moe_combine_kernel<f16> : moe_combine_kernel<bf16>, dim3((unsigned)n * (unsigned)chunks), dim3(kCombineThreads), 0,
+                           static_cast<hipStream_t>(hip_stream), b);
+    });
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? LQ_OK : fail(LQ_ERR_HIP, "combine launch failed: %s", hipGetErrorString(e));
 }
@@ -377,7 +381,7 @@ extern "C" int moe_combine_backward(int dtype, int tokens, int each, int rows, i
                                     const int *places, const float *weights, const int *rows_used, void *grad_Y, float *grad_weights, void *hip_stream)
 {
     if (const int rc = combine_shape(dtype, tokens, each, rows, N); rc != LQ_OK) return rc;
-    if (tokens > kMostBlocks - 1024) return fail(LQ_ERR_INVALID, "too large: %d tokens", tokens);
+    if (tokens >= kMostTokens) return fail(LQ_ERR_INVALID, "too large: %d tokens (up to 2^23)", tokens);
     if ((tokens && (!grad || !places || !weights || !grad_weights)) || (rows && (!Y || !grad_Y))) return fail(LQ_ERR_INVALID, "null pointer");
     if (((uintptr_t)grad | (uintptr_t)Y | (uintptr_t)grad_Y) & 15) return fail(LQ_ERR_ALIGN, "grad, Y and grad_Y must be 16-byte aligned");
     if (((uintptr_t)places | (uintptr_t)weights | (uintptr_t)rows_used | (uintptr_t)grad_weights) & 3)
@@ -387,8 +391,21 @@ extern "C" int moe_combine_backward(int dtype, int tokens, int each, int rows, i
     if (tokens + clearing == 0) return LQ_OK;
     const CombineArgs a{Y, grad, places, rows_used, weights, grad_Y, grad_weights, rows > 1 ? y_row : 0, tokens > 1 ? grad_row : 0, tokens, each, rows, pieces};
     (void)hipGetLastError();
-    hipLaunchKernelGGL(dtype == LQ_F16 ? moe_combine_backward_kernel<f16> : moe_combine_backward_kernel<bf16>, dim3((unsigned)(tokens + clearing)),
-                       dim3(pieces > 256 ? kGradThreads : 256), 0, static_cast<hipStream_t>(hip_stream), a);
+    const int threads = pieces > 256 ? kGradThreads : 256;
+    const auto go = [&](long long first, int n) {
+        CombineArgs b = a;
+        b.grad = static_cast<const char *>(grad) + 2 * first * a.grad_row;
+        b.places += first * each;
+        b.weights += first * each;
+        b.grad_weights += first * each;
+        b.tokens = n;
+        hipLaunchKernelGGL(dtype == LQ_F16 ? moe_combine_backward_kernel<f16> : moe_combine_backward_kernel<bf16>, dim3((unsigned)(n + (first ? 0 : clearing))),
+                           dim3((unsigned)threads), 0, static_cast<hipStream_t>(hip_stream), b);
+    };
+    if (tokens)
+        in_launches(tokens, blocks_of_launch(threads), go);
+    else
+        go(0, 0);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? LQ_OK : fail(LQ_ERR_HIP, "gradient launch failed: %s", hipGetErrorString(e));
 }

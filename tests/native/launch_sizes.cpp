@@ -61,6 +61,19 @@ int main()
                 check("dispatch", tokens, K, rc, 1, tokens);
             }
     }
+    // (back: as many blocks a token as its row has pieces of 256 times 16 bytes; the gradients: 256 blocks clear what no expert has)
+    for (const int tokens : {0, 1, (1 << 21) + 3, 1 << 22, 5000000, (1 << 23) - 1025, (1 << 23) - 1024, (1 << 23) - 1, 1 << 23, (1 << 24) + 5}) {
+        for (const int N : {8, 2048, 2056, 4096, 8200, 1 << 24}) {
+            if ((long long)tokens * ((N + 2047) / 2048) < 1LL << 31) {
+                const int rc = moe_combine(LQ_BF16, tokens, 2, 100, N, p, N, ints, nullptr, p, nullptr);
+                check("combine", tokens, N, rc, 0, (unsigned long long)tokens * ((N + 2047) / 2048));
+            }
+            if (tokens < 1 << 23) {
+                const int rc = moe_combine_backward(LQ_F16, tokens, 2, 100, N, p, N, p, N, ints, reinterpret_cast<float *>(p), ints, p, reinterpret_cast<float *>(p), nullptr);
+                check("gradients", tokens, N, rc, 0, tokens + 256ull);
+            }
+        }
+    }
     if (wrong) return 1;
     printf("launch_sizes ok\n");
     return 0;

@@ -473,3 +473,42 @@ def test_dispatch_of_millions_of_tokens():
     n, source = len(source), _gpu(source)
     assert torch.equal(rows[:n], buffer.as_strided((T, K), (8, 1))[source]) and (rows[n:] == 99).all()
     assert torch.equal(row_scales[:n], scales[source]) and (row_scales[n:] == 99).all()
+
+
+@pytest.mark.parametrize("T,N,weighted", [(2 ** 23 + 9, 8, True), (2 ** 22 + 7, 2056, False)])
+def test_combine_of_millions_of_tokens(T, N, weighted):
+    """More blocks than one launch holds; nearly all tokens have no row."""
+    import torch
+
+    rng = np.random.default_rng(41)
+    tokens = sorted({0, 1, 2 ** 21, 2 ** 22 - 1, 2 ** 22, T - 10, T - 9, T - 8, T - 1, *rng.integers(0, T, 40).tolist()})
+    Y, places, w = _draw(rng, (30, N), A.BF16), torch.full((T, 2), -1, dtype=torch.int32), torch.from_numpy(rng.random((T, 2)).astype(np.float32))
+    places[tokens] = torch.from_numpy(rng.integers(0, 30, (len(tokens), 2)).astype(np.int32))
+    out = torch.full((T, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    assert api.moe_combine(_gpu(Y, A.BF16), places.cuda(), w.cuda() if weighted else None, out=out) is out
+    want, size = R.combine(Y, places[tokens].numpy(), w[tokens].numpy() if weighted else None)
+    at = _gpu(np.array(tokens))
+    assert (np.abs(_np(out[at]) - want) <= A.UNIT[A.BF16] * np.abs(want) * 1.001 + 3 * 2.0 ** -24 * size + 2.0 ** -25).all()
+    out[at] = 0
+    assert not out.any()
+
+
+@pytest.mark.parametrize("T,N", [(2 ** 22 + 5, 4104), (2 ** 23 - 1, 8)])
+def test_gradients_of_millions_of_tokens(T, N):
+    """The same of the gradients (whose rows overlap in memory, eight elements apart)."""
+    import torch
+
+    rng = np.random.default_rng(42)
+    ids = torch.full((T, 2), -1, dtype=torch.int32)
+    tokens = sorted({0, 1, 2 ** 21, 2 ** 22 - 1, 2 ** 22, T - 2, T - 1, *rng.integers(0, T, 40).tolist()})
+    ids[tokens] = torch.from_numpy(rng.integers(-1, 4, (len(tokens), 2)).astype(np.int32))
+    offsets, places, source = R.dispatch(ids.numpy(), 3)
+    rows = len(source) + 3
+    grad, Y, w = torch.randn(8 * T + N, device="cuda").half().as_strided((T, N), (8, 1)), _draw(rng, (rows, N), A.F16), torch.rand((T, 2), device="cuda")
+    gY, gw = api.moe_combine_backward(grad, _gpu(Y, A.F16), _gpu(places), w, row_offsets=_gpu(offsets))
+    at = _gpu(np.array(tokens))
+    of_rows, of_weights, size = R.combine_backward(_np(grad[at]), Y, places[tokens], w[at].cpu().numpy(), A.F16)
+    assert np.array_equal(_np(gY)[:len(source)], of_rows[:len(source)]) and not gY[len(source):].any()
+    assert (np.abs(gw[at].double().cpu().numpy() - of_weights) <= (N / 256 + 16) * 2.0 ** -24 * size).all()
+    gw[at] = 0
+    assert not gw.any()
