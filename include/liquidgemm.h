@@ -277,7 +277,7 @@ int w4a8_quantize_activations(int M, int K, const uint16_t *X_f16, const float *
 int w4a8_norm_quantize(int dtype, int M, int K, const void *x, long long x_row, const void *residual, long long residual_row,
                        const float *weight, float eps, void *h, void *y_out, int8_t *X_i8, float *act_scales, void *hip_stream);
 
-/* y = gate / (1 + exp(-gate)) * up for x [M, 2K], a row's K gates before its K ups, in FP32 (to within (4 + |gate|) * 2^-22 of itself),
+/* y = gate / (1 + exp(-gate)) * up for x [M, 2K], a row's K gates before its K ups, in FP32 (to within (4 + |gate|) * 2^-22 of itself, or 2^-149),
  * quantised as above.  Rows with a NaN or an infinity in x or y give unspecified codes for that row only. */
 int w4a8_swiglu_quantize(int dtype, int M, int K, const void *x, long long x_row, int8_t *X_i8, float *act_scales, void *hip_stream);
 

@@ -512,3 +512,26 @@ def test_gradients_of_millions_of_tokens(T, N):
     assert (np.abs(gw[at].double().cpu().numpy() - of_weights) <= (N / 256 + 16) * 2.0 ** -24 * size).all()
     gw[at] = 0
     assert not gw.any()
+
+
+# ------------------------------------------------------------------- gates and rows at the ends of FP32
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("K", [64, 33000])
+def test_swiglu_of_gates_whose_exponential_overflows(dtype, K):
+    """exp(-gate) overflows FP32 from a gate of -88.7 on, where gate * exp(gate) * up is still an ordinary number if up is large: rows of such gates alone, and of some next to
+    others.  A subnormal result is rounded to 2^-149, and so is the scale, which 127 times that is an error of a value; hence the absolute term."""
+    rng = np.random.default_rng(K)
+    ranges = [(-81, -79), (-89, -86), (-90, -89), (-96, -90), (-104, -96), (-115, -104)] + ([(-150, -115), (-180, -150), (-192, -180)] if dtype == A.BF16 else [])
+    gate = np.stack([rng.uniform(a, b, K) for a, b in ranges] + [np.where(np.arange(K) % 5 == 2, rng.uniform(-100, -70, K), rng.standard_normal(K))])
+    up = np.exp2(rng.uniform(110, 127, gate.shape) if dtype == A.BF16 else rng.uniform(5, 15.9, gate.shape)) * rng.choice([-1, 1], gate.shape)
+    up[-1] = np.where(gate[-1] < -60, up[-1], 2.0 ** -30)
+    x = A.round_to(np.concatenate([gate, up], 1).astype(np.float32), dtype)
+    q, s = (t.cpu().numpy().astype(np.float64) for t in api.w4a8_swiglu_quantize(_gpu(x, dtype)))
+    y, least = R.gated(x), 128 * 2.0 ** -149
+    d = (4 + np.abs(x[:, :K].astype(np.float64))) * 2.0 ** -22
+    most = np.abs(y).max(-1)
+    assert (most > 2 * least).sum() >= len(x) - 1
+    assert (np.abs(s * 127 - most) <= (d * np.abs(y)).max(-1) + 2.0 ** -23 * most + least)[most > 2 * least].all()
+    assert (np.abs(q * s[:, None] - y) <= s[:, None] * (0.5 + 127 * 2.0 ** -22) + d * np.abs(y) + least).all()
+    one = api.w4a8_swiglu_quantize(_gpu(x[:, np.r_[0:8, K:K + 8]], dtype))    # (whatever stands next to a gate)
+    assert np.isfinite(one[1].cpu().numpy()).all()
