@@ -269,7 +269,7 @@ int w4a8_quantize_activations(int M, int K, const uint16_t *X_f16, const float *
 /* The residual's addition, the root-mean-square norm and the INT8 quantisation in one pass:
  *   h = x + residual, rounded to the type (h = x where residual and h are NULL)   -> h, [M,K] (what the next layer adds to)
  *   r = fp32(1 / sqrt(mean(h^2) + eps)), the mean and the root in FP64;  y = (h * weight) * r, each product rounded to FP32
- *   act_scales[m] = max_k |y| / 127  (1 if the row is zero);  X_i8 = clamp(rint(y / act_scales[m]), -127, 127)
+ *   act_scales[m] = max_k |y| / 127  (1 if that is zero);  X_i8 = clamp(rint(y / act_scales[m]), -127, 127)
  *   y rounded to the type -> y_out [M,K], where it is not NULL (for a router)
  * weight: device FP32 [K], or NULL for ones.  h may be residual or x itself (rows without gaps); other overlaps are not allowed.
  * eps: positive.  The results are determined bit for bit (but where the FP64 mean lies within 2^-50 of a rounding border).  Rows with a NaN or an

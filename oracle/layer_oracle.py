@@ -12,8 +12,8 @@ from .attention_oracle import round_to
 
 def quantise_rows(y):
     """y [M, K] float32 -> codes int8, scales float32: every operation one FP32 rounding."""
-    most = np.abs(y).max(-1)
-    scales = np.where(most > 0, most / np.float32(127), np.float32(1)).astype(np.float32)
+    scales = (np.abs(y).max(-1) / np.float32(127)).astype(np.float32)
+    scales[scales == 0] = 1
     return np.clip(np.rint(y / scales[:, None]), -127, 127).astype(np.int8), scales
 
 

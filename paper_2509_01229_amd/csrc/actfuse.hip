@@ -4,7 +4,7 @@
 //     h  = T(x + residual)                        (where there is a residual: what the next layer adds to, rounded to the type)
 //     r  = fp32(1 / sqrt(mean(h^2) + eps))        (mean and root in FP64, rounded once)
 //     y  = (h * weight) * r                       |     y = gate / (1 + exp(-gate)) * up
-//     s  = max |y| / 127   (1 where the row is zero),   Q = clamp(rint(y / s), -127, 127)
+//     s  = max |y| / 127   (1 where that is zero),   Q = clamp(rint(y / s), -127, 127)
 //
 // The norm: squares of 11-bit (8-bit) numbers are exact in FP64 and their sum is right to 2^-50, so whatever the order of the additions r is the
 // definition's but for one sum in 2^25 that lies that near a rounding border; everything behind it is single FP32 roundings, which makes the codes
@@ -39,6 +39,13 @@ struct GateArgs {
     long long x_row;
     int K;
 };
+
+// A row's scale, from its largest value: 1 for a row of zeros, or of numbers too small for a scale
+__device__ __forceinline__ float scale_of(float most)
+{
+    const float s = most / 127.0f;
+    return s > 0.0f ? s : 1.0f;
+}
 
 template <class T>
 __device__ __forceinline__ void widen(const u32x4 x, float (&f)[8])
@@ -152,7 +159,7 @@ __global__ __launch_bounds__(NT) void norm_quantize_rows_kernel(const NormArgs a
         most = max_abs8(f[it], most);
     }
     norm_of_row<NT / 64>(sum, most, r, a);
-    const float s = most > 0.0f ? most / 127.0f : 1.0f, rcp_s = __builtin_amdgcn_rcpf(s);
+    const float s = scale_of(most), rcp_s = __builtin_amdgcn_rcpf(s);
     if (threadIdx.x == 0) a.scales[m] = s;
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
@@ -183,7 +190,7 @@ __global__ __launch_bounds__(kLongRow) void norm_quantize_long_kernel(const Norm
         most = max_abs8(f, most);
     }
     norm_of_row<kLongRow / 64>(sum, most, r, a);
-    const float s = most > 0.0f ? most / 127.0f : 1.0f, rcp_s = __builtin_amdgcn_rcpf(s);
+    const float s = scale_of(most), rcp_s = __builtin_amdgcn_rcpf(s);
     if (threadIdx.x == 0) a.scales[m] = s;
     for (int piece = threadIdx.x; piece < n8; piece += kLongRow) {
         widen<T>(RESIDUAL ? h[piece] : stream_of<T, false>(a, m, piece), f);
@@ -234,7 +241,7 @@ __global__ __launch_bounds__(NT) void swiglu_quantize_rows_kernel(const GateArgs
         most = max_abs8(f[it], most);
     }
     most = block_max<NT / 64>(most, s_part);
-    const float s = most > 0.0f ? most / 127.0f : 1.0f, rcp_s = __builtin_amdgcn_rcpf(s);
+    const float s = scale_of(most), rcp_s = __builtin_amdgcn_rcpf(s);
     if (threadIdx.x == 0) a.scales[m] = s;
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
@@ -254,7 +261,7 @@ __global__ __launch_bounds__(kLongRow) void swiglu_quantize_long_kernel(const Ga
         most = max_abs8(f, most);
     }
     most = block_max<kLongRow / 64>(most, s_part);
-    const float s = most > 0.0f ? most / 127.0f : 1.0f, rcp_s = __builtin_amdgcn_rcpf(s);
+    const float s = scale_of(most), rcp_s = __builtin_amdgcn_rcpf(s);
     if (threadIdx.x == 0) a.scales[m] = s;
     for (int piece = threadIdx.x; piece < n8; piece += kLongRow) {
         gated<T>(a, m, piece, f);

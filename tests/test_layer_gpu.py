@@ -535,3 +535,21 @@ def test_swiglu_of_gates_whose_exponential_overflows(dtype, K):
     assert (np.abs(q * s[:, None] - y) <= s[:, None] * (0.5 + 127 * 2.0 ** -22) + d * np.abs(y) + least).all()
     one = api.w4a8_swiglu_quantize(_gpu(x[:, np.r_[0:8, K:K + 8]], dtype))    # (whatever stands next to a gate)
     assert np.isfinite(one[1].cpu().numpy()).all()
+
+
+def test_rows_whose_scale_is_subnormal():
+    """Rows so small that the scale has few bits, or none: codes are those of the division by the scale, up to 127 (and of a row without a scale 0, with scale 1)."""
+    rng = np.random.default_rng(50)
+    K, sizes = 256, np.array([2.0 ** -e for e in (120, 125, 126, 127, 130, 133, 136, 138, 139, 140, 141, 142, 143, 144, 146, 149)], dtype=np.float32)
+    x = _draw(rng, (len(sizes), K), A.BF16)
+    x[:, 0] = 0
+    for weight in (sizes[:, None] * np.float32(1.0) * np.ones((1, K), dtype=np.float32)):
+        q, s, _, y = R.norm_quantise(x, None, weight, 1e-6, A.BF16)
+        got = api.w4a8_norm_quantize(_gpu(x, A.BF16), _gpu(weight), eps=1e-6)
+        assert np.array_equal(got[1].cpu().numpy().view(np.uint32), s.view(np.uint32)) and np.array_equal(got[0].cpu().numpy(), q), weight[0]
+    # gates of 64, whose logistic is 1 in FP32; ups as small as the type has them
+    up = A.round_to(rng.standard_normal((len(sizes), K)).astype(np.float32) * sizes[:, None] * np.float32(2.0 ** -6), A.BF16)
+    up[:, 1] = 0
+    q, s = R.quantise_rows((np.float32(64) * up).astype(np.float32))
+    got = api.w4a8_swiglu_quantize(_gpu(np.concatenate([np.full_like(up, 64), up], 1), A.BF16))
+    assert np.array_equal(got[1].cpu().numpy().view(np.uint32), s.view(np.uint32)) and np.array_equal(got[0].cpu().numpy(), q)
