@@ -9,7 +9,8 @@
 // quarter of them.  Both products run on 32x32x16 MFMAs with the cache as the first operand (S^T = K Q^T, O^T = V^T P^T): a lane's scores are 32
 // keys of one row, in the order in which the weights enter the second product.  Value codes lie in a page as pairs of tokens, and so they are unpacked to
 // [element][keys]: both operands come out of LDS in 16-byte reads.  Codes are masked out of their dword (5 instructions for 8) and go in as the subnormal FP16
-// numbers that they then are, which the matrix cores multiply exactly; what the keys' zero points take off the scores is one more product, with the sum of a query's
+// numbers that they then are, whose products the matrix cores form exactly (and cut, in sums of eight, below 2^-24 of the largest, in which a subnormal number counts as 2^-14: a
+// key loses at most 2^-14 of the largest weight of its eight for each element); what the keys' zero points take off the scores is one more product, with the sum of a query's
 // elements; the values' are taken off the codes (4 more instructions), as their sums may cancel.
 //
 // The scales never meet the codes.  The keys' are applied to the scores; the values' enter as logarithms,
@@ -23,9 +24,14 @@
 // own, 32 at a time, straight from the cache into the operands' registers, and the waves' results are joined in LDS at the end.  (24 sequences, three of them
 // chunks, 97 -> 73 us; 17 tokens of 517, 32 heads, 18.2 -> 15.6.)
 //
+// There, where the result is FP16, what the rounding of a weight leaves goes into the second product as a second number, so that a token has the same error as in a
+// step of single tokens (attn_decode.hip): 2.1e-4 of the result, that of its own rounding, with one number 2.8 to 2.9e-4.  It costs 17 tokens of 517 12.5 -> 13.2 us, 64 single tokens over
+// up to 4096, 32/8 heads, 51 -> 58, the 24 sequences 63.6 -> 64.5.  Tiles of more rows have one number a weight, as attn_prompt.hip's have: with two, chunks of FP16 take 2425 -> 3250 us
+// (two of 2048 over up to 16384), the 24 sequences 76.  Beside the rounding of BF16 results neither shows (1.67e-3 for 1.66e-3).
+//
 // Heads of 64 leave room for three blocks a CU: two chunks of 2048 over up to 16384, 64/8 heads, 1516 us, with two 1620.
 // Measured, heads of 128 (by machine; the clock is 1.95 to 2.2 GHz under this load): two chunks of 2048 over up to 16384, 64/8 heads, BF16, 2230 to 2470 us (820 to 900
-// TFLOP/s); 512 tokens over 1536 earlier ones, 32/8 heads, 39 us; 24 sequences with up to 4096 tokens, 640 new ones, 63; 17 of 517, 32/32 heads, 12.3.  A wave
+// TFLOP/s); 512 tokens over 1536 earlier ones, 32/8 heads, 39 us; 24 sequences with up to 4096 tokens, 640 new ones, 64; 17 of 517, 32/32 heads, 13.2.  A wave
 // takes 34 MFMAs (1088 cycles) and 250 vector instructions with 34 exponentials or the like (1330) for 32 rows and 64 keys, and 56 reads of LDS of 16 bytes a lane
 // (49% of its cycles, with the writes; none meet in a bank); two waves a SIMD make that in 2600 cycles each, so that MFMAs (43%) and vector instructions (51 to 57%) hardly overlap.  Tried, and slower or
 // within 1% (2270 us beside them): two tiles of rows a wave with one wave a SIMD (3480 when this took 2660; halves the LDS reads); blocks of 8 waves and 256 rows, of which four
@@ -104,6 +110,7 @@ template <int D, class T>
 __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kernel(const ChunkArgs a)
 {
     constexpr int KW = kKeys / kWaves, DW = D / 32, STEPS = D / 16, W = D / 16;  // (a wave unpacks KW keys; a lane DW dwords of codes)
+    constexpr bool kTwo = __is_same(T, f16);  // (two numbers a weight, in tiles of few rows)
     // Unpacked codes of two tiles (rows of keys are 16 bytes longer than they need be: lanes that read together meet in no bank); or, of a tile with
     // few rows, the waves' results
     struct Tiles {
@@ -310,7 +317,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kerne
     };
 
     v16f o[D / 32], s[2];
-    vec<f16, 8> w[4];
+    vec<f16, 8> w[4], rest[2];  // weights as FP16 numbers, and what the rounding leaves of them
     float m = -__builtin_inff(), l = 0.0f;  // maximum of t, this lane's part of sum x / sv
     // The softmax of place p's scores: s -> w, l, m
     const auto softmax = [&](int slot, int key, int limit, bool far, auto n_u) __attribute__((always_inline)) {
@@ -368,8 +375,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kerne
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float x = __builtin_amdgcn_exp2f(s[i >> 2][4 * (i & 3) + e] + base);
+                const f16 y = (f16)x;
                 l = __builtin_fmaf(x, rv[e], l);
-                w[i >> 1][4 * (i & 1) + e] = (f16)x;
+                w[i >> 1][4 * (i & 1) + e] = y;
+                if constexpr (U == 1 && kTwo) rest[i >> 1][4 * (i & 1) + e] = (f16)__builtin_fmaf((float)y, -1.0f, x);
             }
         }
         if constexpr (U == 2) asm volatile("" : "+v"(l), "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));  // (here, not among the products, where the scores would have to stay)
@@ -553,7 +562,11 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kerne
                     for (int i = 0; i < 2; ++i) x[g][i] = halves8(D == 128 ? v_now[u][g][i] : v_now[u][g][i] >> (8 * (n & 1)), i ? z4.y : z4.x);
                 }
 #pragma unroll
-                for (int e = 0; e < D / 32; ++e) o[e] = mfma32(__builtin_bit_cast(vec<f16, 8>, u32x4{x[0][0][e], x[0][1][e], x[1][0][e], x[1][1][e]}), w[u], o[e]);
+                for (int e = 0; e < D / 32; ++e) {
+                    const auto codes = __builtin_bit_cast(vec<f16, 8>, u32x4{x[0][0][e], x[0][1][e], x[1][0][e], x[1][1][e]});
+                    o[e] = mfma32(codes, w[u], o[e]);
+                    if constexpr (kTwo) o[e] = mfma32(codes, rest[u], o[e]);
+                }
             }
         }
     } else if (n_tiles > 0) {

@@ -419,3 +419,36 @@ def test_through_the_native_module_and_without(monkeypatch):
         monkeypatch.setattr(api, "_native", stands_in)
         assert torch.equal(call(), want)
     assert len(answers) == 1 and answers[0] is not None
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 1), (8, 8)])
+def test_fp16_results_of_few_rows_have_their_own_rounding_alone(D, Hq, Hkv):
+    """Tiles of up to 32 rows multiply the weights as two FP16 numbers each where the result is FP16, as kv4_attention does.
+
+    Queries are small whole numbers, so that the products with the codes and their sums are exact; a score (below 16) times its scale and the logarithm of the value's scale are off
+    by 2^-19 at most, the second number of a weight leaves 2^-22 of it, sums of 60 terms in FP32 are off by 2^-18 of the terms: together below 2^-16 of sum_j p_j |v_j|.  Beside that, the
+    matrix cores cut the products that they add up, of eight keys at a time, below 2^-24 of the largest, and a subnormal number counts as 2^-14 in that.  A weight's product with a code
+    difference, which is the difference times 2^-24 in the even places of a dword (times 2^-20 in the odd ones), so loses up to 2^(24 - 14 - 24) = 2^-14 of the largest weight times its value's scale
+    among the eight keys; these lie in sixteen consecutive ones, the rests of the weights lose 2^-11 of that.  Hence 16 * 2^-14 of the largest p_j s_j of every sixteen keys."""
+    rng = np.random.default_rng(D + Hkv)
+    new, contexts, page = [1, 2, 1, 4, 1, 3], [2, 5, 17, 33, 60, 3], 16
+    cache, table, keys, values = _filled(rng, contexts, page, Hkv, D, A.F16)
+    starts = _starts(new)
+    q = rng.integers(-2, 3, (starts[-1], Hq, D)).astype(np.float32)
+    args = (cache, _gpu(table), _ints(contexts))
+    got = _np(api.kv4_attention_chunks(_gpu(q, A.F16), *args, _ints(starts)))
+    for s, c in enumerate(contexts):
+        mine, limit = slice(starts[s], starts[s + 1]), c - new[s] + 1 + np.arange(new[s])
+        want, spread = A.attention(q[mine], keys[s], values[s], D ** -0.5, limit)
+        k, v = (np.repeat(x.astype(np.float64), Hq // Hkv, 1) for x in (keys[s], values[s]))
+        scores = np.einsum("nhd,khd->nhk", q[mine].astype(np.float64), k) * D ** -0.5
+        scores = np.where(np.arange(c) < limit[:, None, None], scores, -np.inf)
+        p = np.exp(scores - scores.max(-1, keepdims=True))
+        step = np.stack([[np.diff(np.unique(x)).min(initial=np.inf) for x in row] for row in v])                 # [keys, heads]: numbers are whole multiples of the scale apart
+        step = np.where(np.isfinite(step), step, 0.0)
+        weighed = p / p.sum(-1, keepdims=True) * step.T
+        weighed = np.pad(weighed, ((0, 0), (0, 0), (0, -c % 16))).reshape(*p.shape[:2], -1, 16).max(-1).sum(-1)
+        tol = 1.1 * (A.UNIT[A.F16] * np.abs(want) + 2.0 ** -16 * spread) + 2.0 ** -24 + 16 * 2.0 ** -14 * 1.001 * weighed[..., None]
+        err = np.abs(got[mine] - want)
+        assert (err <= tol).all(), f"sequence {s}: {new[s]} of {c}: {np.sum(err > tol)} of {err.size}, worst {np.max(err / tol):.2f} times the tolerance"
