@@ -553,3 +553,57 @@ def test_rows_whose_scale_is_subnormal():
     q, s = R.quantise_rows((np.float32(64) * up).astype(np.float32))
     got = api.w4a8_swiglu_quantize(_gpu(np.concatenate([np.full_like(up, 64), up], 1), A.BF16))
     assert np.array_equal(got[1].cpu().numpy().view(np.uint32), s.view(np.uint32)) and np.array_equal(got[0].cpu().numpy(), q)
+
+
+# -------------------------------------------------------------------------- rows that a block goes through more than once
+@pytest.mark.parametrize("dtype,K", [("float16", 4096), ("bfloat16", 4104), ("float16", 8200), ("bfloat16", 16392), ("int8", 8192), ("int8", 8208), ("int8", 16400), ("int8", 32784)])
+def test_dispatch_of_long_rows(dtype, K):
+    """More than 2048 pairs, rows of up to 512 pieces of 16 bytes and of more: one, two and three pieces a thread."""
+    import torch
+
+    rng = np.random.default_rng(K)
+    T, each, E = 750, 3, 5
+    ids = _route(rng, T, each, E, "absent")
+    offsets, places, tokens = R.dispatch(ids, E)
+    x = _gpu(rng.integers(-127, 128, (T, K + 16)).astype(np.int8)).to(getattr(torch, dtype))[:, :K]
+    out = torch.full((T * each, K), 99, dtype=x.dtype, device="cuda")
+    got = api.moe_dispatch(x, _gpu(ids), E, out=out)
+    n = len(tokens)
+    assert np.array_equal(got[2].cpu().numpy(), offsets) and np.array_equal(got[3].cpu().numpy(), places)
+    assert torch.equal(out[:n], x[_gpu(tokens)]) and (out[n:] == 99).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [2048, 2056, 4104, 8192, 8200, 12296])
+def test_gradients_of_long_rows(dtype, N):
+    """One to four pieces a thread, whole turns of the block and remainders; six rows a token, in two lots."""
+    rng = np.random.default_rng(N)
+    T, each, E = 23, 6, 7
+    offsets, places, tokens = R.dispatch(_route(rng, T, each, E, "absent"), E)
+    Y, grad, w = _draw(rng, (T * each, N), dtype), _draw(rng, (T, N), dtype), rng.random((T, each)).astype(np.float32)
+    gY, gw = api.moe_combine_backward(_rows(grad, dtype, 8), _rows(Y, dtype, 24), _gpu(places), _gpu(w), row_offsets=_gpu(offsets))
+    of_rows, of_weights, size = R.combine_backward(grad, Y, places, w, dtype)
+    assert np.array_equal(_np(gY)[:len(tokens)], of_rows[:len(tokens)]) and not gY[len(tokens):].any()
+    assert (np.abs(gw.double().cpu().numpy() - of_weights) <= (N / 256 + 16) * 2.0 ** -24 * size).all()
+    got = _np(api.moe_combine(_rows(Y, dtype, 24), _gpu(places), _gpu(w)))
+    want, size = R.combine(Y, places, w)
+    assert (np.abs(got - want) <= A.UNIT[dtype] * np.abs(want) * 1.001 + (each + 1) * 2.0 ** -24 * size + 2.0 ** -25).all()
+
+
+@pytest.mark.parametrize("T,N", [(700, 1000), (300, 4104)])
+def test_many_rows_that_no_expert_has_are_cleared(T, N):
+    """More of them than the blocks that clear take at once."""
+    import torch
+
+    rng = np.random.default_rng(T)
+    each = 4
+    ids = np.full((T, each), -1, dtype=np.int32)
+    ids[rng.integers(0, T, 9), rng.integers(0, each, 9)] = 2
+    offsets, places, tokens = R.dispatch(ids, 3)
+    assert (T * each - len(tokens)) * N // 8 > 256 * 512
+    Y, grad, w = _draw(rng, (T * each, N), A.BF16), _draw(rng, (T, N), A.BF16), rng.random((T, each)).astype(np.float32)
+    out = torch.full((T * each, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    gY, gw = api.moe_combine_backward(_gpu(grad, A.BF16), _gpu(Y, A.BF16), _gpu(places), _gpu(w), row_offsets=_gpu(offsets), out_Y=out)
+    of_rows, of_weights, size = R.combine_backward(grad, Y, places, w, A.BF16)
+    assert gY is out and np.array_equal(_np(gY)[:len(tokens)], of_rows[:len(tokens)]) and not gY[len(tokens):].any()
+    assert (np.abs(gw.double().cpu().numpy() - of_weights) <= (N / 256 + 16) * 2.0 ** -24 * size).all()
