@@ -398,7 +398,10 @@ int kv4_attention(int dtype, int n_seqs, int n_new, int Hq, int Hkv, int head_di
  * chunks and single tokens together.  out [total_q, Hq, head_dim]; a query that sees no key gets zeros, rows that belong to no
  * sequence are left alone.  A page number outside the cache, or a context longer than the table, gives NaN to the queries that see keys of it (and may to
  * others of the sequence).  total_q <= 2^28.  workspace as for w4a8_gemm (kv4_attention_chunks_workspace_size() bytes, 0 where there are many
- * queries; the first 32 KiB zeroed once; may be NULL: slower where few queries read many keys). */
+ * queries or more than 64 sequences; the first 32 KiB zeroed once; may be NULL: slower where few queries read many keys).
+ * Long contexts are cut into parts that run side by side only where the workspace is used: up to 64 sequences with fewer than 512 tiles (for each kv head
+ * (total_q * Hq / Hkv + 127 * n_seqs) / 128, the most that there can be).  Else one block goes through all keys of a tile: with 8/1 heads and one context of 32768 among single tokens over 1024, 64 sequences
+ * take 20 us and 65 of them 252.  (kv4_attention cuts the contexts of any number of sequences, for as many new tokens each.) */
 size_t kv4_attention_chunks_workspace_size(int n_seqs, int total_q, int Hq, int Hkv, int head_dim, int page_size, int table_width);
 int kv4_attention_chunks(int dtype, int n_seqs, int total_q, int Hq, int Hkv, int head_dim, const void *q, long long q_token, long long q_head,
                          const int *starts_q, const void *cache, int num_pages, int page_size, const int *block_table, int table_width,

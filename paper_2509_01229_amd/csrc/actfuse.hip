@@ -12,7 +12,7 @@
 // reduction over the block for the sum and the maximum, one barrier.
 //
 // A block takes a row, which stays in registers between the two passes over it; rows beyond 32768 elements are read twice.  Bound by memory:
-// 2 to 4 bytes in and 1 to 5 out an element (4093 rows of 8192 with residual and y in 56 us, 5.4 TB/s; the gate of 2039 rows of 28672 in 55, 5.3: the rate
+// 2 to 4 bytes in and 1 to 5 out an element (4093 rows of 8192 with residual and y in 56 us, 5.4 TB/s; the gate of 2039 rows of 28672 in 56.5, 5.2: the rate
 // of a large copy).  Few rows: a launch, a load, a reduction and a store one after the other, 2.5 us for one row of 4096.
 #include <algorithm>
 

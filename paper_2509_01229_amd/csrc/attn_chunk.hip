@@ -29,8 +29,9 @@
 // up to 4096, 32/8 heads, 51 -> 58, the 24 sequences 63.6 -> 64.5.  Tiles of more rows have one number a weight, as attn_prompt.hip's have: with two, chunks of FP16 take 2425 -> 3250 us
 // (two of 2048 over up to 16384), the 24 sequences 76.  Beside the rounding of BF16 results neither shows (1.67e-3 for 1.66e-3).
 //
-// Heads of 64 leave room for three blocks a CU: two chunks of 2048 over up to 16384, 64/8 heads, 1516 us, with two 1620.
-// Measured, heads of 128 (by machine; the clock is 1.95 to 2.2 GHz under this load): two chunks of 2048 over up to 16384, 64/8 heads, BF16, 2230 to 2470 us (820 to 900
+// Heads of 64 leave room for three blocks a CU: two chunks of 2048 over up to 16384, 64/8 heads, 1516 us, with two 1620.  They have half the products of heads of 128 and the same
+// softmax: vector instructions take 74% of a SIMD's cycles, MFMAs 34%, LDS 54% of a CU's (4096 tokens of two sequences over 16384 and 11253, BF16, 1206 us, 695 TFLOP/s).
+// Measured, heads of 128 (by machine; the clock is 1.95 to 2.2 GHz under this load): two chunks of 2048 over up to 16384, 64/8 heads, BF16, 2210 to 2470 us (820 to 910
 // TFLOP/s); 512 tokens over 1536 earlier ones, 32/8 heads, 39 us; 24 sequences with up to 4096 tokens, 640 new ones, 64; 17 of 517, 32/32 heads, 13.2.  A wave
 // takes 34 MFMAs (1088 cycles) and 250 vector instructions with 34 exponentials or the like (1330) for 32 rows and 64 keys, and 56 reads of LDS of 16 bytes a lane
 // (49% of its cycles, with the writes; none meet in a bank); two waves a SIMD make that in 2600 cycles each, so that MFMAs (43%) and vector instructions (51 to 57%) hardly overlap.  Tried, and slower or
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void kv4_chunks_kerne
 
     // The block's tile of rows and its part of the keys.  Up to 64 sequences: a lane looks at each; with a workspace (slots > 0) the tiles of a
     // sequence are cut into parts of at most `size` tiles of keys, the smallest size with which all parts run at a time.  More sequences are searched for
-    // as in attn_prompt.hip, and their keys are not cut.
+    // as in attn_prompt.hip, and their keys are not cut (8/1 heads, one context of 32768 among single tokens over 1024: 64 sequences 20 us, 65 252).
     const auto start_of = [&](int s) { return min(max(a.starts[s], 0), a.total_q); };
     const bool few = a.n_seqs <= kFew;
     int from = 0, len = 0, context = 0, mine = 0, parts = 1, upto = 0, all = a.tiles;

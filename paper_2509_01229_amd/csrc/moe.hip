@@ -10,8 +10,8 @@
 // them each token's block counts its own pairs' places itself and copies the row in the same launch.
 //
 // Bound by memory, or by the launch where there are few tokens.  Measured (by run; inputs that change): 8191 FP16 rows of 4096, 8 of 64 experts each, half of them here,
-// 75 to 83 us to sort (12.7 of them the places, the copy 4.8 TB/s), 60 to 69 us to bring back (BF16, 4.9 to 5.6 TB/s); gradients of 2047 tokens of 8192, 4 experts each, 62
-// to 63 us (4.8 TB/s).  16 tokens: kernels of 2.5 to 2.8 us.
+// 75 to 83 us to sort (12.9 of them the places, the copy 4.9 to 5.1 TB/s), 60 to 69 us to bring back (BF16, 4.9 to 5.6 TB/s); gradients of 2047 tokens of 8192, 4 experts each, 62
+// to 64 us (4.7 TB/s).  16 tokens: kernels of 2.5 to 2.8 us.
 #include <algorithm>
 
 #include "attn_common.h"

@@ -69,6 +69,13 @@ def test_chunks_workspace():
         assert size(*bad) == 0
 
 
+def test_chunks_workspace_of_many_sequences():
+    """None from 65 sequences on, or where the tiles of rows may be 512 (8 kv heads, four rows each: (4 + 127) * 62 / 128 = 63 tiles, of 63 sequences 64): keys are not cut there."""
+    size = api.lib().kv4_attention_chunks_workspace_size
+    assert size(64, 64, 8, 1, 128, 64, 600) > 32768 and size(65, 65, 8, 1, 128, 64, 600) == 0
+    assert size(62, 62, 32, 8, 128, 64, 600) > 32768 and size(63, 63, 32, 8, 128, 64, 600) == 0
+
+
 def test_tensors_on_the_cpu_are_refused():
     import torch
 
