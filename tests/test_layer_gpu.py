@@ -607,3 +607,34 @@ def test_many_rows_that_no_expert_has_are_cleared(T, N):
     of_rows, of_weights, size = R.combine_backward(grad, Y, places, w, A.BF16)
     assert gY is out and np.array_equal(_np(gY)[:len(tokens)], of_rows[:len(tokens)]) and not gY[len(tokens):].any()
     assert (np.abs(gw.double().cpu().numpy() - of_weights) <= (N / 256 + 16) * 2.0 ** -24 * size).all()
+
+
+def test_norm_and_swiglu_of_millions_of_rows():
+    """More rows than one launch takes, with strides of their own."""
+    M, K, period = 2 ** 21 + 70001, 16, 997
+    rng = np.random.default_rng(60)
+    x, res = _draw(rng, (period, K), A.F16), _draw(rng, (period, K), A.F16)
+    at = np.arange(M) % period
+    # (the rows repeat, the last of a period next to the first of the next: an odd number of them, so that no launch begins where one does)
+    many = lambda a, pad: _rows(a, A.F16, pad)[_gpu(at)] if not pad else _rows(a[at], A.F16, pad)  # noqa: E731
+    q, s, h, y = api.w4a8_norm_quantize(many(x, 8), residual=many(res, 0), want_y=True)
+    want = R.norm_quantise(x, res, None, 1e-6, A.F16)
+    for got, one in ((q, want[0]), (s, want[1]), (h, want[2]), (y, A.round_to(want[3], A.F16))):
+        assert np.array_equal(got.cpu().numpy().astype(np.float32), one.astype(np.float32)[at])
+    q, s = api.w4a8_swiglu_quantize(many(x, 8))
+    one_q, one_s = (t.cpu().numpy() for t in api.w4a8_swiglu_quantize(_gpu(x, A.F16)))
+    assert np.array_equal(q.cpu().numpy(), one_q[at]) and np.array_equal(s.cpu().numpy(), one_s[at])
+
+
+@pytest.mark.parametrize("T,each,E", [(3000, 1, 1), (70000, 2, 1), (40000, 1, 256), (2048, 1, 1), (1025, 2, 255)])
+def test_dispatch_of_one_expert_and_of_all(T, each, E):
+    """As many blocks an expert as there are, or one each."""
+    import torch
+
+    rng = np.random.default_rng(T)
+    ids = _route(rng, T, each, E, "absent")
+    offsets, places, tokens = R.dispatch(ids, E)
+    x = _gpu(rng.integers(-127, 128, (T, 16)).astype(np.int8))
+    rows, _, got_offsets, got_places = api.moe_dispatch(x, _gpu(ids), E)
+    assert np.array_equal(got_offsets.cpu().numpy(), offsets) and np.array_equal(got_places.cpu().numpy(), places)
+    assert torch.equal(rows[:len(tokens)], x[_gpu(tokens)])
