@@ -307,7 +307,7 @@ int moe_combine(int dtype, int tokens, int each, int rows, int N, const void *Y,
 /* The gradients of moe_combine from grad [tokens, N], that of out:
  *   grad_Y[places[t][j]] = weights[t][j] * grad[t], rounded once   ([rows, N], without gaps)
  *   grad_weights[t][j]   = grad[t] . Y[places[t][j]], FP32 (0 for a place outside the rows)
- * rows_used: device, one integer (moe_dispatch's row_offsets + n_experts): the rows of grad_Y from there on are zeroed; NULL: rows that no place names
+ * rows_used: device, one integer (moe_dispatch's row_offsets + n_experts): the rows of grad_Y from there on are zeroed (no place may be one of them); NULL: rows that no place names
  * are left alone.  No two pairs may have the same place (undefined which is kept, piece by piece).  tokens < 2^23. */
 int moe_combine_backward(int dtype, int tokens, int each, int rows, int N, const void *grad, long long grad_row, const void *Y, long long y_row,
                          const int *places, const float *weights, const int *rows_used, void *grad_Y, float *grad_weights, void *hip_stream);
